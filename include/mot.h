@@ -51,7 +51,8 @@ typedef enum {
   MOT_ERR_OOM = 5,           /* device allocation failed */
   MOT_ERR_CUDA = 6,          /* a CUDA runtime/driver call failed (incl. no GPU) */
   MOT_ERR_SEQ_LEN = 7,       /* a sequence length was outside [0, max_seq] */
-  MOT_ERR_TIMEOUT = 8        /* a bounded device-side pipeline wait gave up */
+  MOT_ERR_TIMEOUT = 8,       /* a bounded device-side pipeline wait gave up */
+  MOT_ERR_PAGES = 9          /* a paged cache: no room, or a slot or page out of range */
 } mot_status;
 
 typedef enum { MOT_BF16 = 0, MOT_FP32 = 1 } mot_dtype;
@@ -135,8 +136,8 @@ mot_status mot_translate_host(mot_handle h, const void* src_k, const void* src_v
 
 /*
  * Synchronise `stream`, then report and clear the sticky device status word:
- * MOT_ERR_SEQ_LEN, MOT_ERR_TIMEOUT, or MOT_OK. MOT_ERR_CUDA if the stream
- * reports an error.
+ * MOT_ERR_SEQ_LEN, MOT_ERR_TIMEOUT, MOT_ERR_PAGES, or MOT_OK. MOT_ERR_CUDA if
+ * the stream reports an error.
  */
 mot_status mot_get_device_status(mot_handle h, mot_stream_t stream);
 
@@ -442,6 +443,162 @@ mot_status mot_replay_attention(mot_handle h, int32_t layer, const void* q, cons
                                 int32_t batch, void* out, mot_stream_t stream);
 mot_status mot_replay_select(mot_handle h, const void* guide, const int32_t* seq_lens,
                              int32_t batch, int32_t* sel, mot_stream_t stream);
+
+/*
+ * Paged cache of the target model: what it works on after translation (the
+ * paper's prompt prefill and completion over a replayed or translated cache,
+ * App. E's many agents on one translated context). A sequence's positions lie
+ * in pages of P = page positions, which sequences share:
+ *   pools  k, v   [n_layers][n_pages][kv_heads][P][head_dim] (dtype)
+ *   table  int32  [max_seqs][max_pages]: page of positions j P .. j P + P - 1
+ *                 of the sequence in slot s, -1 behind its last
+ *   lens   int32  [max_seqs]: its positions; 0: the slot is empty
+ *   refs   int32  [n_pages]: sequences that hold the page; 0: it is free
+ * All of it is caller-owned device memory (pools 16-byte aligned), described
+ * by a mot_paged_cache. An empty cache is table = -1, lens = 0, refs = 0.
+ * A batch (mot_paged_batch) names n distinct slots and their new rows: entry i
+ * has the rows starts[i] .. starts[i + 1] - 1 (ascending, within 0 .. rows) of
+ * the call's row buffers, its last m = starts[i + 1] - starts[i] positions in
+ * order: row r is position lens - m + (r - starts[i]). `rows` (at most 2^26)
+ * and `max_chunk` (the most rows of an entry; rows where it is not known) are
+ * host numbers that bound the work.
+ *
+ * A step of a serving loop: mot_paged_reserve once, then per layer
+ * mot_paged_append and mot_paged_attention.
+ *
+ * Every call is asynchronous on `stream`, allocates nothing and may be captured
+ * into a graph; calls of one handle must not overlap on the device (shared
+ * workspace), nor may two calls that change one cache. What the device finds
+ * is reported by mot_get_device_status as MOT_ERR_PAGES:
+ *   - a change that cannot be made as a whole (reserve, fork, free: a slot
+ *     outside the table or named twice, a length beyond max_pages P or
+ *     2^30 - 1, not enough free pages, and what is said below) changes nothing,
+ *     and neither do the calls behind it that change a cache (reserve, fork,
+ *     free, compact, store, append) until the status has been read;
+ *   - lengths, starts, slots and table entries out of their ranges are held
+ *     inside them by the calls that read them: nothing outside the buffers is
+ *     touched, and the results of the entries concerned mean nothing.
+ * Errors: MOT_ERR_INVALID_ARG (NULL or misaligned pointers, sizes out of
+ * range, overlapping buffers, a handle of another kind), MOT_ERR_CUDA.
+ *
+ * Config: bf16 or fp32, head_dim in {64, 128}, page in {16, 32, 64, 128},
+ * q_heads a multiple of kv_heads and at most 16 times it, max_seqs <= 32768,
+ * n_pages * kv_heads * page <= 2^30, rot_dim a multiple of 16 (else
+ * MOT_ERR_UNSUPPORTED). A paged handle accepts these calls and the
+ * profiling, launch-count, device-status, test-hook and destroy calls.
+ */
+typedef struct {
+  int32_t n_layers, q_heads, kv_heads, head_dim;
+  int32_t page;        /* P */
+  int32_t n_pages;
+  int32_t max_seqs;    /* slots */
+  int32_t max_pages;   /* entries of a slot's table row */
+  int32_t rot_dim;     /* leading dimensions of a head that mot_paged_append rotates; 0: none */
+  int32_t rot_pairs;   /* 0: dimension i with i + rot_dim / 2; 1: 2 i with 2 i + 1 */
+  float rot_base;      /* pair i turns by position * rot_base^(-2 i / rot_dim) */
+  float norm_eps;
+  mot_dtype dtype;
+} mot_paged_config;
+
+typedef struct {
+  void* k;
+  void* v;
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+} mot_paged_cache;
+
+typedef struct {
+  const int32_t* seqs;     /* device [n]: slots */
+  const int32_t* starts;   /* device [n + 1] */
+  int32_t n;
+  int32_t rows;
+  int32_t max_chunk;
+} mot_paged_batch;
+
+mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out);
+
+/*
+ * Room for new positions: entry i's sequence becomes m_i longer, and the pages
+ * it lacks for that are taken. Taken pages (here and in mot_paged_fork) are the
+ * lowest free ones, in the order of the entries and of their positions. Their
+ * contents are what they were.
+ */
+mot_status mot_paged_reserve(mot_handle h, const mot_paged_cache* cache,
+                             const mot_paged_batch* batch, mot_stream_t stream);
+
+/*
+ * Sequence dst[i] (an empty slot) becomes a copy of src[i], i < n <= max_seqs:
+ * it shares src[i]'s full pages; of a last page that is partly filled it gets
+ * a copy of the filled positions, every layer, in a page of its own, so that
+ * both may grow. A slot may be the source of several; one that is a source
+ * and a destination is refused, as is a destination that is not empty.
+ */
+mot_status mot_paged_fork(mot_handle h, const mot_paged_cache* cache, const int32_t* src,
+                          const int32_t* dst, int32_t n, mot_stream_t stream);
+
+/* Sequences end: their slots are empty, and the pages that nobody else holds free. */
+mot_status mot_paged_free(mot_handle h, const mot_paged_cache* cache, const int32_t* seqs,
+                          int32_t n, mot_stream_t stream);
+
+/*
+ * The pages in use become the pages 0 .. c - 1, c their count (written to the
+ * device int32 *live where live is not NULL): the i-th lowest page in use at
+ * or above c moves to the i-th lowest free page below it. The pool above c can
+ * then be cut off or given away.
+ */
+mot_status mot_paged_compact(mot_handle h, const mot_paged_cache* cache, int32_t* live,
+                             mot_stream_t stream);
+
+/*
+ * Between a contiguous cache [n_layers][batch][kv_heads][max_seq][head_dim] (the
+ * target cache of mot_translate, or a source cache for it) and the pages of
+ * layers first_layer .. first_layer + n_layers - 1: batch entry i < n <= batch
+ * is slot seqs[i], positions 0 .. lens - 1 (at most max_seq). store writes
+ * the pages (of sequences that hold them alone), load the contiguous cache;
+ * other positions keep their contents.
+ */
+mot_status mot_paged_store(mot_handle h, const mot_paged_cache* cache, int32_t first_layer,
+                           int32_t n_layers, const int32_t* seqs, int32_t n, int32_t batch,
+                           int32_t max_seq, const void* src_k, const void* src_v,
+                           mot_stream_t stream);
+mot_status mot_paged_load(mot_handle h, const mot_paged_cache* cache, int32_t first_layer,
+                          int32_t n_layers, const int32_t* seqs, int32_t n, int32_t batch,
+                          int32_t max_seq, void* dst_k, void* dst_v, mot_stream_t stream);
+
+/*
+ * New queries, keys and values of one layer, in one pass: q [rows][q_heads]
+ * [head_dim] and k, v [rows][kv_heads][head_dim], rows q_stride, k_stride and
+ * v_stride elements apart (a multiple of 16 bytes; columns of one fused
+ * projection's output, say; 16-byte aligned). Each head of q and k is
+ *   normed, where q_norm / k_norm [head_dim] is given (NULL: not):
+ *     x rsqrt(mean(x^2) + norm_eps) w,
+ *   then rotated by its row's position (rot_dim > 0): a pair (a, b) becomes
+ *     (a cos t - b sin t, b cos t + a sin t), t as in mot_paged_config,
+ * in fp32 with angles exact for any position, and rounded once. q goes to
+ * q_out [rows][q_heads][head_dim] (which may be q itself where its rows are
+ * contiguous), k and v into the pages. Rows of no entry are not read or
+ * written.
+ */
+mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cache,
+                            const mot_paged_batch* batch, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            const void* q_norm, const void* k_norm, void* q_out,
+                            mot_stream_t stream);
+
+/*
+ * Attention of the batch's rows over one layer's pages: row r at position p of
+ * its sequence and query head h (key / value head h / (q_heads / kv_heads))
+ *   o = softmax over j <= p of q . k_j / sqrt(head_dim), applied to v_j
+ * q, out: [rows][q_heads][head_dim], 16-byte aligned. A row before position 0
+ * (a sequence shorter than its rows) sees nothing and is written as zeros;
+ * rows of no entry are not written. Positions behind p add nothing, whatever
+ * they hold, NaN and infinities included. One row per entry is a decoding
+ * step; any mixture with longer chunks is one call.
+ */
+mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cache* cache,
+                               const mot_paged_batch* batch, const void* q, void* out,
+                               mot_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -13,6 +13,7 @@
 
 #include "bt_internal.h"
 #include "mot_internal.h"
+#include "paged_internal.h"
 #include "replay_internal.h"
 
 using namespace mot;
@@ -170,6 +171,12 @@ struct mot_ctx {
   ReplayDims rd{};
   int32_t* rsel = nullptr;   // [B][N][S] selection workspace
   void* rvt = nullptr;       // [B][Hkv][d][N] bf16: V^T for the tensor-core full attention
+  // paged cache: kind 4
+  PagedDims pd{};
+  PagedWork pw{};
+  uint64_t* pfreq = nullptr;   // [rot_dim / 2] turns per position, in units of 2^-64
+  float* ppart = nullptr;      // partial results of the attention's split items
+  int32_t* pcount = nullptr;   // its arrival counters, zero between calls
   // Top-K routing (tensor-core path, 0 < top_k < E): token buckets per expert
   bool sparse_ok = false;   // the shapes support it
   int routing = 0;          // 0 dense compute with a zeroed gate, 1 token buckets
@@ -218,7 +225,8 @@ void free_all(mot_ctx* h) {
                   h->sp.row0, h->sp.plan, h->sp.pairs, h->sp.ltok, h->sp.lslot, h->sp.gatep,
                   h->sp.gate16p, h->sp.zp, h->sp.a2p, h->sp.ybuf, h->wkv, h->ahat,
                   h->proj_layer,
-                  h->rsel, h->rvt,
+                  h->rsel, h->rvt, h->pw.first, h->pw.take, h->pw.map, h->pw.moves, h->pw.count,
+                  h->pfreq, h->ppart, h->pcount,
                   h->n_tiles, h->status, h->counters, h->st_src[0], h->st_src[1], h->st_dst[0],
                   h->st_dst[1], h->st_len};
   for (void* p : ptrs)
@@ -520,6 +528,7 @@ const char* mot_status_string(mot_status s) {
     case MOT_ERR_CUDA: return "MOT_ERR_CUDA";
     case MOT_ERR_SEQ_LEN: return "MOT_ERR_SEQ_LEN";
     case MOT_ERR_TIMEOUT: return "MOT_ERR_TIMEOUT";
+    case MOT_ERR_PAGES: return "MOT_ERR_PAGES";
   }
   return "MOT_ERR_UNKNOWN";
 }
@@ -1159,7 +1168,7 @@ mot_status mot_create_h(const mot_h_config* cfg, mot_handle* out) {
 }
 
 mot_status mot_load_weights(mot_handle h, const void* host_blob, size_t bytes) {
-  if (!h || !host_blob) return MOT_ERR_INVALID_ARG;
+  if (!h || !host_blob || h->kind == 4) return MOT_ERR_INVALID_ARG;
   if (h->kind == 2) return bt_load(h, host_blob, bytes);
   const Dims& d = h->d;
   const size_t es = esize(d), gsz = group_elems(d);
@@ -1360,6 +1369,7 @@ mot_status mot_get_device_status(mot_handle h, mot_stream_t stream) {
   MOT_CUDA_TRY(cudaMemset(h->status, 0, 4));
   if (v & kStatusTimeout) return MOT_ERR_TIMEOUT;
   if (v & kStatusSeqLen) return MOT_ERR_SEQ_LEN;
+  if (v & (kStatusPages | kStatusPageUse)) return MOT_ERR_PAGES;
   return MOT_OK;
 }
 
@@ -1812,6 +1822,284 @@ mot_status mot_expert_usage(const int32_t* counts, int32_t n, double* cv2, doubl
         h -= p * std::log(p);
       }
   *entropy = h;
+  return MOT_OK;
+}
+
+// ---------------------------------------------------------------- paged cache
+
+mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
+  if (!out) return MOT_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!cfg) return MOT_ERR_INVALID_ARG;
+  const mot_paged_config& c = *cfg;
+  if (c.n_layers <= 0 || c.q_heads <= 0 || c.kv_heads <= 0 || c.head_dim <= 0 || c.page <= 0 ||
+      c.n_pages <= 0 || c.max_seqs <= 0 || c.max_pages <= 0 || c.q_heads % c.kv_heads ||
+      c.rot_dim < 0 || c.rot_dim > c.head_dim || c.rot_pairs < 0 || c.rot_pairs > 1 ||
+      !(c.norm_eps >= 0.f) || !std::isfinite(c.norm_eps) ||
+      (c.rot_dim > 0 && (!(c.rot_base >= 1.f) || !std::isfinite(c.rot_base))) ||
+      (c.dtype != MOT_BF16 && c.dtype != MOT_FP32))
+    return MOT_ERR_INVALID_ARG;
+  if ((c.head_dim != 64 && c.head_dim != 128) || c.page < 16 || c.page > 128 || (c.page & (c.page - 1)) ||
+      c.q_heads / c.kv_heads > kPagedMaxGroup || c.max_seqs > kPagedMaxSeqs || c.rot_dim % 16 ||
+      c.n_layers > 65535 || c.q_heads > 65535 || int64_t(c.n_pages) * c.kv_heads * c.page > (1 << 30))
+    return MOT_ERR_UNSUPPORTED;
+  mot_ctx* h = new (std::nothrow) mot_ctx();
+  if (!h) return MOT_ERR_OOM;
+  h->kind = 4;
+  PagedDims& d = h->pd;
+  d = PagedDims{c.n_layers, c.q_heads, c.kv_heads, c.head_dim, c.page, 0, c.n_pages, c.max_seqs, c.max_pages,
+                c.rot_dim, c.rot_pairs, c.norm_eps, c.dtype == MOT_BF16 ? 0 : 1};
+  while ((1 << d.lp) < d.P) ++d.lp;
+  int cc_major = 0, cc_minor = 0;
+  if (cudaGetDevice(&h->device) != cudaSuccess ||
+      cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device) != cudaSuccess ||
+      cudaDeviceGetAttribute(&cc_major, cudaDevAttrComputeCapabilityMajor, h->device) != cudaSuccess ||
+      cudaDeviceGetAttribute(&cc_minor, cudaDevAttrComputeCapabilityMinor, h->device) != cudaSuccess) {
+    cudaGetLastError();
+    delete h;
+    return MOT_ERR_CUDA;
+  }
+  if (cc_major != 10 || cc_minor != 3) {
+    delete h;
+    return MOT_ERR_UNSUPPORTED;
+  }
+  // pair i turns by base^(-2 i / rot) / (2 pi) of a turn per position
+  uint64_t freq[64] = {};
+  for (int i = 0; i < d.rot / 2; ++i) {
+    const long double turns = std::pow(static_cast<long double>(c.rot_base), -2.0L * i / d.rot) /
+                              6.283185307179586476925286766559005768L;
+    freq[i] = static_cast<uint64_t>(std::ldexp(turns, 64) + 0.5L);   // at most 1 / (2 pi) of 2^64
+  }
+  const size_t pages = d.n_pages, counters = size_t(paged_counters(h->num_sms)) * 4;
+  if (cudaMalloc(&h->pw.first, (size_t(d.max_seqs) + 1) * 4) != cudaSuccess ||
+      cudaMalloc(&h->pw.take, pages * 4) != cudaSuccess || cudaMalloc(&h->pw.map, pages * 4) != cudaSuccess ||
+      cudaMalloc(&h->pw.moves, std::max<size_t>(pages, d.max_seqs) * 8) != cudaSuccess ||
+      cudaMalloc(&h->pw.count, 16) != cudaSuccess || cudaMalloc(&h->pfreq, sizeof(freq)) != cudaSuccess ||
+      cudaMalloc(&h->ppart, paged_part_floats(d, h->num_sms) * 4) != cudaSuccess ||
+      cudaMalloc(&h->pcount, counters) != cudaSuccess || cudaMalloc(&h->status, 16) != cudaSuccess) {
+    cudaGetLastError();
+    free_all(h);
+    delete h;
+    return MOT_ERR_OOM;
+  }
+  if (cudaMemset(h->pw.map, 0, pages * 4) != cudaSuccess || cudaMemset(h->pw.count, 0, 16) != cudaSuccess ||
+      cudaMemset(h->pcount, 0, counters) != cudaSuccess || cudaMemset(h->status, 0, 16) != cudaSuccess ||
+      cudaMemcpy(h->pfreq, freq, sizeof(freq), cudaMemcpyHostToDevice) != cudaSuccess ||
+      cudaDeviceSynchronize() != cudaSuccess) {
+    cudaGetLastError();
+    free_all(h);
+    delete h;
+    return MOT_ERR_CUDA;
+  }
+  h->pw.status = h->status;
+  h->weights_loaded = true;   // nothing to load
+  *out = h;
+  return MOT_OK;
+}
+
+namespace {
+
+size_t paged_es(const PagedDims& d) { return d.dtype ? 4 : 2; }
+size_t paged_layer_bytes(const PagedDims& d) { return size_t(d.n_pages) * d.H * d.P * d.d * paged_es(d); }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+mot_status paged_args(mot_handle h, const mot_paged_cache* c, PagedCache& pc) {
+  if (!h || h->kind != 4 || !c) return MOT_ERR_INVALID_ARG;
+  if (!c->k || !c->v || !c->table || !c->lens || !c->refs || !aligned16(c->k) || !aligned16(c->v) ||
+      !aligned4(c->table) || !aligned4(c->lens) || !aligned4(c->refs))
+    return MOT_ERR_INVALID_ARG;
+  const size_t bytes = paged_layer_bytes(h->pd) * h->pd.L;
+  if (overlap(c->k, bytes, c->v, bytes)) return MOT_ERR_INVALID_ARG;
+  pc = PagedCache{c->k, c->v, c->table, c->lens, c->refs};
+  return MOT_OK;
+}
+
+// Whether [p, p + n) meets the pools.
+bool meets_pools(const mot_ctx* h, const PagedCache& c, const void* p, size_t n) {
+  const size_t bytes = paged_layer_bytes(h->pd) * h->pd.L;
+  return overlap(p, n, c.k, bytes) || overlap(p, n, c.v, bytes);
+}
+
+mot_status paged_batch_args(mot_handle h, const mot_paged_batch* b, PagedBatch& pb) {
+  if (!b || b->n < 0 || b->n > h->pd.max_seqs || b->rows < 0 || b->rows > (1 << 26) || b->max_chunk < 0)
+    return MOT_ERR_INVALID_ARG;
+  if (b->n > 0 && (!b->seqs || !b->starts || !aligned4(b->seqs) || !aligned4(b->starts)))
+    return MOT_ERR_INVALID_ARG;
+  pb = PagedBatch{b->seqs, b->starts, b->n, b->rows};
+  return MOT_OK;
+}
+
+mot_status paged_slots(mot_handle h, const int32_t* seqs, int32_t n) {
+  if (n < 0 || n > h->pd.max_seqs || (n > 0 && (!seqs || !aligned4(seqs)))) return MOT_ERR_INVALID_ARG;
+  return MOT_OK;
+}
+
+mot_status paged_copy(mot_handle h, const mot_paged_cache* cache, const PagedCopy& p, cudaStream_t st) {
+  PagedCache c;
+  mot_status r = paged_args(h, cache, c);
+  if (r != MOT_OK) return r;
+  const PagedDims& d = h->pd;
+  if ((r = paged_slots(h, p.seqs, p.n)) != MOT_OK) return r;
+  if (p.first < 0 || p.n_layers <= 0 || p.first > d.L - p.n_layers || p.B < p.n || p.B <= 0 || p.S <= 0)
+    return MOT_ERR_INVALID_ARG;
+  if (!p.k || !p.v || !aligned16(p.k) || !aligned16(p.v)) return MOT_ERR_INVALID_ARG;
+  const size_t bytes = size_t(p.n_layers) * p.B * d.H * size_t(p.S) * d.d * paged_es(d);
+  if (overlap(p.k, bytes, p.v, bytes) || meets_pools(h, c, p.k, bytes) || meets_pools(h, c, p.v, bytes))
+    return MOT_ERR_INVALID_ARG;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
+  if (p.n == 0) return MOT_OK;
+  MOT_CUDA_TRY(timed(h, p.store ? "paged_store" : "paged_load", st,
+                     [&] { return launch_paged_copy(d, c, p, h->pw, h->num_sms, st); }));
+  return MOT_OK;
+}
+
+}  // namespace
+
+mot_status mot_paged_reserve(mot_handle h, const mot_paged_cache* cache, const mot_paged_batch* batch,
+                             mot_stream_t stream) {
+  NvtxRange range("mot_paged_reserve");
+  PagedCache c;
+  PagedBatch b;
+  mot_status r = paged_args(h, cache, c);
+  if (r != MOT_OK || (r = paged_batch_args(h, batch, b)) != MOT_OK) return r;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
+  if (b.n == 0) return MOT_OK;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  MOT_CUDA_TRY(timed(h, "paged_reserve", st, [&] { return launch_paged_reserve(h->pd, c, b, h->pw, st); }));
+  return MOT_OK;
+}
+
+mot_status mot_paged_fork(mot_handle h, const mot_paged_cache* cache, const int32_t* src, const int32_t* dst,
+                          int32_t n, mot_stream_t stream) {
+  NvtxRange range("mot_paged_fork");
+  PagedCache c;
+  mot_status r = paged_args(h, cache, c);
+  if (r != MOT_OK || (r = paged_slots(h, src, n)) != MOT_OK || (r = paged_slots(h, dst, n)) != MOT_OK) return r;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
+  if (n == 0) return MOT_OK;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  MOT_CUDA_TRY(timed(h, "paged_fork_plan", st,
+                     [&] { return launch_paged_fork_plan(h->pd, c, src, dst, n, h->pw, st); }));
+  MOT_CUDA_TRY(timed(h, "paged_fork", st, [&] { return launch_paged_fork(h->pd, c, src, dst, n, h->pw, st); }));
+  return MOT_OK;
+}
+
+mot_status mot_paged_free(mot_handle h, const mot_paged_cache* cache, const int32_t* seqs, int32_t n,
+                          mot_stream_t stream) {
+  NvtxRange range("mot_paged_free");
+  PagedCache c;
+  mot_status r = paged_args(h, cache, c);
+  if (r != MOT_OK || (r = paged_slots(h, seqs, n)) != MOT_OK) return r;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
+  if (n == 0) return MOT_OK;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  MOT_CUDA_TRY(timed(h, "paged_free", st,
+                     [&] { return launch_paged_free(h->pd, c, seqs, n, h->pw, h->num_sms, st); }));
+  return MOT_OK;
+}
+
+mot_status mot_paged_compact(mot_handle h, const mot_paged_cache* cache, int32_t* live, mot_stream_t stream) {
+  NvtxRange range("mot_paged_compact");
+  PagedCache c;
+  mot_status r = paged_args(h, cache, c);
+  if (r != MOT_OK) return r;
+  if (!aligned4(live)) return MOT_ERR_INVALID_ARG;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  MOT_CUDA_TRY(timed(h, "paged_compact_plan", st,
+                     [&] { return launch_paged_compact_plan(h->pd, c, live, h->pw, st); }));
+  MOT_CUDA_TRY(timed(h, "paged_compact", st,
+                     [&] { return launch_paged_compact(h->pd, c, h->pw, h->num_sms, st); }));
+  return MOT_OK;
+}
+
+mot_status mot_paged_store(mot_handle h, const mot_paged_cache* cache, int32_t first_layer, int32_t n_layers,
+                           const int32_t* seqs, int32_t n, int32_t batch, int32_t max_seq, const void* src_k,
+                           const void* src_v, mot_stream_t stream) {
+  NvtxRange range("mot_paged_store");
+  const PagedCopy p{seqs, n, first_layer, n_layers, batch, max_seq, const_cast<void*>(src_k),
+                    const_cast<void*>(src_v), true};
+  return paged_copy(h, cache, p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+mot_status mot_paged_load(mot_handle h, const mot_paged_cache* cache, int32_t first_layer, int32_t n_layers,
+                          const int32_t* seqs, int32_t n, int32_t batch, int32_t max_seq, void* dst_k,
+                          void* dst_v, mot_stream_t stream) {
+  NvtxRange range("mot_paged_load");
+  const PagedCopy p{seqs, n, first_layer, n_layers, batch, max_seq, dst_k, dst_v, false};
+  return paged_copy(h, cache, p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cache,
+                            const mot_paged_batch* batch, const void* q, int64_t q_stride, const void* k,
+                            int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm,
+                            const void* k_norm, void* q_out, mot_stream_t stream) {
+  NvtxRange range("mot_paged_append");
+  PagedCache c;
+  PagedAppend p{};
+  mot_status r = paged_args(h, cache, c);
+  if (r != MOT_OK || (r = paged_batch_args(h, batch, p.b)) != MOT_OK) return r;
+  const PagedDims& d = h->pd;
+  if (layer < 0 || layer >= d.L) return MOT_ERR_INVALID_ARG;
+  if (!q || !k || !v || !q_out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
+      !aligned16(q_norm) || !aligned16(k_norm))
+    return MOT_ERR_INVALID_ARG;
+  const int64_t es = int64_t(paged_es(d)), unit = 16 / es, qw = int64_t(d.Hq) * d.d, kw = int64_t(d.H) * d.d;
+  if (q_stride < qw || k_stride < kw || v_stride < kw || q_stride > INT32_MAX || k_stride > INT32_MAX ||
+      v_stride > INT32_MAX || q_stride % unit || k_stride % unit || v_stride % unit)
+    return MOT_ERR_INVALID_ARG;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
+  if (p.b.rows == 0 || p.b.n == 0) return MOT_OK;
+  auto span = [&](int64_t stride, int64_t w) { return size_t((int64_t(p.b.rows) - 1) * stride + w) * es; };
+  const size_t qb = span(q_stride, qw), kb = span(k_stride, kw), vb = span(v_stride, kw), ob = span(qw, qw);
+  if ((overlap(q_out, ob, q, qb) && !(q_out == q && q_stride == qw)) || overlap(q_out, ob, k, kb) ||
+      overlap(q_out, ob, v, vb) || meets_pools(h, c, q, qb) || meets_pools(h, c, k, kb) ||
+      meets_pools(h, c, v, vb) || meets_pools(h, c, q_out, ob))
+    return MOT_ERR_INVALID_ARG;
+  p.layer = layer;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.q_norm = q_norm;
+  p.k_norm = k_norm;
+  p.freq = h->pfreq;
+  p.q_out = q_out;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  MOT_CUDA_TRY(timed(h, "paged_append", st,
+                     [&] { return launch_paged_append(d, c, p, h->pw, h->num_sms, st); }));
+  return MOT_OK;
+}
+
+mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cache* cache,
+                               const mot_paged_batch* batch, const void* q, void* out, mot_stream_t stream) {
+  NvtxRange range("mot_paged_attention");
+  PagedCache c;
+  PagedAttnArgs a{};
+  mot_status r = paged_args(h, cache, c);
+  if (r != MOT_OK || (r = paged_batch_args(h, batch, a.b)) != MOT_OK) return r;
+  const PagedDims& d = h->pd;
+  if (layer < 0 || layer >= d.L || !q || !out || !aligned16(q) || !aligned16(out)) return MOT_ERR_INVALID_ARG;
+  const size_t qb = size_t(a.b.rows) * d.Hq * d.d * paged_es(d);
+  if (overlap(out, qb, q, qb) || meets_pools(h, c, out, qb)) return MOT_ERR_INVALID_ARG;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
+  if (a.b.rows == 0 || a.b.n == 0) return MOT_OK;
+  const size_t at = paged_layer_bytes(d) * size_t(layer);
+  a.d = d;
+  a.q = q;
+  a.out = out;
+  a.k = static_cast<const char*>(c.k) + at;
+  a.v = static_cast<const char*>(c.v) + at;
+  a.table = c.table;
+  a.lens = c.lens;
+  a.part = h->ppart;
+  a.count = h->pcount;
+  a.status = h->status;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  MOT_CUDA_TRY(timed(h, "paged_attn", st,
+                     [&] { return launch_paged_attn(a, h->num_sms, batch->max_chunk, st); }));
   return MOT_OK;
 }
 

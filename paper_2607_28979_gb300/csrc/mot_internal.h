@@ -67,7 +67,9 @@ constexpr int kTileM = 128;   // tokens per token tile (rows of one MMA tile)
 constexpr int kMaxE = 16;     // translators per (layer, K/V) group
 
 // Sticky device status bits, OR-ed into the handle's status word.
-enum : int32_t { kStatusSeqLen = 1, kStatusTimeout = 2 };
+// kStatusPages: a change of a paged cache was refused (further ones do nothing until the word is read);
+// kStatusPageUse: a batch or a table entry was out of range and was held inside it.
+enum : int32_t { kStatusSeqLen = 1, kStatusTimeout = 2, kStatusPages = 4, kStatusPageUse = 8 };
 
 // One 128-token tile of the ragged batch: batch entry b, positions
 // [s0, s0 + rows).

@@ -30,7 +30,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 # ---------------------------------------------------------------- C types
 
 MOT_OK, MOT_ERR_INVALID_ARG, MOT_ERR_UNSUPPORTED, MOT_ERR_NO_WEIGHTS, MOT_ERR_WEIGHTS_SIZE, \
-    MOT_ERR_OOM, MOT_ERR_CUDA, MOT_ERR_SEQ_LEN, MOT_ERR_TIMEOUT = range(9)
+    MOT_ERR_OOM, MOT_ERR_CUDA, MOT_ERR_SEQ_LEN, MOT_ERR_TIMEOUT, MOT_ERR_PAGES = range(10)
 MOT_BF16, MOT_FP32 = 0, 1
 
 
@@ -65,6 +65,26 @@ class mot_replay_config(ctypes.Structure):
                 ("max_seq", ctypes.c_int32), ("top_s", ctypes.c_int32), ("n_full", ctypes.c_int32)]
 
 
+class mot_paged_config(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("rot_pairs", ctypes.c_int32),
+                ("rot_base", ctypes.c_float), ("norm_eps", ctypes.c_float),
+                ("dtype", ctypes.c_int32)]
+
+
+class mot_paged_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class mot_paged_batch(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("n", ctypes.c_int32),
+                ("rows", ctypes.c_int32), ("max_chunk", ctypes.c_int32)]
+
+
 class mot_kernel_stat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double)]
@@ -73,6 +93,8 @@ class mot_kernel_stat(ctypes.Structure):
 _H = ctypes.c_void_p
 _P = ctypes.c_void_p
 _S = ctypes.c_int
+_I = ctypes.c_int32
+_CACHE, _BATCH = ctypes.POINTER(mot_paged_cache), ctypes.POINTER(mot_paged_batch)
 
 _SIGS = {
     "mot_create": [ctypes.POINTER(mot_config), ctypes.POINTER(ctypes.c_void_p)],
@@ -106,6 +128,16 @@ _SIGS = {
     "mot_create_replay": [ctypes.POINTER(mot_replay_config), ctypes.POINTER(ctypes.c_void_p)],
     "mot_replay_attention": [_H, ctypes.c_int32, _P, _P, _P, _P, _P, ctypes.c_int32, _P, _P],
     "mot_replay_select": [_H, _P, _P, ctypes.c_int32, _P, _P],
+    "mot_create_paged": [ctypes.POINTER(mot_paged_config), ctypes.POINTER(ctypes.c_void_p)],
+    "mot_paged_reserve": [_H, _CACHE, _BATCH, _P],
+    "mot_paged_fork": [_H, _CACHE, _P, _P, _I, _P],
+    "mot_paged_free": [_H, _CACHE, _P, _I, _P],
+    "mot_paged_compact": [_H, _CACHE, _P, _P],
+    "mot_paged_store": [_H, _CACHE, _I, _I, _P, _I, _I, _I, _P, _P, _P],
+    "mot_paged_load": [_H, _CACHE, _I, _I, _P, _I, _I, _I, _P, _P, _P],
+    "mot_paged_append": [_H, _I, _CACHE, _BATCH, _P, ctypes.c_int64, _P, ctypes.c_int64, _P,
+                         ctypes.c_int64, _P, _P, _P, _P],
+    "mot_paged_attention": [_H, _I, _CACHE, _BATCH, _P, _P, _P],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -259,6 +291,108 @@ def mot_replay_attention(h: Handle, layer: int, q, k, v, guide, seq_lens, batch:
 def mot_replay_select(h: Handle, guide, seq_lens, batch: int, sel, stream=None) -> None:
     _check(_lib.mot_replay_select(h.ptr, _addr(guide), _addr(seq_lens), int(batch), _addr(sel),
                                   _stream(stream)), "mot_replay_select")
+
+
+def make_paged_config(n_layers, q_heads, kv_heads, head_dim, page, n_pages, max_seqs, max_pages,
+                      rot_dim=0, rot_pairs=False, rot_base=1e4, norm_eps=1e-6, dtype="bf16"):
+    return mot_paged_config(n_layers, q_heads, kv_heads, head_dim, page, n_pages, max_seqs,
+                            max_pages, rot_dim, int(bool(rot_pairs)), rot_base, norm_eps,
+                            MOT_BF16 if dtype in ("bf16", MOT_BF16) else MOT_FP32)
+
+
+def paged_cache(k, v, table, lens, refs) -> mot_paged_cache:
+    """The arrays of a paged cache (contiguous device tensors): pools k, v
+    [n_layers][n_pages][kv_heads][page][head_dim], int32 table [max_seqs][max_pages], lens
+    [max_seqs] and refs [n_pages]. The struct keeps the tensors."""
+    c = mot_paged_cache(*[_addr(x) for x in (k, v, table, lens, refs)])
+    c._keep = (k, v, table, lens, refs)
+    return c
+
+
+def paged_batch(seqs, starts, n: int, rows: int, max_chunk: Optional[int] = None) -> mot_paged_batch:
+    """n slots (device int32 ``seqs`` [n]) with their new rows (device int32 ``starts`` [n + 1]);
+    ``max_chunk``: the most rows of one (``rows`` where it is not known)."""
+    b = mot_paged_batch(_addr(seqs), _addr(starts), int(n), int(rows),
+                        int(rows if max_chunk is None else max_chunk))
+    b._keep = (seqs, starts)
+    return b
+
+
+def mot_create_paged(cfg: mot_paged_config) -> Handle:
+    out = ctypes.c_void_p()
+    _check(_lib.mot_create_paged(ctypes.byref(cfg), ctypes.byref(out)), "mot_create_paged")
+    return Handle(out.value, 0)
+
+
+def mot_paged_reserve(h: Handle, cache: mot_paged_cache, batch: mot_paged_batch, stream=None) -> None:
+    _check(_lib.mot_paged_reserve(h.ptr, ctypes.byref(cache), ctypes.byref(batch), _stream(stream)),
+           "mot_paged_reserve")
+
+
+def mot_paged_fork(h: Handle, cache: mot_paged_cache, src, dst, n: int, stream=None) -> None:
+    _check(_lib.mot_paged_fork(h.ptr, ctypes.byref(cache), _addr(src), _addr(dst), int(n),
+                               _stream(stream)), "mot_paged_fork")
+
+
+def mot_paged_free(h: Handle, cache: mot_paged_cache, seqs, n: int, stream=None) -> None:
+    _check(_lib.mot_paged_free(h.ptr, ctypes.byref(cache), _addr(seqs), int(n), _stream(stream)),
+           "mot_paged_free")
+
+
+def mot_paged_compact(h: Handle, cache: mot_paged_cache, live=None, stream=None) -> None:
+    _check(_lib.mot_paged_compact(h.ptr, ctypes.byref(cache), _addr(live), _stream(stream)),
+           "mot_paged_compact")
+
+
+def _contiguous_shape(k, v):
+    """(n_layers, batch, max_seq) of contiguous caches [n_layers][batch][kv_heads][max_seq][head_dim]."""
+    if tuple(k.shape) != tuple(v.shape) or len(k.shape) != 5:
+        raise ValueError("contiguous caches are [n_layers][batch][kv_heads][max_seq][head_dim], K and V alike")
+    for x in (k, v):
+        if hasattr(x, "is_contiguous") and not x.is_contiguous():
+            raise ValueError("contiguous caches are wanted")
+    return int(k.shape[0]), int(k.shape[1]), int(k.shape[3])
+
+
+def mot_paged_store(h: Handle, cache: mot_paged_cache, seqs, n: int, src_k, src_v, first_layer: int = 0,
+                    stream=None) -> None:
+    """Tensors src_k, src_v [n_layers][batch][kv_heads][max_seq][head_dim] into the pages of the
+    slots ``seqs``, layers first_layer ..."""
+    layers, batch, max_seq = _contiguous_shape(src_k, src_v)
+    _check(_lib.mot_paged_store(h.ptr, ctypes.byref(cache), int(first_layer), layers, _addr(seqs), int(n),
+                                batch, max_seq, _addr(src_k), _addr(src_v), _stream(stream)),
+           "mot_paged_store")
+
+
+def mot_paged_load(h: Handle, cache: mot_paged_cache, seqs, n: int, dst_k, dst_v, first_layer: int = 0,
+                   stream=None) -> None:
+    """The pages of the slots ``seqs`` into tensors [n_layers][batch][kv_heads][max_seq][head_dim]."""
+    layers, batch, max_seq = _contiguous_shape(dst_k, dst_v)
+    _check(_lib.mot_paged_load(h.ptr, ctypes.byref(cache), int(first_layer), layers, _addr(seqs), int(n),
+                               batch, max_seq, _addr(dst_k), _addr(dst_v), _stream(stream)),
+           "mot_paged_load")
+
+
+def _row_stride(x, what: str) -> int:
+    if x.dim() != 3 or x.stride(2) != 1 or x.stride(1) != x.shape[2]:
+        raise ValueError(f"{what}: [rows][heads][head_dim] with contiguous rows is wanted")
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * x.shape[2])
+
+
+def mot_paged_append(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, k, v, q_out,
+                     q_norm=None, k_norm=None, stream=None) -> None:
+    """Tensors q, k, v [rows][heads][head_dim], whose rows may lie apart (columns of a fused
+    projection); q_out [rows][q_heads][head_dim] contiguous."""
+    _check(_lib.mot_paged_append(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), _addr(q),
+                                 _row_stride(q, "q"), _addr(k), _row_stride(k, "k"), _addr(v),
+                                 _row_stride(v, "v"), _addr(q_norm), _addr(k_norm), _addr(q_out),
+                                 _stream(stream)), "mot_paged_append")
+
+
+def mot_paged_attention(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, out,
+                        stream=None) -> None:
+    _check(_lib.mot_paged_attention(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), _addr(q),
+                                    _addr(out), _stream(stream)), "mot_paged_attention")
 
 
 def mot_create(cfg: mot_config) -> Handle:
