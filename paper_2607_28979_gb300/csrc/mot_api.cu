@@ -2097,7 +2097,18 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.part = h->ppart;
   a.count = h->pcount;
   a.status = h->status;
+  a.wait_limit = h->wait_limit;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (paged_fmha_takes(d, batch->max_chunk)) {
+    CUtensorMap tmK{}, tmV{};
+    const uint64_t dims[2] = {uint64_t(d.d), uint64_t(d.n_pages) * d.H * d.P};
+    const uint64_t st_b[1] = {uint64_t(d.d) * 2};
+    const uint32_t box[2] = {64, uint32_t(d.P)};
+    if (!encode_bf16(&tmK, a.k, 2, dims, st_b, box) || !encode_bf16(&tmV, a.v, 2, dims, st_b, box))
+      return MOT_ERR_CUDA;
+    MOT_CUDA_TRY(timed(h, "paged_fmha", st, [&] { return launch_paged_fmha(a, tmK, tmV, h->num_sms, st); }));
+    return MOT_OK;
+  }
   MOT_CUDA_TRY(timed(h, "paged_attn", st,
                      [&] { return launch_paged_attn(a, h->num_sms, batch->max_chunk, st); }));
   return MOT_OK;

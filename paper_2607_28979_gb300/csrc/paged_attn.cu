@@ -228,15 +228,17 @@ cudaError_t launch_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
 
 }  // namespace
 
-size_t paged_part_floats(const PagedDims& d, int num_sms) { return size_t(num_sms) * 4 * 2 * 64 * (d.d + 2); }
+// Two places per CTA: 256 rows with one CTA per SM, fewer rows with more.
+size_t paged_part_floats(const PagedDims& d, int num_sms) { return size_t(num_sms) * 2 * 256 * (d.d + 2); }
 int paged_counters(int num_sms) { return num_sms * 4; }
+bool paged_fmha_takes(const PagedDims& d, int max_chunk) {
+  return d.dtype == 0 && int64_t(max_chunk) * (d.Hq / d.H) > 16;
+}
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st) {
   const bool few = int64_t(max_chunk) * (a.d.Hq / a.d.H) <= 16;
-  if (a.d.dtype == 0) {
-    if (a.d.d == 64) return few ? launch_simt<uint16_t, 64, 16>(a, num_sms, st) : launch_simt<uint16_t, 64, 64>(a, num_sms, st);
-    return few ? launch_simt<uint16_t, 128, 16>(a, num_sms, st) : launch_simt<uint16_t, 128, 64>(a, num_sms, st);
-  }
+  if (a.d.dtype == 0)   // chunks: launch_paged_fmha
+    return a.d.d == 64 ? launch_simt<uint16_t, 64, 16>(a, num_sms, st) : launch_simt<uint16_t, 128, 16>(a, num_sms, st);
   if (a.d.d == 64) return few ? launch_simt<float, 64, 16>(a, num_sms, st) : launch_simt<float, 64, 64>(a, num_sms, st);
   return few ? launch_simt<float, 128, 16>(a, num_sms, st) : launch_simt<float, 128, 64>(a, num_sms, st);
 }

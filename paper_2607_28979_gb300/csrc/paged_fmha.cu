@@ -1,0 +1,526 @@
+// Attention of chunks of new tokens over a paged cache on the tensor cores of sm_103a (bf16).
+//
+//   paged_fmha_kernel   persistent, one CTA per SM over its run of key tiles (paged_common.cuh). An
+//                       item is 256 rows (new token, query head of the group) of one key/value head, as
+//                       two streams of 128 rows whose softmax and products alternate, over tiles of
+//                       128 keys:
+//                         warp 0     TMA: a tile's pages, keys and values as they lie in the pool, a
+//                                    lane per (page, 64 dimensions), into rings of 2 and 3 tiles;
+//                         warp 1     S_i = Q_i K^T (Q_i and K from shared memory) and O_i += P_i V (P_i
+//                                    from TMEM, over S_i; V's rows are keys, so it is an MN-major
+//                                    operand and needs no transpose), i = 0, 1 in turn;
+//                         warps 2-3  values before the second product: rows behind the sequence's
+//                                    end become zeros, and in tiles that some rows see only in part
+//                                    infinite and NaN values do too (a masked key's weight is 0, and 0
+//                                    times them would not be); their keys are noted, and the rows
+//                                    that do see them add them at the end;
+//                         warps 4-11 one thread per row: queries into shared memory, scores from TMEM,
+//                                    running maximum (base 2; raised, and O and the sum rescaled, only
+//                                    when a tile exceeds it by 2^8) and sum, P as bf16 pairs into TMEM
+//                                    in two halves, so that the second product starts on the first
+//                                    while the other is made; at the end O from TMEM to the output or
+//                                    to the piece's partial results.
+//                       Every wait is bounded; on a timeout the roles unwind, copies and MMAs in flight
+//                       are drained, TMEM is freed and kStatusTimeout is raised.
+#include "paged_common.cuh"
+
+namespace mot {
+namespace {
+
+template <int D>
+struct Pf {
+  static constexpr int kBM = 256, kTK = 128;
+  static constexpr int kBlk = 128 * 128;               // 128 rows of 64 elements
+  static constexpr int kTile = D / 64 * kBlk;          // a tile of keys, of values or of queries
+  static constexpr int kNK = 2, kNV = 3;               // tiles in flight
+  static constexpr int kThreads = 32 * 12;
+  static constexpr int kBytes = (2 + kNK + kNV) * kTile;
+  static constexpr int kSmem = kBytes + 1024 + 1024;   // barriers and notes; alignment
+  static constexpr int kO = 256;                       // TMEM: S at 0 and 128, O at 256 and 256 + D
+};
+static_assert(Pf<128>::kSmem <= 232448, "shared memory budget");
+static_assert(Pf<128>::kO + 2 * 128 <= 512, "TMEM columns");
+
+// Barriers and what the roles leave for one another.
+struct PfShared {
+  uint64_t q_ready[2], s_full[2], p_half[2][2], pv_done[2];
+  uint64_t k_full[2], k_empty[2], v_full[3], v_ready[3], v_empty[3], drain;
+  uint32_t tmem;
+  int32_t abort;
+  int32_t last;              // this CTA joins the item
+  int32_t pieces;            // pieces finished
+  uint32_t notes[4][4][4];   // [piece & 3][tile of the masked ones][128 keys]: values that are not finite
+};
+static_assert(sizeof(PfShared) <= 1024, "barrier block");
+
+// Tiles of an item that some of its rows see only in part: [first, units).
+__device__ __forceinline__ int first_masked(const PagedSeq& s, int G, int row0) {
+  const int p = s.len - s.m + row0 / G;
+  return p < 0 ? 0 : (p + 1) >> 7;
+}
+
+template <int D>
+__global__ void __launch_bounds__(Pf<D>::kThreads, 1)
+    paged_fmha_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                      const PagedAttnArgs a) {
+  using F = Pf<D>;
+  constexpr int kHalves = D / 64;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem =
+      reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* sQ = smem;                       // two tiles
+  uint8_t* sK = sQ + 2 * F::kTile;          // kNK tiles
+  uint8_t* sV = sK + F::kNK * F::kTile;     // kNV tiles
+  PfShared& sh = *reinterpret_cast<PfShared*>(sV + F::kNV * F::kTile);
+  __shared__ int64_t scan[33];
+  __shared__ PagedCursor s_cur;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int H = a.d.H, G = a.d.Hq / H;
+  const long long wl = a.wait_limit;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(&sh.abort);
+  PagedCursor c;
+  if (!paged_begin<F::kBM, F::kTK>(a, scan, &s_cur, c)) return;   // uniform over the CTA
+
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.q_ready[i], 4);
+      mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.p_half[i][0], 4);
+      mbar_init(&sh.p_half[i][1], 4);
+      mbar_init(&sh.pv_done[i], 1);
+      mbar_init(&sh.k_full[i], 1);
+      mbar_init(&sh.k_empty[i], 1);
+    }
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(&sh.v_full[i], 1);
+      mbar_init(&sh.v_ready[i], 2);
+      mbar_init(&sh.v_empty[i], 1);
+    }
+    mbar_init(&sh.drain, 1);
+    sh.abort = 0;
+    sh.pieces = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  if (warp == 2) {
+    tmem_alloc(&sh.tmem, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  // for the drain after a timeout: loads that have been issued, by ring place
+  uint32_t k_issued = 0, k_par = 0, v_issued = 0, v_par = 0;
+  bool mma_issued = false;
+
+  if (warp == 0) {
+    // ------------------------------------------------ TMA producer
+    uint32_t t = 0;   // tiles so far
+    bool ok = true;
+    const int pages = F::kTK >> a.d.lp;                       // of a tile
+    const int x = lane / kHalves, half = lane % kHalves;      // this lane's page and half
+    while (ok && c.u < c.u_end) {
+      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+      for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
+        const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0);
+        const int n_pages = n_keys <= 0 ? 0 : (n_keys + a.d.P - 1) >> a.d.lp;
+        const bool mine = x < n_pages && lane < pages * kHalves;
+        int row = 0;
+        if (mine) row = (paged_page(a.d, a.table, a.status, c.s.slot, k0 + (x << a.d.lp)) * H + c.hk) << a.d.lp;
+        const uint32_t bytes = static_cast<uint32_t>(n_pages) * a.d.P * 128 * kHalves;
+        for (int kv = 0; ok && kv < 2; ++kv) {
+          const uint32_t n = kv ? F::kNV : F::kNK, st = t % n, use = t / n;
+          uint64_t* full = kv ? &sh.v_full[st] : &sh.k_full[st];
+          if (lane == 0) {
+            ok = mbar_wait_sleep(kv ? &sh.v_empty[st] : &sh.k_empty[st], (use & 1u) ^ 1u, abort_flag, wl);
+            if (ok) mbar_arrive_expect_tx(full, bytes);
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (ok && mine)
+            tma_load_2d((kv ? sV : sK) + st * F::kTile + half * F::kBlk + (x << a.d.lp) * 128, kv ? &tmV : &tmK, full,
+                        half * 64, row);
+          __syncwarp();
+          if (ok) {
+            uint32_t& issued = kv ? v_issued : k_issued;
+            uint32_t& par = kv ? v_par : k_par;
+            issued |= 1u << st;
+            par = (par & ~(1u << st)) | ((use & 1u) << st);
+          }
+        }
+      }
+      paged_next<F::kBM, F::kTK>(a, c, p);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------ MMA issuer (warp-uniform, elected lane)
+    const uint32_t idS = idesc_bf16_f32(128, 128), idPV = idesc_bf16_f32_bmn(128, D);
+    uint32_t t = 0, n_q[2] = {0, 0}, n_s[2] = {0, 0};   // tiles; items and tiles of each stream
+    bool ok = true;
+    auto issue_s = [&](int i, uint32_t st) -> bool {   // S_i of the keys in place st
+      // P_i of the tile before lies where S_i goes: its product has to be done
+      if (n_s[i] && !mbar_wait(&sh.pv_done[i], (n_s[i] - 1) & 1u, abort_flag, wl)) return false;
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int kb = 0; kb < kHalves; ++kb) {
+          const uint64_t ad = sdesc_k_sw128(smem_u32(sQ + i * F::kTile + kb * F::kBlk));
+          const uint64_t bd = sdesc_k_sw128(smem_u32(sK + st * F::kTile + kb * F::kBlk));
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_bf16(tmem + i * 128, ad + 2 * k, bd + 2 * k, idS, (kb | k) != 0);
+        }
+        umma_commit(&sh.s_full[i]);
+      }
+      __syncwarp();
+      mma_issued = true;
+      return true;
+    };
+    auto issue_pv = [&](int i, uint32_t st, int steps, bool first) -> bool {   // O_i += P_i V
+      const uint32_t tO = tmem + F::kO + i * D, tP = tmem + i * 128;
+      const uint64_t bd = sdesc_mn_sw128(smem_u32(sV + st * F::kTile), F::kBlk);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!mbar_wait(&sh.p_half[i][h], n_s[i] & 1u, abort_flag, wl)) return false;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 4 * h; k < 4 * h + 4; ++k)
+            if (k < steps) umma_bf16_ts(tO, tP + 8 * k, bd + 128 * k, idPV, !(first && k == 0));
+          if (h == 1) umma_commit(&sh.pv_done[i]);
+        }
+        __syncwarp();
+      }
+      ++n_s[i];
+      return true;
+    };
+    auto release = [&](uint64_t* bar) {
+      if (elect_one()) umma_commit(bar);
+      __syncwarp();
+    };
+    while (ok && c.u < c.u_end) {
+      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+      const int n_str = c.s.m * G - c.rt * F::kBM > 128 ? 2 : 1;
+      for (int i = 0; ok && i < n_str; ++i) {
+        ok = mbar_wait(&sh.q_ready[i], n_q[i]++ & 1u, abort_flag, wl);
+        if (ok && i == 0) ok = mbar_wait(&sh.k_full[t % F::kNK], (t / F::kNK) & 1u, abort_flag, wl);
+        tc_fence_after();
+        ok = ok && issue_s(i, t % F::kNK);
+      }
+      if (ok) release(&sh.k_empty[t % F::kNK]);
+      for (int j = 0; ok && j < p.n; ++j, ++t) {
+        const uint32_t vs = t % F::kNV, ks = (t + 1) % F::kNK;
+        const int n_keys = min(F::kTK, c.s.len - (p.kt + j) * F::kTK);
+        const int steps = n_keys <= 0 ? 0 : (n_keys + 15) >> 4;
+        const bool more = j + 1 < p.n;
+        ok = mbar_wait(&sh.v_ready[vs], (t / F::kNV) & 1u, abort_flag, wl);
+        for (int i = 0; ok && i < n_str; ++i) {
+          ok = issue_pv(i, vs, steps, j == 0);
+          if (ok && i == n_str - 1) release(&sh.v_empty[vs]);
+          if (ok && more) {
+            if (i == 0) ok = mbar_wait(&sh.k_full[ks], ((t + 1) / F::kNK) & 1u, abort_flag, wl);
+            ok = ok && issue_s(i, ks);
+            if (ok && i == n_str - 1) release(&sh.k_empty[ks]);
+          }
+        }
+      }
+      paged_next<F::kBM, F::kTK>(a, c, p);
+    }
+  } else if (warp < 4) {
+    // ------------------------------------------------ values before the second product
+    uint32_t t = 0;
+    bool ok = true;
+    for (int piece = 0; ok && c.u < c.u_end; ++piece) {
+      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+      const int masked = first_masked(c.s, G, c.rt * F::kBM);
+      uint32_t (*notes)[4] = sh.notes[piece & 3];
+      // the notes of four pieces ago are read: this piece's values were loaded behind products that
+      // the softmax warps started after them
+      bool cleared = false;
+      for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
+        const uint32_t st = t % F::kNV;
+        int w = 1;
+        if (lane == 0) w = mbar_wait_sleep(&sh.v_full[st], (t / F::kNV) & 1u, abort_flag, wl);
+        ok = __shfl_sync(0xffffffffu, w, 0) != 0;
+        if (!ok) break;
+        if (!cleared) {
+          cleared = true;
+          if (lane < 8) notes[lane >> 1][2 * (warp - 2) + (lane & 1)] = 0;   // this warp's keys
+          __syncwarp();
+        }
+        if (kt >= masked) {
+          const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0), rows = n_keys <= 0 ? 0 : (n_keys + 15) & ~15;
+          uint8_t* tile = sV + st * F::kTile;
+          // a warp takes the 64-element blocks' rows 64 w ..; lane: 16 bytes of a row, 4 rows at a time
+          const int r0 = (warp - 2) * 64;
+          const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+          for (int b = 0; b < kHalves; ++b)
+            for (int r = r0 + (lane >> 3); r < min(r0 + 64, rows); r += 4) {
+              const uint32_t at = smem_u32(tile + b * F::kBlk + r * 128 + (lane & 7) * 16);
+              if (r >= n_keys) {
+                st_shared_v4(at, 0u, 0u, 0u, 0u);
+                continue;
+              }
+              uint4 v = ld_shared_v4(at);
+              __nv_bfloat162 x = zero;   // NaN where a value is not finite: 0 times it
+              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.x), zero, x);
+              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.y), zero, x);
+              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.z), zero, x);
+              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.w), zero, x);
+              const uint32_t bits = *reinterpret_cast<uint32_t*>(&x);
+              if ((bits & 0x7FFF7FFFu) == 0) continue;
+              uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
+                if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+              }
+              st_shared_v4(at, u[0], u[1], u[2], u[3]);
+              atomicOr(&notes[min(kt - masked, 3)][r >> 5], 1u << (r & 31));
+            }
+          fence_proxy_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.v_ready[st]);
+      }
+      paged_next<F::kBM, F::kTK>(a, c, p);
+    }
+  } else {
+    // ------------------------------------------------ softmax: warps 4 + 4 i + q, stream i, lane quarter q
+    constexpr float kTau = 8.f;
+    const int i = (warp - 4) >> 2, quarter = warp & 3;
+    const int r = quarter * 32 + lane;   // row of the stream
+    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t tS = tmem + lanes + i * 128, tO = tmem + lanes + F::kO + i * D;
+    const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
+    uint32_t t = 0;   // tiles of this stream
+    bool ok = true;
+    auto wait0 = [&](uint64_t* bar, uint32_t par) -> bool {
+      int w = 1;
+      if (lane == 0) w = mbar_wait_sleep(bar, par, abort_flag, wl) ? 1 : 0;
+      return __shfl_sync(0xffffffffu, w, 0) != 0;
+    };
+    for (int piece = 0; ok && c.u < c.u_end; ++piece) {
+      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+      const int row = c.rt * F::kBM + i * 128 + r, n_rows = c.s.m * G;
+      const bool active = n_rows - c.rt * F::kBM > i * 128;   // the stream has rows
+      const bool valid = row < n_rows;
+      const int pos = valid ? c.s.len - c.s.m + row / G : -1;
+      const int64_t out_row = valid ? paged_out_row(c, H, G, row) : 0;
+      float m = -INFINITY, l = 0.f;
+      if (active) {
+        // the row's query, swizzled as TMA would write it
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + out_row * D);
+#pragma unroll
+        for (int e = 0; e < D / 8; ++e) {
+          const uint4 u = valid ? src[e] : make_uint4(0u, 0u, 0u, 0u);
+          st_shared_v4(smem_u32(sQ + i * F::kTile + (e >> 3) * F::kBlk + r * 128 + (((e & 7) ^ (r & 7)) << 4)), u.x,
+                       u.y, u.z, u.w);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_ready[i]);
+        for (int kt = p.kt; kt < p.kt + p.n; ++kt, ++t) {
+          if (!wait0(&sh.s_full[i], t & 1u)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          uint32_t v[4][32];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tmem_ld_32x32b_x32(tS + 32 * e, v[e]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tmem_ld_wait(v[e]);
+          const int see = pos - kt * F::kTK;   // keys 0 .. see of the tile count
+          if (!__all_sync(0xffffffffu, see >= F::kTK - 1)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (32 * e + k > see) v[e][k] = 0xFF800000u;   // -inf: its weight is 0 exactly
+          }
+          float mk[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mk[e] = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+              mk[k & 7] = fmax3(mk[k & 7], __uint_as_float(v[e][2 * k]), __uint_as_float(v[e][2 * k + 1]));
+          const float mx =
+              fmaxf(fmax3(mk[0], mk[1], mk[2]), fmax3(mk[3], mk[4], fmax3(mk[5], mk[6], mk[7]))) * sl2;
+          const bool raise = mx > m + kTau;   // always where m = -inf and a key is seen
+          const float alpha = (raise && m != -INFINITY) ? ex2_fast(m - mx) : 1.f;
+          if (__any_sync(0xffffffffu, alpha != 1.f)) {   // needs the products before in O
+            if (!wait0(&sh.pv_done[i], (t - 1) & 1u)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+#pragma unroll 1
+            for (int e = 0; e < D / 32; ++e) {
+              uint32_t o[32];
+              tmem_ld_32x32b_x32(tO + 32 * e, o);
+              tmem_ld_wait(o);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+              tmem_st_32x32b_x32(tO + 32 * e, o);
+            }
+            l *= alpha;
+          }
+          if (raise) m = mx;
+          const float mu = m == -INFINITY ? 0.f : m;
+          const uint64_t s2 = f32x2(sl2, sl2), nm2 = f32x2(-mu, -mu);
+          uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const uint64_t x = ffma_x2((static_cast<uint64_t>(v[e][2 * k + 1]) << 32) | v[e][2 * k], s2, nm2);
+              const float p0 = ex2_fast(__uint_as_float(static_cast<uint32_t>(x)));
+              const float p1 = ex2_fast(__uint_as_float(static_cast<uint32_t>(x >> 32)));
+              sum[k & 1] = fadd_x2(sum[k & 1], f32x2(p0, p1));
+              __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);
+              pk[k] = *reinterpret_cast<uint32_t*>(&pb);
+            }
+            tmem_st_32x32b_x16(tS + 16 * e, pk);
+            if (e & 1) {
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.p_half[i][e >> 1]);
+            }
+          }
+          const uint64_t s01 = fadd_x2(sum[0], sum[1]);
+          l += __uint_as_float(static_cast<uint32_t>(s01)) + __uint_as_float(static_cast<uint32_t>(s01 >> 32));
+        }
+        ok = ok && wait0(&sh.pv_done[i], (t - 1) & 1u);
+      }
+      float* part = p.whole ? nullptr : paged_part<F::kBM, D>(a, blockIdx.x, p.kt == 0);
+      if (ok && active) {
+        tc_fence_after();
+        const int masked = first_masked(c.s, G, c.rt * F::kBM);
+        uint32_t any = 0;   // notes of this piece (uniform over the CTA)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) any |= reinterpret_cast<volatile uint32_t*>(sh.notes[piece & 3])[e];
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        uint16_t* dst = static_cast<uint16_t*>(a.out) + out_row * D;
+#pragma unroll 1
+        for (int e = 0; e < D / 32; ++e) {
+          uint32_t o[32];
+          tmem_ld_32x32b_x32(tO + 32 * e, o);
+          tmem_ld_wait(o);
+          if (l == 0.f) {   // no key was seen
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = 0u;
+          }
+          if (any) {   // values that are not finite, of keys that this row sees
+            for (int kt = max(masked, p.kt); kt < p.kt + p.n; ++kt)
+              for (int w = 0; w < 4; ++w)
+                for (uint32_t bits = sh.notes[piece & 3][min(kt - masked, 3)][w]; bits; bits &= bits - 1) {
+                  const int j = kt * F::kTK + 32 * w + __ffs(bits) - 1;
+                  if (j > pos) continue;
+                  const int page = paged_page(a.d, a.table, a.status, c.s.slot, j);
+                  const uint16_t* vr = static_cast<const uint16_t*>(a.v) + paged_row(a.d, page, c.hk, j) * D + 32 * e;
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) {
+                    const float x = __uint_as_float(static_cast<uint32_t>(vr[k]) << 16);
+                    if (!isfinite(x)) o[k] = __float_as_uint(__uint_as_float(o[k]) + x);
+                  }
+                }
+          }
+          if (!valid) continue;
+          if (part) {
+            float* to = part + (i * 128 + r) * D + 32 * e;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              reinterpret_cast<uint4*>(to)[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          } else {
+            uint32_t w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              __nv_bfloat162 u =
+                  __floats2bfloat162_rn(__uint_as_float(o[2 * k]) * f, __uint_as_float(o[2 * k + 1]) * f);
+              w[k] = *reinterpret_cast<uint32_t*>(&u);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              reinterpret_cast<uint4*>(dst + 32 * e)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+          }
+        }
+        if (part && valid) {
+          part[F::kBM * D + i * 128 + r] = m;
+          part[F::kBM * (D + 1) + i * 128 + r] = l;
+        }
+        tc_fence_before();
+      }
+      // both streams are through the piece (or all of them stop)
+      if (!bar_and(1, 256, ok)) {
+        ok = false;
+        break;
+      }
+      if (part) {
+        if (tid == 128) sh.last = paged_arrive(a, p);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (*reinterpret_cast<volatile int32_t*>(&sh.last))
+          paged_join<uint16_t, F::kBM, D>(a, c, p, tid - 128, 256);
+      }
+      if (tid == 128) *reinterpret_cast<volatile int32_t*>(&sh.pieces) = piece + 1;
+      paged_next<F::kBM, F::kTK>(a, c, p);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (warp == 0 && lane == 0) {
+      for (int kv = 0; kv < 2; ++kv)
+        for (int st = 0; st < 3; ++st)
+          if (((kv ? v_issued : k_issued) >> st) & 1u) {
+            const uint32_t ad = smem_u32(kv ? &sh.v_full[st] : &sh.k_full[st]);
+            const long long t0 = clock64();
+            while (!mbar_try_wait(ad, ((kv ? v_par : k_par) >> st) & 1u) && clock64() - t0 < wl) {
+            }
+          }
+    }
+    if (warp == 1 && mma_issued) {
+      if (elect_one()) umma_commit(&sh.drain);
+      __syncwarp();
+      const uint32_t ad = smem_u32(&sh.drain);
+      const long long t0 = clock64();
+      while (!mbar_try_wait(ad, 0) && clock64() - t0 < wl) {
+      }
+    }
+    if (tid == 128) {   // the arrivals that are still owed, so that the counters are zero for the next call
+      PagedCursor w = s_cur;
+      for (int piece = 0; w.u < w.u_end; ++piece) {
+        const PagedPiece p = paged_piece<F::kBM, F::kTK>(w, G);
+        if (piece >= sh.pieces && !p.whole) paged_arrive(a, p);
+        paged_next<F::kBM, F::kTK>(a, w, p);
+      }
+      atomicOr(a.status, kStatusTimeout);
+    }
+    __syncthreads();
+  }
+  if (warp == 2) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_paged_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV, int num_sms,
+                              cudaStream_t st) {
+  static SmemOptIn opt_in[2];
+  auto kern = a.d.d == 128 ? paged_fmha_kernel<128> : paged_fmha_kernel<64>;
+  const int smem = a.d.d == 128 ? Pf<128>::kSmem : Pf<64>::kSmem;
+  if (cudaError_t e = opt_in[a.d.d == 128](kern, smem)) return e;
+  return launch_kernel(false, kern, num_sms, Pf<128>::kThreads, smem, st, tmK, tmV, a);
+}
+
+}  // namespace mot

@@ -95,10 +95,15 @@ struct PagedAttnArgs {
   float* part;
   int32_t* count;
   int32_t* status;
+  long long wait_limit;   // bound of every pipeline wait (SM cycles)
 };
 constexpr int kPagedMaxGroup = 16;   // query heads per key/value head
 size_t paged_part_floats(const PagedDims& d, int num_sms);
 int paged_counters(int num_sms);
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st);
+// Chunks in bf16 on the tensor cores: maps over the layer's pools as rows [n_pages * H * P][d], box 64 x P.
+bool paged_fmha_takes(const PagedDims& d, int max_chunk);
+cudaError_t launch_paged_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                              int num_sms, cudaStream_t st);
 
 }  // namespace mot

@@ -53,79 +53,10 @@ static_assert(Fa<128>::kSmem <= 232448, "shared memory budget");
 static_assert(Fa<128>::kQcol + 64 <= 512 && Fa<64>::kQcol + 32 <= 512, "TMEM columns");
 static_assert(Fa<64>::kThreads == Fa<128>::kThreads, "one launch size for both head widths");
 
-// Named barrier `id` over `n` threads, returning the AND of `p`.
-__device__ __forceinline__ bool lane_and_n(int id, int n, bool p) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred a, q;\n\t"
-      "setp.ne.u32 a, %1, 0;\n\t"
-      "bar.red.and.pred q, %2, %3, a;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"(static_cast<uint32_t>(p)), "r"(id), "r"(n)
-      : "memory");
-  return r != 0;
-}
-
-__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-
 __device__ __forceinline__ void tmem_st_32x32b_x8(uint32_t taddr, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
                "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
-}
-
-// mbar_wait for the attention kernel's TMA producer and the softmax warps' lane-0
-// waits: each poll may suspend the thread (up to 0.5 us, ended early when the
-// phase completes), so waiting warps leave their sub-partition's issue slots to
-// the softmax warps. The MMA issuer keeps the polling mbar_wait.
-__device__ __forceinline__ bool mbar_try_wait_sleep(uint32_t bar_addr, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar_addr), "r"(parity), "r"(500u)
-      : "memory");
-  return ok != 0;
-}
-
-__device__ __forceinline__ bool mbar_wait_sleep(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
-                                                long long limit) {
-  const uint32_t a = smem_u32(bar);
-  const long long t0 = clock64();
-  while (!mbar_try_wait_sleep(a, parity)) {
-    if (*abort_flag) return false;
-    if (clock64() - t0 > limit) {
-      *abort_flag = 1;
-      return false;
-    }
-  }
-  return true;
-}
-
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-
-// Packed pairs of fp32 (sm_100 family): d = a * b + c per lane.
-__device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
-  return (static_cast<uint64_t>(__float_as_uint(hi)) << 32) | __float_as_uint(lo);
-}
-__device__ __forceinline__ uint64_t ffma_x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
 }
 
 // One 32-key chunk (keys k0 .. k0 + 31 of the tile) of a query row's scores v, in
@@ -166,19 +97,6 @@ __device__ __forceinline__ uint32_t tmem_ld_x1(uint32_t taddr) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(taddr) : "memory");
   asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v)::"memory");
   return v;
-}
-
-// D[tmem] (+)= A[tmem] * B[smem]^T, issued by a single thread: A (M = 128 rows,
-// 16-bit elements, two consecutive K values per 32-bit column) is read from the
-// lanes of the issuing CTA's tensor memory.
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
-                                             uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
 }
 
 // One CTA per (b, query head, 128-query tile), persistent over key tiles
@@ -392,7 +310,7 @@ __global__ void __launch_bounds__(Fa<D>::kThreads, 1)
     }
     float m = -INFINITY;
     bool ok = true;
-    auto agree = [&](bool p) -> bool { return lane_and_n(1 + q, 128, p); };
+    auto agree = [&](bool p) -> bool { return bar_and(1 + q, 128, p); };
     auto wait_lane0 = [&](uint64_t* bar, uint32_t par) -> bool {
       int w = 1;
       if (lane == 0) w = mbar_wait_sleep(bar, par, abort_flag, wl) ? 1 : 0;
