@@ -2109,8 +2109,10 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
     MOT_CUDA_TRY(timed(h, "paged_fmha", st, [&] { return launch_paged_fmha(a, tmK, tmV, h->num_sms, st); }));
     return MOT_OK;
   }
-  MOT_CUDA_TRY(timed(h, "paged_attn", st,
-                     [&] { return launch_paged_attn(a, h->num_sms, batch->max_chunk, st); }));
+  MOT_CUDA_TRY(timed(h, d.dtype ? "paged_simt" : "paged_decode", st, [&] {
+    return d.dtype ? launch_paged_simt(a, h->num_sms, batch->max_chunk, st)
+                   : launch_paged_decode(a, h->num_sms, batch->max_chunk, st);
+  }));
   return MOT_OK;
 }
 

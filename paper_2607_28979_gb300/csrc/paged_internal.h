@@ -1,4 +1,4 @@
-// Internal declarations of the paged cache (paged.cu: its pages and the append; paged_attn.cu:
+// Internal declarations of the paged cache (paged.cu: its pages and the append; paged_simt.cu, paged_decode.cu, paged_fmha.cu:
 // attention over it), shared with the C-ABI layer.
 #pragma once
 
@@ -100,7 +100,10 @@ struct PagedAttnArgs {
 constexpr int kPagedMaxGroup = 16;   // query heads per key/value head
 size_t paged_part_floats(const PagedDims& d, int num_sms);
 int paged_counters(int num_sms);
-cudaError_t launch_paged_attn(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st);
+// fp32.
+cudaError_t launch_paged_simt(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st);
+// bf16, few rows per key/value head (any number is right).
+cudaError_t launch_paged_decode(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st);
 // Chunks in bf16 on the tensor cores: maps over the layer's pools as rows [n_pages * H * P][d], box 64 x P.
 bool paged_fmha_takes(const PagedDims& d, int max_chunk);
 cudaError_t launch_paged_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV,

@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged cache on sm_103a, on the FMA units.
+// Attention of new tokens over a paged cache on sm_103a, in fp32 on the FMA units.
 //
 //   paged_simt_kernel   o_r = sum_{j <= p_r} softmax_j(q_r . k_j / sqrt(d)) v_j for BM rows (new token,
 //                       query head of the group) of one key/value head at a time, in tiles of 64
@@ -21,16 +21,11 @@ struct Simt {
 };
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const uint16_t* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xFFFF0000u));
-}
 __device__ __forceinline__ bool finite4(const float4& v) {
   return isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w);
 }
 
-template <class T, int D, int BM>
+template <int D, int BM>
 __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAttnArgs a) {
   using P = Simt<D, BM>;
   constexpr int kR = BM / 16;     // rows of a thread
@@ -56,7 +51,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
     for (int x = tid; x < BM * (D / 4); x += kSimtThreads) {
       const int r = x / (D / 4), col = (x - r * (D / 4)) * 4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < n_rows) v = load4(static_cast<const T*>(a.q) + paged_out_row(c, H, G, r0 + r) * D + col);
+      if (r < n_rows) v = load4(static_cast<const float*>(a.q) + paged_out_row(c, H, G, r0 + r) * D + col);
       *reinterpret_cast<float4*>(sq + r * P::kLd + col) = v;
     }
     int pos[kR];   // a row sees the keys 0 .. pos
@@ -83,8 +78,8 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
         if (j < n_keys) {
           const int page = paged_page(a.d, a.table, a.status, c.s.slot, k0 + j);
           const int64_t row = paged_row(a.d, page, c.hk, k0 + j) * D + col;
-          kv = load4(static_cast<const T*>(a.k) + row);
-          vv = load4(static_cast<const T*>(a.v) + row);
+          kv = load4(static_cast<const float*>(a.k) + row);
+          vv = load4(static_cast<const float*>(a.v) + row);
           odd |= !finite4(vv);
         }
         *reinterpret_cast<float4*>(sk + j * P::kLd + col) = kv;
@@ -185,7 +180,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
         const int r = ty * kR + i;
         if (r >= n_rows) continue;
         const float f = l[i] == 0.f ? 0.f : 1.f / l[i];
-        T* dst = static_cast<T*>(a.out) + paged_out_row(c, H, G, r0 + r) * D;
+        float* dst = static_cast<float*>(a.out) + paged_out_row(c, H, G, r0 + r) * D;
 #pragma unroll
         for (int h = 0; h < kC; ++h) {
           const float t[4] = {o[i][4 * h], o[i][4 * h + 1], o[i][4 * h + 2], o[i][4 * h + 3]};
@@ -210,17 +205,17 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
       __syncthreads();
       if (tid == 0) s_last = paged_arrive(a, p);
       __syncthreads();
-      if (s_last) paged_join<T, BM, D>(a, c, p, tid, kSimtThreads);
+      if (s_last) paged_join<float, BM, D>(a, c, p, tid, kSimtThreads);
     }
     paged_next<BM, kTK>(a, c, p);
     __syncthreads();   // s_last and the queries are read
   }
 }
 
-template <class T, int D, int BM>
+template <int D, int BM>
 cudaError_t launch_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
   static SmemOptIn opt_in;
-  auto kern = paged_simt_kernel<T, D, BM>;
+  auto kern = paged_simt_kernel<D, BM>;
   if (cudaError_t e = opt_in(kern, Simt<D, BM>::kSmem)) return e;
   const int per_sm = BM == 16 ? 2 : 1;
   return launch_kernel(false, kern, num_sms * per_sm, kSimtThreads, Simt<D, BM>::kSmem, st, a);
@@ -235,12 +230,10 @@ bool paged_fmha_takes(const PagedDims& d, int max_chunk) {
   return d.dtype == 0 && int64_t(max_chunk) * (d.Hq / d.H) > 16;
 }
 
-cudaError_t launch_paged_attn(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st) {
+cudaError_t launch_paged_simt(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st) {
   const bool few = int64_t(max_chunk) * (a.d.Hq / a.d.H) <= 16;
-  if (a.d.dtype == 0)   // chunks: launch_paged_fmha
-    return a.d.d == 64 ? launch_simt<uint16_t, 64, 16>(a, num_sms, st) : launch_simt<uint16_t, 128, 16>(a, num_sms, st);
-  if (a.d.d == 64) return few ? launch_simt<float, 64, 16>(a, num_sms, st) : launch_simt<float, 64, 64>(a, num_sms, st);
-  return few ? launch_simt<float, 128, 16>(a, num_sms, st) : launch_simt<float, 128, 64>(a, num_sms, st);
+  if (a.d.d == 64) return few ? launch_simt<64, 16>(a, num_sms, st) : launch_simt<64, 64>(a, num_sms, st);
+  return few ? launch_simt<128, 16>(a, num_sms, st) : launch_simt<128, 64>(a, num_sms, st);
 }
 
 }  // namespace mot
