@@ -259,27 +259,74 @@ __device__ __forceinline__ void paged_store4(T* dst, const float (&o)[4], float 
     *reinterpret_cast<float4*>(dst) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
   }
 }
+// By all threads of the CTA; `fs`: paged_join_floats<BM>() floats of shared memory that nothing else holds.
+constexpr int kJoinPieces = 32;
+template <int BM>
+__host__ __device__ constexpr int paged_join_floats() {
+  return BM * (kJoinPieces + 2);
+}
 template <class T, int BM, int D>
-__device__ __forceinline__ void paged_join(const PagedAttnArgs& a, const PagedCursor& c, const PagedPiece& p, int tid,
-                                           int n_threads) {
-  const int G = a.d.Hq / a.d.H, r0 = c.rt * BM, rows = min(BM, c.s.m * G - r0);
-  for (int x = tid; x < rows * (D / 4); x += n_threads) {
-    const int r = x / (D / 4), col = (x - r * (D / 4)) * 4;
-    float m = -INFINITY;
-    for (int k = p.c0; k <= p.c1; ++k) m = fmaxf(m, __ldcg(paged_part<BM, D>(a, k, k == p.c0) + BM * D + r));
-    const float ms = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = p.c0; k <= p.c1; ++k) {
-      const float* part = paged_part<BM, D>(a, k, k == p.c0);
-      const float f = exp2f(__ldcg(part + BM * D + r) - ms);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(part + r * D + col));
-      l = fmaf(f, __ldcg(part + BM * (D + 1) + r), l);
-      o[0] = fmaf(f, v.x, o[0]);
-      o[1] = fmaf(f, v.y, o[1]);
-      o[2] = fmaf(f, v.z, o[2]);
-      o[3] = fmaf(f, v.w, o[3]);
+__device__ __forceinline__ void paged_join(const PagedAttnArgs& a, const PagedCursor& c, const PagedPiece& p, float* fs,
+                                           int tid, int n_threads) {
+  const int G = a.d.Hq / a.d.H, r0 = c.rt * BM, rows = min(BM, c.s.m * G - r0), n = p.c1 - p.c0 + 1;
+  float* sw = fs;                       // [piece][row]: a piece's weight
+  float* sms = fs + BM * kJoinPieces;   // the row's maximum
+  float* sinv = sms + BM;               // and 1 / its sum
+  auto part = [&](int k) { return paged_part<BM, D>(a, p.c0 + k, k == 0); };
+  // a warp per row: maximum and sum over the pieces
+  const int warp = tid >> 5, lane = tid & 31;
+  for (int r = warp; r < rows; r += n_threads >> 5) {
+    float m = -INFINITY, l = 0.f;
+    for (int k = lane; k < n; k += 32) m = fmaxf(m, __ldcg(part(k) + BM * D + r));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = m == -INFINITY ? 0.f : m;
+    for (int k = lane; k < n; k += 32)
+      l = fmaf(exp2f(__ldcg(part(k) + BM * D + r) - m), __ldcg(part(k) + BM * (D + 1) + r), l);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (lane == 0) {
+      sms[r] = m;
+      sinv[r] = l == 0.f ? 0.f : 1.f / l;
     }
-    paged_store4(static_cast<T*>(a.out) + paged_out_row(c, a.d.H, G, r0 + r) * D + col, o, l == 0.f ? 0.f : 1.f / l);
+  }
+  // then four columns a thread, kJoinPieces pieces at a time
+  constexpr int kMine = (BM * D / 4 + 127) / 128;   // at 128 threads
+  float o[kMine][4];
+#pragma unroll
+  for (int y = 0; y < kMine; ++y)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[y][e] = 0.f;
+  for (int k0 = 0; k0 < n; k0 += kJoinPieces) {
+    const int nk = min(kJoinPieces, n - k0);
+    __syncthreads();
+    for (int x = tid; x < nk * rows; x += n_threads) {
+      const int k = x / rows, r = x - k * rows;
+      sw[k * BM + r] = exp2f(__ldcg(part(k0 + k) + BM * D + r) - sms[r]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int y = 0; y < kMine; ++y) {
+      const int x = tid + y * n_threads;
+      if (x >= rows * (D / 4)) break;
+      const int r = x / (D / 4), col = (x - r * (D / 4)) * 4;
+#pragma unroll 8
+      for (int k = 0; k < nk; ++k) {
+        const float f = sw[k * BM + r];
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(part(k0 + k) + r * D + col));
+        o[y][0] = fmaf(f, v.x, o[y][0]);
+        o[y][1] = fmaf(f, v.y, o[y][1]);
+        o[y][2] = fmaf(f, v.z, o[y][2]);
+        o[y][3] = fmaf(f, v.w, o[y][3]);
+      }
+    }
+  }
+#pragma unroll
+  for (int y = 0; y < kMine; ++y) {
+    const int x = tid + y * n_threads;
+    if (x >= rows * (D / 4)) break;
+    const int r = x / (D / 4), col = (x - r * (D / 4)) * 4;
+    paged_store4(static_cast<T*>(a.out) + paged_out_row(c, a.d.H, G, r0 + r) * D + col, o[y], sinv[r]);
   }
 }
 

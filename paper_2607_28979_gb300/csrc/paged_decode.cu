@@ -48,6 +48,7 @@ template <int D, int NT>
 __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_kernel(const PagedAttnArgs a) {
   constexpr int BM = 8 * NT, TK = kDecTK, kI = D / 32, kH = D / 64;
   constexpr int kLd = D + 4;
+  static_assert(paged_join_floats<BM>() <= kWarps * BM * kLd, "so holds the join");
   __shared__ int64_t scan[33];
   __shared__ PagedCursor s_cur;
   __shared__ int s_last;
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_ker
     if (part) {
       if (tid == 0) s_last = paged_arrive(a, p);
       __syncthreads();
-      if (s_last) paged_join<uint16_t, BM, D>(a, c, p, tid, kDecThreads);
+      if (s_last) paged_join<uint16_t, BM, D>(a, c, p, &so[0][0][0], tid, kDecThreads);
       __syncthreads();
     }
     paged_next<BM, TK>(a, c, p);

@@ -59,6 +59,55 @@ __device__ __forceinline__ int first_masked(const PagedSeq& s, int G, int row0) 
   return p < 0 ? 0 : (p + 1) >> 7;
 }
 
+// Joins an item's pieces in the order of their CTAs, a thread per row. Here the partial rows lie by
+// fours of columns, [D / 4][256 rows][4], so that the threads of a warp write and read whole lines.
+template <int D>
+__device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCursor& c, const PagedPiece& p, int r) {
+  constexpr int BM = Pf<D>::kBM;
+  const int G = a.d.Hq / a.d.H, row = c.rt * BM + r, n = p.c1 - p.c0 + 1;
+  if (row >= c.s.m * G) return;
+  auto part = [&](int k) { return paged_part<BM, D>(a, p.c0 + k, k == 0); };
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) m = fmaxf(m, __ldcg(part(k) + BM * D + r));
+  m = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k)
+    l = fmaf(exp2f(__ldcg(part(k) + BM * D + r) - m), __ldcg(part(k) + BM * (D + 1) + r), l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* dst = static_cast<uint16_t*>(a.out) + paged_out_row(c, a.d.H, G, row) * D;
+#pragma unroll 1
+  for (int e = 0; e < D / 32; ++e) {   // 32 columns at a time
+    float o[32];
+#pragma unroll
+    for (int k = 0; k < 32; ++k) o[k] = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < n; ++k) {
+      const float* pk = part(k);
+      const float f = exp2f(__ldcg(pk + BM * D + r) - m);
+      const float4* src = reinterpret_cast<const float4*>(pk) + 8 * e * BM + r;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float4 v = __ldcg(src + x * BM);
+        o[4 * x] = fmaf(f, v.x, o[4 * x]);
+        o[4 * x + 1] = fmaf(f, v.y, o[4 * x + 1]);
+        o[4 * x + 2] = fmaf(f, v.z, o[4 * x + 2]);
+        o[4 * x + 3] = fmaf(f, v.w, o[4 * x + 3]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t w[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        __nv_bfloat162 u = __floats2bfloat162_rn(o[8 * k + 2 * x] * inv, o[8 * k + 2 * x + 1] * inv);
+        w[x] = *reinterpret_cast<uint32_t*>(&u);
+      }
+      reinterpret_cast<uint4*>(dst + 32 * e)[k] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     paged_fmha_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -434,10 +483,10 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
           }
           if (!valid) continue;
           if (part) {
-            float* to = part + (i * 128 + r) * D + 32 * e;
+            uint4* to = reinterpret_cast<uint4*>(part) + 8 * e * F::kBM + i * 128 + r;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              reinterpret_cast<uint4*>(to)[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+              to[k * F::kBM] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
           } else {
             uint32_t w[16];
 #pragma unroll
@@ -466,7 +515,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
         if (tid == 128) sh.last = paged_arrive(a, p);
         asm volatile("bar.sync 1, 256;" ::: "memory");
         if (*reinterpret_cast<volatile int32_t*>(&sh.last))
-          paged_join<uint16_t, F::kBM, D>(a, c, p, tid - 128, 256);
+          join_rows<D>(a, c, p, tid - 128);
       }
       if (tid == 128) *reinterpret_cast<volatile int32_t*>(&sh.pieces) = piece + 1;
       paged_next<F::kBM, F::kTK>(a, c, p);

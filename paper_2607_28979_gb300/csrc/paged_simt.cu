@@ -30,6 +30,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
   using P = Simt<D, BM>;
   constexpr int kR = BM / 16;     // rows of a thread
   constexpr int kC = D / 64;      // float4 columns of a thread
+  static_assert(paged_join_floats<BM>() <= kTK * (2 * D + 4), "the keys' and values' place holds the join");
   extern __shared__ float4 smem4[];
   float* sq = reinterpret_cast<float*>(smem4);
   float* sk = sq + BM * P::kLd;
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
       __syncthreads();
       if (tid == 0) s_last = paged_arrive(a, p);
       __syncthreads();
-      if (s_last) paged_join<float, BM, D>(a, c, p, tid, kSimtThreads);
+      if (s_last) paged_join<float, BM, D>(a, c, p, sk, tid, kSimtThreads);
     }
     paged_next<BM, kTK>(a, c, p);
     __syncthreads();   // s_last and the queries are read
