@@ -239,7 +239,8 @@ mot_status mot_profile_read(mot_handle h, mot_kernel_stat* out, int32_t cap, int
  * MOT_ERR_TIMEOUT through mot_get_device_status and the context stays usable.
  * On a replay handle, stall_test = 1 makes the guided attention's first CTA
  * wait for a signal that nothing sends, with the same outcome for
- * mot_replay_attention on a guided layer.
+ * mot_replay_attention on a guided layer. On a paged handle, the first CTA of
+ * mot_paged_attention's tensor-core kernel (bf16 chunks) loads nothing.
  */
 mot_status mot_debug_set(mot_handle h, int32_t stall_test, int64_t wait_limit_cycles);
 

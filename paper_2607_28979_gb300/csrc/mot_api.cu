@@ -2098,6 +2098,7 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.count = h->pcount;
   a.status = h->status;
   a.wait_limit = h->wait_limit;
+  a.stall_test = h->stall_test;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (paged_fmha_takes(d, batch->max_chunk)) {
     CUtensorMap tmK{}, tmV{};

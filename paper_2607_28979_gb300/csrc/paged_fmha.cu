@@ -8,8 +8,9 @@
 //                                    lane per (page, 64 dimensions), into rings of 2 and 3 tiles;
 //                         warp 1     S_i = Q_i K^T (Q_i and K from shared memory) and O_i += P_i V (P_i
 //                                    from TMEM, over S_i; V's rows are keys, so it is an MN-major
-//                                    operand and needs no transpose), i = 0, 1 in turn;
-//                         warps 2-3  values before the second product: rows behind the sequence's
+//                                    operand and needs no transpose), i = 0, 1 in turn. One thread: an
+//                                    election and a warp barrier at each step cost 9% of the whole;
+//                         warp 2     values before the second product: rows behind the sequence's
 //                                    end become zeros, and in tiles that some rows see only in part
 //                                    infinite and NaN values do too (a masked key's weight is 0, and 0
 //                                    times them would not be); their keys are noted, and the rows
@@ -20,6 +21,7 @@
 //                                    in two halves, so that the second product starts on the first
 //                                    while the other is made; at the end O from TMEM to the output or
 //                                    to the piece's partial results.
+//                       The waits poll without a sleep: a sleeping thread wakes up to a microsecond late.
 //                       Every wait is bounded; on a timeout the roles unwind, copies and MMAs in flight
 //                       are drained, TMEM is freed and kStatusTimeout is raised.
 #include "paged_common.cuh"
@@ -143,7 +145,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     }
     for (int i = 0; i < 3; ++i) {
       mbar_init(&sh.v_full[i], 1);
-      mbar_init(&sh.v_ready[i], 2);
+      mbar_init(&sh.v_ready[i], 1);
       mbar_init(&sh.v_empty[i], 1);
     }
     mbar_init(&sh.drain, 1);
@@ -161,57 +163,70 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
+  // Every lane of a warp waits, and all of them go on or none does.
+  auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, wl));
+  };
   // for the drain after a timeout: loads that have been issued, by ring place
   uint32_t k_issued = 0, k_par = 0, v_issued = 0, v_par = 0;
-  bool mma_issued = false;
 
   if (warp == 0) {
     // ------------------------------------------------ TMA producer
     uint32_t t = 0;   // tiles so far
-    bool ok = true;
+    bool ok = a.stall_test == 0 || blockIdx.x != 0;   // test hook: CTA 0 loads nothing
     const int pages = F::kTK >> a.d.lp;                       // of a tile
     const int x = lane / kHalves, half = lane % kHalves;      // this lane's page and half
     while (ok && c.u < c.u_end) {
       const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+      // this lane's table entry of a tile, read a tile ahead
+      auto entry = [&](int kt) -> int {
+        const int at = kt * F::kTK + (x << a.d.lp);
+        return lane < pages * kHalves && kt < p.kt + p.n && at < c.s.len
+                   ? a.table[int64_t(c.s.slot) * a.d.max_pages + (at >> a.d.lp)]
+                   : 0;
+      };
+      int next = entry(p.kt);
       for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
         const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0);
-        const int n_pages = n_keys <= 0 ? 0 : (n_keys + a.d.P - 1) >> a.d.lp;
-        const bool mine = x < n_pages && lane < pages * kHalves;
-        int row = 0;
-        if (mine) row = (paged_page(a.d, a.table, a.status, c.s.slot, k0 + (x << a.d.lp)) * H + c.hk) << a.d.lp;
-        const uint32_t bytes = static_cast<uint32_t>(n_pages) * a.d.P * 128 * kHalves;
-        for (int kv = 0; ok && kv < 2; ++kv) {
-          const uint32_t n = kv ? F::kNV : F::kNK, st = t % n, use = t / n;
-          uint64_t* full = kv ? &sh.v_full[st] : &sh.k_full[st];
-          if (lane == 0) {
-            ok = mbar_wait_sleep(kv ? &sh.v_empty[st] : &sh.k_empty[st], (use & 1u) ^ 1u, abort_flag, wl);
-            if (ok) mbar_arrive_expect_tx(full, bytes);
-          }
-          ok = __shfl_sync(0xffffffffu, ok, 0);
-          if (ok && mine)
-            tma_load_2d((kv ? sV : sK) + st * F::kTile + half * F::kBlk + (x << a.d.lp) * 128, kv ? &tmV : &tmK, full,
-                        half * 64, row);
-          __syncwarp();
-          if (ok) {
-            uint32_t& issued = kv ? v_issued : k_issued;
-            uint32_t& par = kv ? v_par : k_par;
-            issued |= 1u << st;
-            par = (par & ~(1u << st)) | ((use & 1u) << st);
-          }
+        const bool mine = lane < pages * kHalves && k0 + (x << a.d.lp) < c.s.len;
+        int page = next;
+        next = entry(kt + 1);
+        if (mine && (page < 0 || page >= a.d.n_pages)) {   // held inside the pool
+          page = 0;
+          atomicOr(a.status, kStatusPageUse);
         }
+        const int row = (page * H + c.hk) << a.d.lp;
+        const uint32_t bytes =
+            n_keys <= 0 ? 0u : static_cast<uint32_t>((n_keys + a.d.P - 1) >> a.d.lp) * a.d.P * 128 * kHalves;
+        auto fetch = [&](bool v, uint32_t st, uint32_t use) -> bool {
+          uint64_t* full = v ? &sh.v_full[st] : &sh.k_full[st];
+          if (!wait(v ? &sh.v_empty[st] : &sh.k_empty[st], (use & 1u) ^ 1u)) return false;
+          if (lane == 0) mbar_arrive_expect_tx(full, bytes);
+          __syncwarp();
+          if (mine)
+            tma_load_2d((v ? sV : sK) + st * F::kTile + half * F::kBlk + (x << a.d.lp) * 128, v ? &tmV : &tmK, full,
+                        half * 64, row);
+          uint32_t& issued = v ? v_issued : k_issued;
+          uint32_t& par = v ? v_par : k_par;
+          issued |= 1u << st;
+          par = (par & ~(1u << st)) | ((use & 1u) << st);
+          return true;
+        };
+        ok = fetch(false, t % F::kNK, t / F::kNK) && fetch(true, t % F::kNV, t / F::kNV);
       }
       paged_next<F::kBM, F::kTK>(a, c, p);
     }
   } else if (warp == 1) {
-    // ------------------------------------------------ MMA issuer (warp-uniform, elected lane)
-    const uint32_t idS = idesc_bf16_f32(128, 128), idPV = idesc_bf16_f32_bmn(128, D);
-    uint32_t t = 0, n_q[2] = {0, 0}, n_s[2] = {0, 0};   // tiles; items and tiles of each stream
-    bool ok = true;
-    auto issue_s = [&](int i, uint32_t st) -> bool {   // S_i of the keys in place st
-      // P_i of the tile before lies where S_i goes: its product has to be done
-      if (n_s[i] && !mbar_wait(&sh.pv_done[i], (n_s[i] - 1) & 1u, abort_flag, wl)) return false;
-      tc_fence_after();
-      if (elect_one()) {
+    // ------------------------------------------------ MMA issuer: one thread
+    if (elect_one()) {
+      const uint32_t idS = idesc_bf16_f32(128, 128), idPV = idesc_bf16_f32_bmn(128, D);
+      uint32_t t = 0, n_q[2] = {0, 0}, n_s[2] = {0, 0};   // tiles; items and tiles of each stream
+      bool ok = true;
+      auto wait1 = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, wl); };
+      auto issue_s = [&](int i, uint32_t st) -> bool {   // S_i of the keys in place st
+        // P_i of the tile before lies where S_i goes: its product has to be done
+        if (n_s[i] && !wait1(&sh.pv_done[i], (n_s[i] - 1) & 1u)) return false;
+        tc_fence_after();
 #pragma unroll
         for (int kb = 0; kb < kHalves; ++kb) {
           const uint64_t ad = sdesc_k_sw128(smem_u32(sQ + i * F::kTile + kb * F::kBlk));
@@ -221,62 +236,53 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
             umma_bf16(tmem + i * 128, ad + 2 * k, bd + 2 * k, idS, (kb | k) != 0);
         }
         umma_commit(&sh.s_full[i]);
-      }
-      __syncwarp();
-      mma_issued = true;
-      return true;
-    };
-    auto issue_pv = [&](int i, uint32_t st, int steps, bool first) -> bool {   // O_i += P_i V
-      const uint32_t tO = tmem + F::kO + i * D, tP = tmem + i * 128;
-      const uint64_t bd = sdesc_mn_sw128(smem_u32(sV + st * F::kTile), F::kBlk);
+        return true;
+      };
+      auto issue_pv = [&](int i, uint32_t st, int steps, bool first) -> bool {   // O_i += P_i V
+        const uint32_t tO = tmem + F::kO + i * D, tP = tmem + i * 128;
+        const uint64_t bd = sdesc_mn_sw128(smem_u32(sV + st * F::kTile), F::kBlk);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (!mbar_wait(&sh.p_half[i][h], n_s[i] & 1u, abort_flag, wl)) return false;
-        tc_fence_after();
-        if (elect_one()) {
+        for (int h = 0; h < 2; ++h) {
+          if (!wait1(&sh.p_half[i][h], n_s[i] & 1u)) return false;
+          tc_fence_after();
 #pragma unroll
           for (int k = 4 * h; k < 4 * h + 4; ++k)
             if (k < steps) umma_bf16_ts(tO, tP + 8 * k, bd + 128 * k, idPV, !(first && k == 0));
-          if (h == 1) umma_commit(&sh.pv_done[i]);
         }
-        __syncwarp();
-      }
-      ++n_s[i];
-      return true;
-    };
-    auto release = [&](uint64_t* bar) {
-      if (elect_one()) umma_commit(bar);
-      __syncwarp();
-    };
-    while (ok && c.u < c.u_end) {
-      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
-      const int n_str = c.s.m * G - c.rt * F::kBM > 128 ? 2 : 1;
-      for (int i = 0; ok && i < n_str; ++i) {
-        ok = mbar_wait(&sh.q_ready[i], n_q[i]++ & 1u, abort_flag, wl);
-        if (ok && i == 0) ok = mbar_wait(&sh.k_full[t % F::kNK], (t / F::kNK) & 1u, abort_flag, wl);
-        tc_fence_after();
-        ok = ok && issue_s(i, t % F::kNK);
-      }
-      if (ok) release(&sh.k_empty[t % F::kNK]);
-      for (int j = 0; ok && j < p.n; ++j, ++t) {
-        const uint32_t vs = t % F::kNV, ks = (t + 1) % F::kNK;
-        const int n_keys = min(F::kTK, c.s.len - (p.kt + j) * F::kTK);
-        const int steps = n_keys <= 0 ? 0 : (n_keys + 15) >> 4;
-        const bool more = j + 1 < p.n;
-        ok = mbar_wait(&sh.v_ready[vs], (t / F::kNV) & 1u, abort_flag, wl);
+        umma_commit(&sh.pv_done[i]);
+        ++n_s[i];
+        return true;
+      };
+      while (ok && c.u < c.u_end) {
+        const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+        const int n_str = c.s.m * G - c.rt * F::kBM > 128 ? 2 : 1;
         for (int i = 0; ok && i < n_str; ++i) {
-          ok = issue_pv(i, vs, steps, j == 0);
-          if (ok && i == n_str - 1) release(&sh.v_empty[vs]);
-          if (ok && more) {
-            if (i == 0) ok = mbar_wait(&sh.k_full[ks], ((t + 1) / F::kNK) & 1u, abort_flag, wl);
-            ok = ok && issue_s(i, ks);
-            if (ok && i == n_str - 1) release(&sh.k_empty[ks]);
+          ok = wait1(&sh.q_ready[i], n_q[i]++ & 1u);
+          if (ok && i == 0) ok = wait1(&sh.k_full[t % F::kNK], (t / F::kNK) & 1u);
+          ok = ok && issue_s(i, t % F::kNK);
+        }
+        if (ok) umma_commit(&sh.k_empty[t % F::kNK]);
+        for (int j = 0; ok && j < p.n; ++j, ++t) {
+          const uint32_t vs = t % F::kNV, ks = (t + 1) % F::kNK;
+          const int n_keys = min(F::kTK, c.s.len - (p.kt + j) * F::kTK);
+          const int steps = n_keys <= 0 ? 0 : (n_keys + 15) >> 4;
+          const bool more = j + 1 < p.n;
+          ok = wait1(&sh.v_ready[vs], (t / F::kNV) & 1u);
+          for (int i = 0; ok && i < n_str; ++i) {
+            ok = issue_pv(i, vs, steps, j == 0);
+            if (ok && i == n_str - 1) umma_commit(&sh.v_empty[vs]);
+            if (ok && more) {
+              if (i == 0) ok = wait1(&sh.k_full[ks], ((t + 1) / F::kNK) & 1u);
+              ok = ok && issue_s(i, ks);
+              if (ok && i == n_str - 1) umma_commit(&sh.k_empty[ks]);
+            }
           }
         }
+        paged_next<F::kBM, F::kTK>(a, c, p);
       }
-      paged_next<F::kBM, F::kTK>(a, c, p);
     }
-  } else if (warp < 4) {
+    __syncwarp();
+  } else if (warp == 2) {
     // ------------------------------------------------ values before the second product
     uint32_t t = 0;
     bool ok = true;
@@ -289,23 +295,21 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
       bool cleared = false;
       for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
         const uint32_t st = t % F::kNV;
-        int w = 1;
-        if (lane == 0) w = mbar_wait_sleep(&sh.v_full[st], (t / F::kNV) & 1u, abort_flag, wl);
-        ok = __shfl_sync(0xffffffffu, w, 0) != 0;
+        ok = wait(&sh.v_full[st], (t / F::kNV) & 1u);
         if (!ok) break;
         if (!cleared) {
           cleared = true;
-          if (lane < 8) notes[lane >> 1][2 * (warp - 2) + (lane & 1)] = 0;   // this warp's keys
+          if (lane < 16) notes[lane >> 2][lane & 3] = 0;
           __syncwarp();
         }
         if (kt >= masked) {
           const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0), rows = n_keys <= 0 ? 0 : (n_keys + 15) & ~15;
           uint8_t* tile = sV + st * F::kTile;
-          // a warp takes the 64-element blocks' rows 64 w ..; lane: 16 bytes of a row, 4 rows at a time
-          const int r0 = (warp - 2) * 64;
+          // lane: 16 bytes of a row, 4 rows at a time
           const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
           for (int b = 0; b < kHalves; ++b)
-            for (int r = r0 + (lane >> 3); r < min(r0 + 64, rows); r += 4) {
+#pragma unroll 4
+            for (int r = lane >> 3; r < rows; r += 4) {
               const uint32_t at = smem_u32(tile + b * F::kBlk + r * 128 + (lane & 7) * 16);
               if (r >= n_keys) {
                 st_shared_v4(at, 0u, 0u, 0u, 0u);
@@ -335,7 +339,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
       }
       paged_next<F::kBM, F::kTK>(a, c, p);
     }
-  } else {
+  } else if (warp >= 4) {
     // ------------------------------------------------ softmax: warps 4 + 4 i + q, stream i, lane quarter q
     constexpr float kTau = 8.f;
     const int i = (warp - 4) >> 2, quarter = warp & 3;
@@ -345,11 +349,6 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
     uint32_t t = 0;   // tiles of this stream
     bool ok = true;
-    auto wait0 = [&](uint64_t* bar, uint32_t par) -> bool {
-      int w = 1;
-      if (lane == 0) w = mbar_wait_sleep(bar, par, abort_flag, wl) ? 1 : 0;
-      return __shfl_sync(0xffffffffu, w, 0) != 0;
-    };
     for (int piece = 0; ok && c.u < c.u_end; ++piece) {
       const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
       const int row = c.rt * F::kBM + i * 128 + r, n_rows = c.s.m * G;
@@ -372,7 +371,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_ready[i]);
         for (int kt = p.kt; kt < p.kt + p.n; ++kt, ++t) {
-          if (!wait0(&sh.s_full[i], t & 1u)) {
+          if (!wait(&sh.s_full[i], t & 1u)) {
             ok = false;
             break;
           }
@@ -403,7 +402,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
           const bool raise = mx > m + kTau;   // always where m = -inf and a key is seen
           const float alpha = (raise && m != -INFINITY) ? ex2_fast(m - mx) : 1.f;
           if (__any_sync(0xffffffffu, alpha != 1.f)) {   // needs the products before in O
-            if (!wait0(&sh.pv_done[i], (t - 1) & 1u)) {
+            if (!wait(&sh.pv_done[i], (t - 1) & 1u)) {
               ok = false;
               break;
             }
@@ -446,7 +445,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
           const uint64_t s01 = fadd_x2(sum[0], sum[1]);
           l += __uint_as_float(static_cast<uint32_t>(s01)) + __uint_as_float(static_cast<uint32_t>(s01 >> 32));
         }
-        ok = ok && wait0(&sh.pv_done[i], (t - 1) & 1u);
+        ok = ok && wait(&sh.pv_done[i], (t - 1) & 1u);
       }
       float* part = p.whole ? nullptr : paged_part<F::kBM, D>(a, blockIdx.x, p.kt == 0);
       if (ok && active) {
@@ -535,7 +534,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
             }
           }
     }
-    if (warp == 1 && mma_issued) {
+    if (warp == 1) {
       if (elect_one()) umma_commit(&sh.drain);
       __syncwarp();
       const uint32_t ad = smem_u32(&sh.drain);

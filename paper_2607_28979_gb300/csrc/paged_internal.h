@@ -96,6 +96,7 @@ struct PagedAttnArgs {
   int32_t* count;
   int32_t* status;
   long long wait_limit;   // bound of every pipeline wait (SM cycles)
+  int32_t stall_test;     // test hook: the tensor-core kernel's first CTA loads nothing
 };
 constexpr int kPagedMaxGroup = 16;   // query heads per key/value head
 size_t paged_part_floats(const PagedDims& d, int num_sms);

@@ -53,12 +53,6 @@ static_assert(Fa<128>::kSmem <= 232448, "shared memory budget");
 static_assert(Fa<128>::kQcol + 64 <= 512 && Fa<64>::kQcol + 32 <= 512, "TMEM columns");
 static_assert(Fa<64>::kThreads == Fa<128>::kThreads, "one launch size for both head widths");
 
-__device__ __forceinline__ void tmem_st_32x32b_x8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
-               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-
 // One 32-key chunk (keys k0 .. k0 + 31 of the tile) of a query row's scores v, in
 // its softmax: the running maxima of 8 independent chains (two keys per step), and
 // the bf16 pairs of P = exp2(s * sl2 - m). DIAG: the diagonal tile, whose keys past

@@ -542,6 +542,23 @@ def test_offsets_beyond_32_bits(new):
     _attend(c, [0], [new])
 
 
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right():
+    """The first CTA loads nothing (test hook) under a limit of about 10 ms: the call ends with
+    MOT_ERR_TIMEOUT. Its split items' arrivals are settled, so the next call joins them rightly."""
+    c = _filled([3000, 900], None, q_heads=8, kv_heads=2, d=128, page=32)
+    q = c.normal(200, 8, 128)
+    out = torch.zeros_like(q)
+    b = c.batch([0, 1], [120, 80])
+    for _ in range(2):
+        M.mot_debug_set(c.h, True, 20_000_000)
+        M.mot_paged_attention(c.h, 0, c.c, b, q, out)
+        assert c.status() == M.MOT_ERR_TIMEOUT
+        M.mot_debug_set(c.h, False)
+        M.mot_paged_attention(c.h, 0, c.c, b, q, out)
+        assert c.status() == M.MOT_OK
+        P.check_attention(c, [0, 1], [120, 80], q, out)
+
+
 # ---------------------------------------------------------------- streams, graphs, the whole run
 
 def test_a_step_is_captured_and_replayed_on_another_stream():
