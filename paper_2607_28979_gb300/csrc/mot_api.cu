@@ -2097,6 +2097,7 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.part = h->ppart;
   a.count = h->pcount;
   a.status = h->status;
+  a.max_chunk = batch->max_chunk;
   a.wait_limit = h->wait_limit;
   a.stall_test = h->stall_test;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -2111,8 +2112,7 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
     return MOT_OK;
   }
   MOT_CUDA_TRY(timed(h, d.dtype ? "paged_simt" : "paged_decode", st, [&] {
-    return d.dtype ? launch_paged_simt(a, h->num_sms, batch->max_chunk, st)
-                   : launch_paged_decode(a, h->num_sms, batch->max_chunk, st);
+    return d.dtype ? launch_paged_simt(a, h->num_sms, st) : launch_paged_decode(a, h->num_sms, st);
   }));
   return MOT_OK;
 }

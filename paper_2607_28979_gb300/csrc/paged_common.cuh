@@ -69,10 +69,15 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedDims& d, const PagedBat
 // An item is (entry i, key/value head, tile of BM rows), a row being (new token t, query head g of
 // the group): row r = t G + g of the entry's m G rows. Its units are its tiles of TK keys; causal,
 // so an item's units end with the tile that holds its last row's position (one unit at least: rows
-// before position 0 are written too). The W units of a call in the order (entry, head, row tile,
-// key tile) are dealt to the CTAs in equal runs, CTA c of C taking [W c / C, W (c + 1) / C): every
-// CTA has the same work whatever the lengths, at most its first and its last item are shared with
-// others, and those items' partial results are joined by the CTA that finishes last, in order.
+// before position 0 are written too). Two ways to deal them to the CTAs:
+//   runs    the W units of a call in the order (entry, head, row tile, key tile) in equal runs, CTA c of
+//           C taking [W c / C, W (c + 1) / C): every CTA has the same work whatever the lengths, and at
+//           most its first and its last item are shared with others;
+//   pieces  each item in pieces of `coarse` units, one piece per CTA, where that makes no more pieces
+//           than CTAs. No CTA then has parts of two items, which cost it some microseconds (a piece's
+//           start and end do not overlap with another's): taken while coarse is small, where that
+//           outweighs the CTAs that have less than their share.
+// The partial results of an item in several pieces are joined by the CTA that finishes last, in order.
 
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0, by the steps of Euclid's algorithm.
 __device__ inline int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
@@ -96,88 +101,131 @@ template <int BM, int TK>
 struct PagedSplit {
   // Row tiles of an entry.
   static __device__ __forceinline__ int row_tiles(int m, int G) { return (m * G + BM - 1) / BM; }
-  // Units of row tile rt: the position of its last row is len - m + x / G.
-  static __device__ __forceinline__ int units(const PagedSeq& s, int G, int rt) {
+  // Units, or pieces of f units, of row tile rt: the position of its last row is len - m + x / G.
+  static __device__ __forceinline__ int units(const PagedSeq& s, int G, int rt, int f = 1) {
     const int x = min((rt + 1) * BM, s.m * G) - 1;
     const int p = s.len - s.m + x / G;
-    return p < 0 ? 1 : p / TK + 1;
+    return p < 0 ? 1 : p / (TK * f) + 1;
   }
-  // Units of the row tiles [0, rt) of one head.
-  static __device__ __forceinline__ int64_t before(const PagedSeq& s, int G, int rt) {
+  // Those of the row tiles [0, rt) of one head.
+  static __device__ __forceinline__ int64_t before(const PagedSeq& s, int G, int rt, int f = 1) {
     if (rt == 0) return 0;
     if (rt <= 4 || s.len < s.m) {   // few terms, or rows before position 0 (a malformed batch)
       int64_t u = 0;
-      for (int r = 0; r < rt; ++r) u += units(s, G, r);
+      for (int r = 0; r < rt; ++r) u += units(s, G, r, f);
       return u;
     }
     const int R = row_tiles(s.m, G);
     const int whole = rt < R ? rt : R - 1;   // the last tile may be short
-    int64_t u = whole + floor_sum(whole, int64_t(G) * TK, BM, int64_t(s.len - s.m) * G + BM - 1);
-    if (rt == R) u += units(s, G, R - 1);
+    int64_t u = whole + floor_sum(whole, int64_t(G) * TK * f, BM, int64_t(s.len - s.m) * G + BM - 1);
+    if (rt == R) u += units(s, G, R - 1, f);
     return u;
   }
-  static __device__ __forceinline__ int64_t head_units(const PagedSeq& s, int G) {
-    return before(s, G, row_tiles(s.m, G));
+  static __device__ __forceinline__ int64_t head_units(const PagedSeq& s, int G, int f = 1) {
+    return before(s, G, row_tiles(s.m, G), f);
   }
 };
 
-// A run of units: where it stands, and where the call's W units and C CTAs put it.
+// A CTA's share: where it stands, and where the call's units put the others.
 struct PagedCursor {
   PagedSeq s;
-  int64_t u, u_end;      // global units [u, u_end) are left
-  int64_t W, head_u;     // all units; units of one head of the entry
-  int32_t C;             // CTAs that have work
+  int64_t u, u_end;      // runs: global units [u, u_end) are left; pieces: the piece, and one more
+  int64_t W;             // runs: all units
+  int32_t C;             // runs: CTAs that have work
+  int32_t coarse;        // units of a piece; 0: runs
   int32_t i, hk, rt, kt; // the next unit
-  // CTA that unit x belongs to
+  // runs: the CTA that unit x belongs to
   __device__ __forceinline__ int owner(int64_t x) const { return int(((x + 1) * C - 1) / W); }
 };
 
-// The run of CTA blockIdx.x. Called by all threads; `sh` and `out` are shared. False: no work.
+// The share of CTA blockIdx.x: a run of `least` units at least where there are as many, or a piece of
+// `least` to `most` units. Called by all threads; `sh` and `out` are shared. False: no work.
 template <int BM, int TK>
-__device__ bool paged_begin(const PagedAttnArgs& a, int64_t* sh, PagedCursor* out, PagedCursor& c) {
+__device__ bool paged_begin(const PagedAttnArgs& a, int least, int most, int64_t* sh, PagedCursor* out,
+                            PagedCursor& c) {
   using S = PagedSplit<BM, TK>;
   const int G = a.d.Hq / a.d.H, H = a.d.H, T = blockDim.x, tid = threadIdx.x;
-  int64_t mine = 0, W = 0, at = 0;
   const int n = a.b.n;
-  for (int i0 = 0; i0 < n; i0 += T) {
-    mine = 0;
-    if (i0 + tid < n) mine = H * S::head_units(paged_seq(a.d, a.b, a.lens, a.status, i0 + tid), G);
-    int64_t t;
-    at = block_scan(mine, sh, t) + W;
-    W += t;
+  // all entries' units, in pieces of f; `at`, `mine`: of this thread's entry among the last T entries
+  int64_t mine = 0, at = 0;
+  PagedSeq ms{-1, 0, 0, 0};
+  if (n <= T && tid < n) ms = paged_seq(a.d, a.b, a.lens, a.status, tid);
+  auto total = [&](int f) -> int64_t {
+    int64_t W = 0;
+    for (int i0 = 0; i0 < n; i0 += T) {
+      if (n > T) {   // more entries than threads: a piece at a time
+        ms.m = 0;
+        if (i0 + tid < n) ms = paged_seq(a.d, a.b, a.lens, a.status, i0 + tid);
+      }
+      mine = ms.m ? H * S::head_units(ms, G, f) : 0;
+      int64_t t;
+      at = W + block_scan(mine, sh, t);
+      W += t;
+    }
+    return W;
+  };
+  int64_t W = total(1);
+  if (W == 0) return false;
+  const int64_t grid = gridDim.x;
+  // the items of the batch: pieces of f units make W / f + items of them at most
+  const int64_t items = int64_t(H) * (int64_t(a.max_chunk) * G <= BM ? n : int64_t(a.b.rows) * G / BM + n);
+  int f = 0;
+  if (items < grid) {
+    const int64_t need = (W + grid - items - 1) / (grid - items);
+    if (need <= most) {
+      f = need < least ? least : int(need);
+      if (f > 1) W = total(f);
+      if (W > grid) {   // max_chunk was no bound: runs
+        f = 0;
+        W = total(1);
+      }
+    }
   }
-  const int C = W < int64_t(gridDim.x) ? int(W) : int(gridDim.x);
+  int C;
+  int64_t u, u_end;
+  if (f) {
+    C = int(W);
+    u = blockIdx.x;
+    u_end = u + 1;
+  } else {
+    const int64_t runs = (W + least - 1) / least;
+    C = runs < grid ? int(runs) : int(grid);
+    u = W * int(blockIdx.x) / C;
+    u_end = W * (int(blockIdx.x) + 1) / C;
+  }
   if (int(blockIdx.x) >= C) return false;
-  const int64_t u = W * int(blockIdx.x) / C, u_end = W * (int(blockIdx.x) + 1) / C;
+  const int ff = f ? f : 1;
   int64_t carry = 0;
   for (int i0 = 0; i0 < n; i0 += T) {
-    if (n > T) {   // more entries than threads: their sums again, a piece at a time
-      mine = 0;
-      if (i0 + tid < n) mine = H * S::head_units(paged_seq(a.d, a.b, a.lens, a.status, i0 + tid), G);
+    if (n > T) {
+      ms.m = 0;
+      if (i0 + tid < n) ms = paged_seq(a.d, a.b, a.lens, a.status, i0 + tid);
+      mine = ms.m ? H * S::head_units(ms, G, ff) : 0;
       int64_t t;
-      at = block_scan(mine, sh, t) + carry;
+      at = carry + block_scan(mine, sh, t);
       carry += t;
     }
     if (u >= at && u < at + mine) {
       PagedCursor o;
       o.i = i0 + tid;
-      o.s = paged_seq(a.d, a.b, a.lens, a.status, o.i);
+      o.s = ms;
       o.W = W;
       o.C = C;
+      o.coarse = f;
       o.u = u;
       o.u_end = u_end;
-      o.head_u = mine / H;
+      const int64_t head_u = mine / H;
       int64_t r = u - at;
-      o.hk = int(r / o.head_u);
-      r -= o.hk * o.head_u;
+      o.hk = int(r / head_u);
+      r -= o.hk * head_u;
       int lo = 0, hi = S::row_tiles(o.s.m, G) - 1;   // the last rt with before(rt) <= r
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (S::before(o.s, G, mid) <= r) lo = mid;
+        if (S::before(o.s, G, mid, ff) <= r) lo = mid;
         else hi = mid - 1;
       }
       o.rt = lo;
-      o.kt = int(r - S::before(o.s, G, lo));
+      o.kt = int(r - S::before(o.s, G, lo, ff)) * ff;
       *out = o;
     }
     if (n > T && carry > u) break;
@@ -187,7 +235,7 @@ __device__ bool paged_begin(const PagedAttnArgs& a, int64_t* sh, PagedCursor* ou
   return true;
 }
 
-// One piece of a run: units [kt, kt + n) of the item's `units`.
+// One piece of a share: units [kt, kt + n) of the item's `units`.
 struct PagedPiece {
   int32_t kt, n, units;
   bool whole;
@@ -198,6 +246,13 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedCursor& c, int G) {
   PagedPiece p;
   p.units = PagedSplit<BM, TK>::units(c.s, G, c.rt);
   p.kt = c.kt;
+  if (c.coarse) {
+    p.n = min(c.coarse, p.units - p.kt);
+    p.whole = p.n == p.units;
+    p.c0 = int(blockIdx.x) - p.kt / c.coarse;
+    p.c1 = p.c0 + (p.units - 1) / c.coarse;
+    return p;
+  }
   const int64_t left = c.u_end - c.u;
   p.n = left < p.units - c.kt ? int(left) : p.units - c.kt;
   p.whole = p.kt == 0 && p.n == p.units;
@@ -213,7 +268,7 @@ template <int BM, int TK>
 __device__ __forceinline__ void paged_next(const PagedAttnArgs& a, PagedCursor& c, const PagedPiece& p) {
   using S = PagedSplit<BM, TK>;
   const int G = a.d.Hq / a.d.H;
-  c.u += p.n;
+  c.u = c.coarse ? c.u_end : c.u + p.n;
   c.kt = 0;
   if (c.u >= c.u_end) return;
   if (++c.rt < S::row_tiles(c.s.m, G)) return;
@@ -237,18 +292,6 @@ __device__ __forceinline__ int64_t paged_out_row(const PagedCursor& c, int H, in
   const int t = r / G;
   return (int64_t(c.s.r0 + t) * H + c.hk) * G + (r - t * G);
 }
-// After the partial results of a piece are written (by all threads that `tid` counts, and a barrier):
-// true in one thread that finds itself behind the last of the item's CTAs. The counter is zero again
-// for the next call.
-__device__ __forceinline__ bool paged_arrive(const PagedAttnArgs& a, const PagedPiece& p) {
-  __threadfence();
-  const bool last = atomicAdd(&a.count[p.c0], 1) == p.c1 - p.c0;
-  if (last) a.count[p.c0] = 0;
-  __threadfence();
-  return last;
-}
-// Joins the item's pieces in the order of their CTAs, `rows` rows from row r0 of the entry, and writes
-// the output. Four columns a thread.
 template <class T>
 __device__ __forceinline__ void paged_store4(T* dst, const float (&o)[4], float f) {
   if constexpr (sizeof(T) == 2) {
@@ -259,75 +302,129 @@ __device__ __forceinline__ void paged_store4(T* dst, const float (&o)[4], float 
     *reinterpret_cast<float4*>(dst) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
   }
 }
-// By all threads of the CTA; `fs`: paged_join_floats<BM>() floats of shared memory that nothing else holds.
-constexpr int kJoinPieces = 32;
-template <int BM>
-__host__ __device__ constexpr int paged_join_floats() {
-  return BM * (kJoinPieces + 2);
+
+// The join of an item's n pieces: up to 8 at once by the CTA that finishes last; more in two levels, in
+// groups of 8 (of 32 above 64 pieces), each joined into its first piece's place by its last CTA, and the
+// groups by the last of these.
+struct PagedGroup {
+  int32_t first, n, stride;   // places of the CTAs first, first + stride, ..: n of them
+  bool is_item_first;         // `first` is the item's first CTA: its place 1
+  bool final;                 // the join gives the item's result
+};
+template <int BM, int D>
+__device__ __forceinline__ float* paged_place(const PagedAttnArgs& a, const PagedGroup& g, int k) {
+  return paged_part<BM, D>(a, g.first + k * g.stride, k == 0 && g.is_item_first);
 }
+__device__ __forceinline__ int paged_group_size(int n) { return n <= 8 ? n : (n <= 64 ? 8 : 32); }
+// Counters, zero between calls: [2 cta + place] of a group (its first piece's), then [cta] of an item's groups.
+__device__ __forceinline__ bool paged_last(int32_t* counter, int n) {
+  // one operation that releases this CTA's writes and acquires the others'
+  int before;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+  const bool last = before == n - 1;
+  if (last) *counter = 0;
+  return last;
+}
+// In one thread, after the partial results of the piece are written (by all threads, and a barrier):
+// whether this CTA joins the piece's group, which g becomes.
+__device__ __forceinline__ bool paged_arrive(const PagedAttnArgs& a, const PagedPiece& p, PagedGroup& g) {
+  const int n = p.c1 - p.c0 + 1, size = paged_group_size(n), k0 = (int(blockIdx.x) - p.c0) / size * size;
+  g.first = p.c0 + k0;
+  g.n = min(size, n - k0);
+  g.stride = 1;
+  g.is_item_first = k0 == 0;
+  g.final = size == n;
+  return paged_last(&a.count[2 * g.first + (k0 == 0)], g.n);
+}
+// The same after a group that was not final is joined and written: the groups of the item.
+__device__ __forceinline__ bool paged_arrive_group(const PagedAttnArgs& a, const PagedPiece& p, PagedGroup& g) {
+  const int n = p.c1 - p.c0 + 1, size = paged_group_size(n);
+  g.first = p.c0;
+  g.n = (n + size - 1) / size;
+  g.stride = size;
+  g.is_item_first = true;
+  g.final = true;
+  return paged_last(&a.count[2 * int(gridDim.x) + p.c0], g.n);
+}
+// An arrival that a CTA owes after a timeout, without a join.
+__device__ __forceinline__ void paged_arrive_owed(const PagedAttnArgs& a, const PagedPiece& p) {
+  PagedGroup g;
+  if (paged_arrive(a, p, g) && !g.final) paged_arrive_group(a, p, g);
+}
+
+// Joins a group's places in order, by all threads of the CTA: to the output, or into its first place.
+// Four columns a thread; kJoin places at a time with all their loads in flight, under a running maximum.
 template <class T, int BM, int D>
-__device__ __forceinline__ void paged_join(const PagedAttnArgs& a, const PagedCursor& c, const PagedPiece& p, float* fs,
-                                           int tid, int n_threads) {
-  const int G = a.d.Hq / a.d.H, r0 = c.rt * BM, rows = min(BM, c.s.m * G - r0), n = p.c1 - p.c0 + 1;
-  float* sw = fs;                       // [piece][row]: a piece's weight
-  float* sms = fs + BM * kJoinPieces;   // the row's maximum
-  float* sinv = sms + BM;               // and 1 / its sum
-  auto part = [&](int k) { return paged_part<BM, D>(a, p.c0 + k, k == 0); };
-  // a warp per row: maximum and sum over the pieces
-  const int warp = tid >> 5, lane = tid & 31;
-  for (int r = warp; r < rows; r += n_threads >> 5) {
-    float m = -INFINITY, l = 0.f;
-    for (int k = lane; k < n; k += 32) m = fmaxf(m, __ldcg(part(k) + BM * D + r));
+__device__ __forceinline__ void paged_join(const PagedAttnArgs& a, const PagedCursor& c, const PagedGroup& g, int tid,
+                                           int n_threads) {
+  constexpr int kJoin = 8;
+  const int G = a.d.Hq / a.d.H, r0 = c.rt * BM, rows = min(BM, c.s.m * G - r0), items = rows * (D / 4);
+  for (int x0 = 0; x0 < items; x0 += n_threads) {
+    const int x = min(x0 + tid, items - 1), r = x / (D / 4), col = (x - r * (D / 4)) * 4;
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < g.n; k0 += kJoin) {
+      float mk[kJoin], lk[kJoin];
+      float4 v[kJoin];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    m = m == -INFINITY ? 0.f : m;
-    for (int k = lane; k < n; k += 32)
-      l = fmaf(exp2f(__ldcg(part(k) + BM * D + r) - m), __ldcg(part(k) + BM * (D + 1) + r), l);
+      for (int k = 0; k < kJoin; ++k) {
+        const float* part = paged_place<BM, D>(a, g, min(k0 + k, g.n - 1));
+        mk[k] = __ldcg(part + BM * D + r);
+        lk[k] = __ldcg(part + BM * (D + 1) + r);
+        v[k] = __ldcg(reinterpret_cast<const float4*>(part + r * D + col));
+      }
+      float to = m;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (lane == 0) {
-      sms[r] = m;
-      sinv[r] = l == 0.f ? 0.f : 1.f / l;
+      for (int k = 0; k < kJoin; ++k) to = fmaxf(to, mk[k]);
+      const float ms = to == -INFINITY ? 0.f : to, f0 = exp2f(m - ms);
+      m = to;
+      l *= f0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= f0;
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k)
+        if (k0 + k < g.n) {
+          const float f = exp2f(mk[k] - ms);
+          l = fmaf(f, lk[k], l);
+          o[0] = fmaf(f, v[k].x, o[0]);
+          o[1] = fmaf(f, v[k].y, o[1]);
+          o[2] = fmaf(f, v[k].z, o[2]);
+          o[3] = fmaf(f, v[k].w, o[3]);
+        }
     }
-  }
-  // then four columns a thread, kJoinPieces pieces at a time
-  constexpr int kMine = (BM * D / 4 + 127) / 128;   // at 128 threads
-  float o[kMine][4];
-#pragma unroll
-  for (int y = 0; y < kMine; ++y)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[y][e] = 0.f;
-  for (int k0 = 0; k0 < n; k0 += kJoinPieces) {
-    const int nk = min(kJoinPieces, n - k0);
-    __syncthreads();
-    for (int x = tid; x < nk * rows; x += n_threads) {
-      const int k = x / rows, r = x - k * rows;
-      sw[k * BM + r] = exp2f(__ldcg(part(k0 + k) + BM * D + r) - sms[r]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int y = 0; y < kMine; ++y) {
-      const int x = tid + y * n_threads;
-      if (x >= rows * (D / 4)) break;
-      const int r = x / (D / 4), col = (x - r * (D / 4)) * 4;
-#pragma unroll 8
-      for (int k = 0; k < nk; ++k) {
-        const float f = sw[k * BM + r];
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(part(k0 + k) + r * D + col));
-        o[y][0] = fmaf(f, v.x, o[y][0]);
-        o[y][1] = fmaf(f, v.y, o[y][1]);
-        o[y][2] = fmaf(f, v.z, o[y][2]);
-        o[y][3] = fmaf(f, v.w, o[y][3]);
+    if (g.final) {
+      if (x0 + tid < items)
+        paged_store4(static_cast<T*>(a.out) + paged_out_row(c, a.d.H, G, r0 + r) * D + col, o, l == 0.f ? 0.f : 1.f / l);
+    } else {
+      float* part = paged_place<BM, D>(a, g, 0);
+      __syncthreads();   // a row's maximum and sum have been read by the threads of all its columns
+      if (x0 + tid < items) {
+        __stcg(reinterpret_cast<float4*>(part + r * D + col), make_float4(o[0], o[1], o[2], o[3]));
+        if (col == 0) {
+          __stcg(part + BM * D + r, m);
+          __stcg(part + BM * (D + 1) + r, l);
+        }
       }
     }
   }
-#pragma unroll
-  for (int y = 0; y < kMine; ++y) {
-    const int x = tid + y * n_threads;
-    if (x >= rows * (D / 4)) break;
-    const int r = x / (D / 4), col = (x - r * (D / 4)) * 4;
-    paged_store4(static_cast<T*>(a.out) + paged_out_row(c, a.d.H, G, r0 + r) * D + col, o[y], sinv[r]);
-  }
+}
+// What follows a piece's partial results in a kernel whose threads all take part; `sh` is shared.
+struct PagedJoinShared {
+  PagedGroup g;
+  int32_t mine;
+};
+template <class T, int BM, int D>
+__device__ __forceinline__ void paged_finish(const PagedAttnArgs& a, const PagedCursor& c, const PagedPiece& p,
+                                             PagedJoinShared& sh, int tid, int n_threads) {
+  __syncthreads();
+  if (tid == 0) sh.mine = paged_arrive(a, p, sh.g);
+  __syncthreads();
+  if (!sh.mine) return;
+  paged_join<T, BM, D>(a, c, sh.g, tid, n_threads);
+  if (sh.g.final) return;
+  __syncthreads();
+  if (tid == 0) sh.mine = paged_arrive_group(a, p, sh.g);
+  __syncthreads();
+  if (sh.mine) paged_join<T, BM, D>(a, c, sh.g, tid, n_threads);
 }
 
 // The pool row (in rows of d elements) of position `pos` and head hk of a slot's page entry.

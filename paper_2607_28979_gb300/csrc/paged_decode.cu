@@ -24,6 +24,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kDecThreads = 32 * kWarps;
 constexpr int kDecTK = 16 * kWarps;
+constexpr int kLeast = 2, kMost = 8;   // units of a share (a join costs about as much as four)
 
 // 16 bytes that are read once
 __device__ __forceinline__ uint4 ld_stream(const void* p) {
@@ -48,16 +49,15 @@ template <int D, int NT>
 __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_kernel(const PagedAttnArgs a) {
   constexpr int BM = 8 * NT, TK = kDecTK, kI = D / 32, kH = D / 64;
   constexpr int kLd = D + 4;
-  static_assert(paged_join_floats<BM>() <= kWarps * BM * kLd, "so holds the join");
   __shared__ int64_t scan[33];
   __shared__ PagedCursor s_cur;
-  __shared__ int s_last;
+  __shared__ PagedJoinShared s_join;
   __shared__ __align__(16) float so[kWarps][BM][kLd];   // read and written 16 bytes at a time
   __shared__ float sm[kWarps][BM], sl[kWarps][BM];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int H = a.d.H, G = a.d.Hq / H;
   PagedCursor c;
-  if (!paged_begin<BM, TK>(a, scan, &s_cur, c)) return;
+  if (!paged_begin<BM, TK>(a, kLeast, kMost, scan, &s_cur, c)) return;
   const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
   const uint16_t* kp = static_cast<const uint16_t*>(a.k);
   const uint16_t* vp = static_cast<const uint16_t*>(a.v);
@@ -313,13 +313,8 @@ __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_ker
         paged_store4(static_cast<uint16_t*>(a.out) + paged_out_row(c, H, G, r0 + r) * D + col, y, ll == 0.f ? 0.f : 1.f / ll);
       }
     }
-    __syncthreads();   // so is read; the partial results are written
-    if (part) {
-      if (tid == 0) s_last = paged_arrive(a, p);
-      __syncthreads();
-      if (s_last) paged_join<uint16_t, BM, D>(a, c, p, &so[0][0][0], tid, kDecThreads);
-      __syncthreads();
-    }
+    if (part) paged_finish<uint16_t, BM, D>(a, c, p, s_join, tid, kDecThreads);
+    __syncthreads();   // so and s_join are read
     paged_next<BM, TK>(a, c, p);
   }
 }
@@ -331,8 +326,8 @@ cudaError_t launch_decode(const PagedAttnArgs& a, int num_sms, cudaStream_t st) 
 
 }  // namespace
 
-cudaError_t launch_paged_decode(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st) {
-  const bool one = int64_t(max_chunk) * (a.d.Hq / a.d.H) <= 8;
+cudaError_t launch_paged_decode(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
+  const bool one = int64_t(a.max_chunk) * (a.d.Hq / a.d.H) <= 8;
   if (a.d.d == 64) return one ? launch_decode<64, 1>(a, num_sms, st) : launch_decode<64, 2>(a, num_sms, st);
   return one ? launch_decode<128, 1>(a, num_sms, st) : launch_decode<128, 2>(a, num_sms, st);
 }

@@ -29,6 +29,8 @@
 namespace mot {
 namespace {
 
+constexpr int kLeast = 1, kMost = 16;   // units of a share (a piece's start, end and join cost about as much as eight)
+
 template <int D>
 struct Pf {
   static constexpr int kBM = 256, kTK = 128;
@@ -49,7 +51,7 @@ struct PfShared {
   uint64_t k_full[2], k_empty[2], v_full[3], v_ready[3], v_empty[3], drain;
   uint32_t tmem;
   int32_t abort;
-  int32_t last;              // this CTA joins the item
+  PagedJoinShared join;
   int32_t pieces;            // pieces finished
   uint32_t notes[4][4][4];   // [piece & 3][tile of the masked ones][128 keys]: values that are not finite
 };
@@ -61,31 +63,34 @@ __device__ __forceinline__ int first_masked(const PagedSeq& s, int G, int row0) 
   return p < 0 ? 0 : (p + 1) >> 7;
 }
 
-// Joins an item's pieces in the order of their CTAs, a thread per row. Here the partial rows lie by
-// fours of columns, [D / 4][256 rows][4], so that the threads of a warp write and read whole lines.
+// Joins a group's places in order, a thread per row: to the output, or into its first place. Here the
+// partial rows lie by fours of columns, [D / 4][256 rows][4], so that the threads of a warp write and
+// read whole lines.
 template <int D>
-__device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCursor& c, const PagedPiece& p, int r) {
+__device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCursor& c, const PagedGroup& g, int r) {
   constexpr int BM = Pf<D>::kBM;
-  const int G = a.d.Hq / a.d.H, row = c.rt * BM + r, n = p.c1 - p.c0 + 1;
+  const int G = a.d.Hq / a.d.H, row = c.rt * BM + r;
   if (row >= c.s.m * G) return;
-  auto part = [&](int k) { return paged_part<BM, D>(a, p.c0 + k, k == 0); };
-  float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < n; ++k) m = fmaxf(m, __ldcg(part(k) + BM * D + r));
-  m = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-  for (int k = 0; k < n; ++k)
-    l = fmaf(exp2f(__ldcg(part(k) + BM * D + r) - m), __ldcg(part(k) + BM * (D + 1) + r), l);
+  float high = -INFINITY, l = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < g.n; ++k) high = fmaxf(high, __ldcg(paged_place<BM, D>(a, g, k) + BM * D + r));
+  const float m = high == -INFINITY ? 0.f : high;
+#pragma unroll 8
+  for (int k = 0; k < g.n; ++k) {
+    const float* pk = paged_place<BM, D>(a, g, k);
+    l = fmaf(exp2f(__ldcg(pk + BM * D + r) - m), __ldcg(pk + BM * (D + 1) + r), l);
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   uint16_t* dst = static_cast<uint16_t*>(a.out) + paged_out_row(c, a.d.H, G, row) * D;
+  float* to = paged_place<BM, D>(a, g, 0);
 #pragma unroll 1
   for (int e = 0; e < D / 32; ++e) {   // 32 columns at a time
     float o[32];
 #pragma unroll
     for (int k = 0; k < 32; ++k) o[k] = 0.f;
 #pragma unroll 2
-    for (int k = 0; k < n; ++k) {
-      const float* pk = part(k);
+    for (int k = 0; k < g.n; ++k) {
+      const float* pk = paged_place<BM, D>(a, g, k);
       const float f = exp2f(__ldcg(pk + BM * D + r) - m);
       const float4* src = reinterpret_cast<const float4*>(pk) + 8 * e * BM + r;
 #pragma unroll
@@ -97,6 +102,13 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCur
         o[4 * x + 3] = fmaf(f, v.w, o[4 * x + 3]);
       }
     }
+    if (!g.final) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        __stcg(reinterpret_cast<float4*>(to) + (8 * e + x) * BM + r,
+               make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]));
+      continue;
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint32_t w[4];
@@ -107,6 +119,10 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCur
       }
       reinterpret_cast<uint4*>(dst + 32 * e)[k] = make_uint4(w[0], w[1], w[2], w[3]);
     }
+  }
+  if (!g.final) {   // the row's own thread alone reads these
+    __stcg(to + BM * D + r, high);
+    __stcg(to + BM * (D + 1) + r, l);
   }
 }
 
@@ -131,7 +147,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
   const long long wl = a.wait_limit;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(&sh.abort);
   PagedCursor c;
-  if (!paged_begin<F::kBM, F::kTK>(a, scan, &s_cur, c)) return;   // uniform over the CTA
+  if (!paged_begin<F::kBM, F::kTK>(a, kLeast, kMost, scan, &s_cur, c)) return;   // uniform over the CTA
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -511,10 +527,17 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
         break;
       }
       if (part) {
-        if (tid == 128) sh.last = paged_arrive(a, p);
+        if (tid == 128) sh.join.mine = paged_arrive(a, p, sh.join.g);
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (*reinterpret_cast<volatile int32_t*>(&sh.last))
-          join_rows<D>(a, c, p, tid - 128);
+        if (sh.join.mine) {
+          join_rows<D>(a, c, sh.join.g, i * 128 + r);
+          if (!sh.join.g.final) {
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (tid == 128) sh.join.mine = paged_arrive_group(a, p, sh.join.g);
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (sh.join.mine) join_rows<D>(a, c, sh.join.g, i * 128 + r);
+          }
+        }
       }
       if (tid == 128) *reinterpret_cast<volatile int32_t*>(&sh.pieces) = piece + 1;
       paged_next<F::kBM, F::kTK>(a, c, p);
@@ -546,7 +569,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
       PagedCursor w = s_cur;
       for (int piece = 0; w.u < w.u_end; ++piece) {
         const PagedPiece p = paged_piece<F::kBM, F::kTK>(w, G);
-        if (piece >= sh.pieces && !p.whole) paged_arrive(a, p);
+        if (piece >= sh.pieces && !p.whole) paged_arrive_owed(a, p);
         paged_next<F::kBM, F::kTK>(a, w, p);
       }
       atomicOr(a.status, kStatusTimeout);

@@ -95,6 +95,7 @@ struct PagedAttnArgs {
   float* part;
   int32_t* count;
   int32_t* status;
+  int32_t max_chunk;      // most rows of an entry: a hint for the split, never relied on
   long long wait_limit;   // bound of every pipeline wait (SM cycles)
   int32_t stall_test;     // test hook: the tensor-core kernel's first CTA loads nothing
 };
@@ -102,9 +103,9 @@ constexpr int kPagedMaxGroup = 16;   // query heads per key/value head
 size_t paged_part_floats(const PagedDims& d, int num_sms);
 int paged_counters(int num_sms);
 // fp32.
-cudaError_t launch_paged_simt(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st);
+cudaError_t launch_paged_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st);
 // bf16, few rows per key/value head (any number is right).
-cudaError_t launch_paged_decode(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st);
+cudaError_t launch_paged_decode(const PagedAttnArgs& a, int num_sms, cudaStream_t st);
 // Chunks in bf16 on the tensor cores: maps over the layer's pools as rows [n_pages * H * P][d], box 64 x P.
 bool paged_fmha_takes(const PagedDims& d, int max_chunk);
 cudaError_t launch_paged_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV,

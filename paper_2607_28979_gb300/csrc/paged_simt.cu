@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kTK = 64;
 constexpr int kSimtThreads = 256;
+constexpr int kLeast = 1, kMost = 8;   // units of a share
 
 template <int D, int BM>
 struct Simt {
@@ -30,7 +31,6 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
   using P = Simt<D, BM>;
   constexpr int kR = BM / 16;     // rows of a thread
   constexpr int kC = D / 64;      // float4 columns of a thread
-  static_assert(paged_join_floats<BM>() <= kTK * (2 * D + 4), "the keys' and values' place holds the join");
   extern __shared__ float4 smem4[];
   float* sq = reinterpret_cast<float*>(smem4);
   float* sk = sq + BM * P::kLd;
@@ -38,11 +38,11 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
   float* sp = sv + kTK * D;
   __shared__ int64_t sh[33];
   __shared__ PagedCursor s_cur;
-  __shared__ int s_last;
+  __shared__ PagedJoinShared s_join;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int H = a.d.H, G = a.d.Hq / H;
   PagedCursor c;
-  if (!paged_begin<BM, kTK>(a, sh, &s_cur, c)) return;
+  if (!paged_begin<BM, kTK>(a, kLeast, kMost, sh, &s_cur, c)) return;
   const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
 
   while (c.u < c.u_end) {
@@ -203,13 +203,10 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
           part[BM * (D + 1) + r] = l[i];
         }
       }
-      __syncthreads();
-      if (tid == 0) s_last = paged_arrive(a, p);
-      __syncthreads();
-      if (s_last) paged_join<float, BM, D>(a, c, p, sk, tid, kSimtThreads);
+      paged_finish<float, BM, D>(a, c, p, s_join, tid, kSimtThreads);
     }
     paged_next<BM, kTK>(a, c, p);
-    __syncthreads();   // s_last and the queries are read
+    __syncthreads();   // s_join and the queries are read
   }
 }
 
@@ -224,15 +221,15 @@ cudaError_t launch_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
 
 }  // namespace
 
-// Two places per CTA: 256 rows with one CTA per SM, fewer rows with more.
+// Two places per CTA: 256 rows with one CTA per SM, fewer rows with more. Three counters per CTA.
 size_t paged_part_floats(const PagedDims& d, int num_sms) { return size_t(num_sms) * 2 * 256 * (d.d + 2); }
-int paged_counters(int num_sms) { return num_sms * 4; }
+int paged_counters(int num_sms) { return num_sms * 4 * 3; }
 bool paged_fmha_takes(const PagedDims& d, int max_chunk) {
   return d.dtype == 0 && int64_t(max_chunk) * (d.Hq / d.H) > 16;
 }
 
-cudaError_t launch_paged_simt(const PagedAttnArgs& a, int num_sms, int max_chunk, cudaStream_t st) {
-  const bool few = int64_t(max_chunk) * (a.d.Hq / a.d.H) <= 16;
+cudaError_t launch_paged_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
+  const bool few = int64_t(a.max_chunk) * (a.d.Hq / a.d.H) <= 16;
   if (a.d.d == 64) return few ? launch_simt<64, 16>(a, num_sms, st) : launch_simt<64, 64>(a, num_sms, st);
   return few ? launch_simt<128, 16>(a, num_sms, st) : launch_simt<128, 64>(a, num_sms, st);
 }
