@@ -578,8 +578,7 @@ mot_status mot_paged_load(mot_handle h, const mot_paged_cache* cache, int32_t fi
  *     (a cos t - b sin t, b cos t + a sin t), t as in mot_paged_config,
  * in fp32 with angles exact for any position, and rounded once. q goes to
  * q_out [rows][q_heads][head_dim] (which may be q itself where its rows are
- * contiguous), k and v into the pages. Rows of no entry are not read or
- * written.
+ * contiguous), k and v into the pages. Rows of no entry give nothing.
  */
 mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cache,
                             const mot_paged_batch* batch, const void* q, int64_t q_stride,

@@ -1980,7 +1980,7 @@ mot_status mot_paged_fork(mot_handle h, const mot_paged_cache* cache, const int3
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   MOT_CUDA_TRY(timed(h, "paged_fork_plan", st,
                      [&] { return launch_paged_fork_plan(h->pd, c, src, dst, n, h->pw, st); }));
-  MOT_CUDA_TRY(timed(h, "paged_fork", st, [&] { return launch_paged_fork(h->pd, c, src, dst, n, h->pw, st); }));
+  MOT_CUDA_TRY(timed(h, "paged_fork", st, [&] { return launch_paged_fork(h->pd, c, src, dst, n, h->pw, !h->profile, st); }));
   return MOT_OK;
 }
 
@@ -2009,7 +2009,7 @@ mot_status mot_paged_compact(mot_handle h, const mot_paged_cache* cache, int32_t
   MOT_CUDA_TRY(timed(h, "paged_compact_plan", st,
                      [&] { return launch_paged_compact_plan(h->pd, c, live, h->pw, st); }));
   MOT_CUDA_TRY(timed(h, "paged_compact", st,
-                     [&] { return launch_paged_compact(h->pd, c, h->pw, h->num_sms, st); }));
+                     [&] { return launch_paged_compact(h->pd, c, h->pw, h->num_sms, !h->profile, st); }));
   return MOT_OK;
 }
 

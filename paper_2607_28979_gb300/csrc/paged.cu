@@ -204,6 +204,7 @@ __device__ __forceinline__ int elem_bytes(const PagedDims& d) { return d.dtype ?
 __global__ void __launch_bounds__(kCopyThreads)
     paged_fork_kernel(const PagedDims d, const PagedCache c, const int32_t* src, const int32_t* dst, int n,
                       const PagedWork w) {
+  pdl_enter();   // behind the plan
   if (refused(w.status)) return;
   const int i = blockIdx.y, tid = threadIdx.x;
   const int a = src[i], b = dst[i], len = c.lens[a];
@@ -279,6 +280,7 @@ __global__ void __launch_bounds__(kPlanThreads)
 // The moves' pages, all layers; the table's entries at or above the count of pages in use follow.
 __global__ void __launch_bounds__(kCopyThreads)
     paged_compact_kernel(const PagedDims d, const PagedCache c, const PagedWork w) {
+  pdl_enter();   // behind the plan
   const int n = w.count[0], used = w.count[1];
   if (n == 0) return;
   const int vecs = d.H * d.P * d.d * elem_bytes(d) / 16;   // of a page in one layer
@@ -358,44 +360,43 @@ __global__ void __launch_bounds__(kCopyThreads)
 
 // ---------------------------------------------------------------- append
 //
-// A row's query, key and value heads, each on d / kV lanes of kV elements (16 bytes): the norm is a
-// sum over those lanes, a pair's other half the shuffle from lane +- rot / 2 / kV. Angles: F_i =
-// base^(-2 i / rot) / (2 pi) turns per position as a 64-bit fraction, so pos * F_i mod 2^64 is the
-// angle in turns, exact to 2^-44 for any position below 2^20; each is evaluated once per row, in
-// shared memory, for all heads.
-constexpr int kAppendThreads = 256;
-constexpr int kAppendRows = 4;
+// A warp takes some rows, one after another, in steps of 2 or 4 heads (queries, then keys with their
+// values): d / 8 lanes per head with 8 elements each, in two groups of four: i .. i + 3 and i + rot / 2
+// .. in the half-and-half layout of the rotation, so that a pair's elements are in one lane (no shuffles
+// but the norm's sum), 8 in a row otherwise. A lane's angles and norm weights are the same for every
+// head; fp32 in packed pairs. Angles: F_i = base^(-2 i / rot) / (2 pi) turns per position as a 64-bit
+// fraction, so the upper half of pos * F_i mod 2^64 is the angle in 2^-32 turns (1.5e-9), for any
+// position below 2^30.
+constexpr int kAppendThreads = 128;
+constexpr int kAppendDepth = 4;   // steps with their loads in flight
 
 template <class T>
-struct Vec16 {
-  static constexpr int kV = 16 / sizeof(T);
+struct Four;   // four elements, as two pairs of fp32
+template <>
+struct Four<uint16_t> {
+  uint2 u;
+  __device__ __forceinline__ void unpack(uint64_t (&x)[2]) const {
+    x[0] = (uint64_t(u.x & 0xFFFF0000u) << 32) | (u.x << 16);
+    x[1] = (uint64_t(u.y & 0xFFFF0000u) << 32) | (u.y << 16);
+  }
+  __device__ __forceinline__ void pack(const uint64_t (&x)[2]) {
+    __nv_bfloat162 a = __floats2bfloat162_rn(lo_f(x[0]), hi_f(x[0])), b = __floats2bfloat162_rn(lo_f(x[1]), hi_f(x[1]));
+    u = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+  }
+  static __device__ __forceinline__ float lo_f(uint64_t x) { return __uint_as_float(uint32_t(x)); }
+  static __device__ __forceinline__ float hi_f(uint64_t x) { return __uint_as_float(uint32_t(x >> 32)); }
 };
-__device__ __forceinline__ void unpack16(uint4 u, float (&x)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+template <>
+struct Four<float> {
+  uint4 u;
+  __device__ __forceinline__ void unpack(uint64_t (&x)[2]) const {
+    x[0] = (uint64_t(u.y) << 32) | u.x;
+    x[1] = (uint64_t(u.w) << 32) | u.z;
   }
-}
-__device__ __forceinline__ void unpack16(uint4 u, float (&x)[4]) {
-  x[0] = __uint_as_float(u.x);
-  x[1] = __uint_as_float(u.y);
-  x[2] = __uint_as_float(u.z);
-  x[3] = __uint_as_float(u.w);
-}
-__device__ __forceinline__ uint4 pack16(const float (&x)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    w[i] = *reinterpret_cast<uint32_t*>(&v);
+  __device__ __forceinline__ void pack(const uint64_t (&x)[2]) {
+    u = make_uint4(uint32_t(x[0]), uint32_t(x[0] >> 32), uint32_t(x[1]), uint32_t(x[1] >> 32));
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ uint4 pack16(const float (&x)[4]) {
-  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-}
+};
 
 // The last entry i with starts[i] <= row, by a 32-way search of one warp.
 __device__ __forceinline__ int entry_of(const int32_t* starts, int n, int row) {
@@ -412,121 +413,203 @@ __device__ __forceinline__ int entry_of(const int32_t* starts, int n, int row) {
   return lo;
 }
 
-template <class T>
-__global__ void __launch_bounds__(kAppendThreads)
-    paged_append_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w) {
-  constexpr int kV = Vec16<T>::kV;
-  __shared__ float2 cs[kAppendRows][128 / 2];   // cos, sin of a row's angles
-  __shared__ int s_pos[kAppendRows];            // position, -1: a row of no entry
-  __shared__ int s_page[kAppendRows];           // page of the position, -1: nothing is stored
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+enum { kRotNone = 0, kRotHalves = 1, kRotPairs = 2 };
+
+// cos and sin of t / 2^32 turns: the nearest quarter turn off, then their series to x^10 and x^9 (off by
+// 2^-29 at most on |x| <= pi / 4).
+__device__ __forceinline__ float2 cos_sin_turns(uint32_t t) {
+  const uint32_t quarter = (t + 0x20000000u) >> 30;
+  const float x = float(int32_t(t - (quarter << 30))) * 1.46291807926715968e-9f;   // 2 pi / 2^32
+  const float z = x * x;
+  const float sn = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), x);
+  const float cn =
+      fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800, 1.f / 40320), -1.f / 720), 1.f / 24), -0.5f), 1.f);
+  const float c = quarter & 1u ? sn : cn, s = quarter & 1u ? cn : sn;
+  return make_float2((quarter + 1u) & 2u ? -c : c, quarter & 2u ? -s : s);
+}
+
+template <class T, int D, int ROT>
+__global__ void __launch_bounds__(kAppendThreads, 6)
+    paged_append_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w, int rows_each,
+                        int parts) {
+  using F = Four<T>;
+  constexpr int kLph = D / 8, kAtOnce = 32 / kLph, kStep = kAtOnce * D;   // lanes per head; heads and elements of a step
+  __shared__ __align__(16) float2 cs[kAppendThreads / 32][D / 2];        // cos, sin of a row's angles
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (refused(w.status)) return;
-  const int lph = d.d / kV;                     // lanes per head: 8, 16 or 32
-  const int heads = d.Hq + 2 * d.H, per_pass = kAppendThreads / lph;
-  const int el = tid & (lph - 1), e0 = el * kV; // this lane's elements of a head
+  const int sub = lane / kLph, el = lane % kLph;           // this lane's head and place in it
   const int half = d.rot >> 1;
-  for (int row0 = blockIdx.x * kAppendRows; row0 < p.b.rows; row0 += gridDim.x * kAppendRows) {
-    const int nr = min(kAppendRows, p.b.rows - row0);
-    __syncthreads();   // the rows before are done
-    if (warp < nr) {
-      const int row = row0 + warp;
+  const bool turned = ROT != kRotNone && 8 * el < d.rot;   // the lane's elements are rotated
+  const bool halves = ROT == kRotHalves && turned;
+  const int eA = halves ? 4 * el : 8 * el, eB = halves ? half + 4 * el : 8 * el + 4;
+  uint64_t wq[4], wk[4];
+  auto weights = [&](const void* src, uint64_t (&x)[4]) {
+    if (!src) return;
+    uint64_t a[2], b[2];
+    reinterpret_cast<const F*>(static_cast<const T*>(src) + eA)->unpack(a);
+    reinterpret_cast<const F*>(static_cast<const T*>(src) + eB)->unpack(b);
+    x[0] = a[0];
+    x[1] = a[1];
+    x[2] = b[0];
+    x[3] = b[1];
+  };
+  weights(p.q_norm, wq);
+  weights(p.k_norm, wk);
+  // steps 0 .. sq - 1: queries, .. sq + sk - 1: a step of keys and one of values; this warp's: [s0, s1)
+  const int sq = (d.Hq + kAtOnce - 1) / kAtOnce, sk = (d.H + kAtOnce - 1) / kAtOnce, steps = sq + sk;
+  const int unit = blockIdx.x * (kAppendThreads / 32) + warp, part = unit % parts;
+  const int per = (steps + parts - 1) / parts, s0 = part * per, s1 = min(steps, s0 + per);
+  const int row_begin = min(int64_t(unit / parts) * rows_each, int64_t(p.b.rows));
+  const int row_end = min(row_begin + rows_each, p.b.rows);
+  const int off = sub * D + eA, ab = eB - eA;              // the lane's first group in a step, and the second behind it
+  const int pool_step = (kAtOnce * D) << d.lp;             // from a step's rows of a page to the next's
+  int first = 0, last = 0, pos0 = 0;   // rows [first, last) are of one entry; row r's position is pos0 + r
+  int slot = -1, page = -1;
+  for (int row = row_begin; row < row_end; ++row) {
+    const T* q = static_cast<const T*>(p.q) + row * p.q_stride + off;
+    F a[kAppendDepth], b[kAppendDepth];
+    auto load_q = [&](int st) {
+#pragma unroll
+      for (int y = 0; y < kAppendDepth; ++y)
+        if (st + y < min(sq, s1) && (st + y) * kAtOnce + sub < d.Hq) {
+          a[y] = *reinterpret_cast<const F*>(q + (st + y) * kStep);
+          b[y] = *reinterpret_cast<const F*>(q + (st + y) * kStep + ab);
+        }
+    };
+    load_q(s0);   // under way while the row's place is found
+    const bool fresh = row < first || row >= last;
+    if (fresh) {
       const int i = entry_of(p.b.starts, p.b.n, row);
-      if (lane == 0) {
-        int pos = -1, page = -1;
-        if (p.b.n > 0 && row >= p.b.starts[i] && row < p.b.starts[i + 1]) {
-          const PagedSeq s = paged_seq(d, p.b, c.lens, w.status, i);
-          pos = s.len - s.m + (row - s.r0);
-          if (pos < 0)
-            atomicOr(w.status, kStatusPageUse);
-          else {
-            page = c.table[int64_t(s.slot) * d.max_pages + (pos >> d.lp)];
-            if (page < 0 || page >= d.n_pages) {
-              atomicOr(w.status, kStatusPageUse);
-              page = -1;
-            }
-          }
-        }
-        s_pos[warp] = pos;
-        s_page[warp] = page;
+      const int from = p.b.starts[i], to = p.b.starts[i + 1];
+      first = row;
+      last = row + 1;
+      slot = -1;
+      if (row >= from && row < to) {
+        const PagedSeq s = paged_seq(d, p.b, c.lens, w.status, i);
+        if (row < s.r0 + s.m) last = s.r0 + s.m;   // starts that are out of order: this row alone
+        slot = s.slot;
+        pos0 = s.len - s.m - s.r0;
       }
     }
-    __syncthreads();
-    for (int t = tid; t < nr * half; t += kAppendThreads) {
-      const int r = t / half, k = t - r * half;
-      if (s_pos[r] >= 0) {
-        const int64_t turns = int64_t(uint64_t(s_pos[r]) * p.freq[k]);
-        float sn, cn;
-        sincospif(__ll2float_rn(turns) * 0x1p-63f, &sn, &cn);
-        cs[r][k] = make_float2(cn, sn);
+    const int pos = slot < 0 ? -1 : pos0 + row;
+    if (pos < 0) {   // a row of no entry, or of one that is shorter than its rows
+      if (fresh && row >= p.b.starts[0] && row < p.b.starts[p.b.n] && lane == 0) atomicOr(w.status, kStatusPageUse);
+      continue;
+    }
+    if (fresh || (pos & (d.P - 1)) == 0) {
+      page = c.table[int64_t(slot) * d.max_pages + (pos >> d.lp)];
+      if (page < 0 || page >= d.n_pages) {
+        page = -1;
+        if (lane == 0) atomicOr(w.status, kStatusPageUse);
       }
     }
-    __syncthreads();
-    for (int x0 = 0; x0 < nr * heads; x0 += per_pass) {
-      const int x = x0 + tid / lph;
-      const bool in = x < nr * heads;
-      const int r = in ? x / heads : 0, h = in ? x - r * heads : 0;
-      const int pos = s_pos[r], page = s_page[r];
-      const int64_t row = row0 + r;
-      const bool is_q = h < d.Hq, is_k = !is_q && h < d.Hq + d.H;
-      const int hk = is_q ? 0 : (is_k ? h - d.Hq : h - d.Hq - d.H);
-      const bool live = in && pos >= 0;
-      const T* src = is_q ? static_cast<const T*>(p.q) + row * p.q_stride + h * d.d
-                          : (is_k ? static_cast<const T*>(p.k) + row * p.k_stride
-                                  : static_cast<const T*>(p.v) + row * p.v_stride) + hk * d.d;
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (live) u = *reinterpret_cast<const uint4*>(src + e0);
-      if (is_q || is_k) {
-        float y[kV];
-        unpack16(u, y);
-        const T* nw = static_cast<const T*>(is_q ? p.q_norm : p.k_norm);
-        if (nw) {
-          float ss = 0.f;
+    uint64_t tc[2] = {}, ts[2] = {};   // cos and sin of the lane's four angles, in pairs
+    if (ROT != kRotNone) {
 #pragma unroll
-          for (int e = 0; e < kV; ++e) ss = fmaf(y[e], y[e], ss);
-          // the group's lanes are of one kind: a head is a query, a key or a value as a whole
-          const uint32_t mask = lph == 32 ? 0xffffffffu : ((1u << lph) - 1) << (lane & ~(lph - 1));
-          for (int o = lph >> 1; o; o >>= 1) ss += __shfl_xor_sync(mask, ss, o);
-          const float f = rsqrtf(ss / float(d.d) + d.eps);
-          float g[kV];
-          unpack16(*reinterpret_cast<const uint4*>(nw + e0), g);
-#pragma unroll
-          for (int e = 0; e < kV; ++e) y[e] = y[e] * f * g[e];
-        }
-        if (d.rot_pairs) {
-          if (e0 < d.rot)
-#pragma unroll
-            for (int e = 0; e < kV; e += 2) {
-              const float2 t = cs[r][(e0 + e) >> 1];
-              const float a = y[e], b = y[e + 1];
-              y[e] = a * t.x - b * t.y;
-              y[e + 1] = b * t.x + a * t.y;
-            }
-        } else if (d.rot) {
-          // element e pairs with e +- rot / 2, rot / 2 / kV lanes away
-          const int off = half / kV;
-          const bool lo = e0 < half, rotated = e0 < d.rot;
-          const int from = rotated ? (lo ? lane + off : lane - off) : lane;
-          const uint32_t mask = lph == 32 ? 0xffffffffu : ((1u << lph) - 1) << (lane & ~(lph - 1));
-#pragma unroll
-          for (int e = 0; e < kV; ++e) {
-            const float other = __shfl_sync(mask, y[e], from);
-            if (rotated) {
-              const float2 t = cs[r][lo ? e0 + e : e0 + e - half];
-              y[e] = lo ? y[e] * t.x - other * t.y : y[e] * t.x + other * t.y;
-            }
-          }
-        }
-        if (nw || d.rot) u = pack16(y);
+      for (int k = lane; k < D / 2; k += 32)
+        if (k < half) cs[warp][k] = cos_sin_turns(uint32_t(uint64_t(pos) * p.freq[k] >> 32));
+      __syncwarp();
+      if (turned) {
+        const float4 x = *reinterpret_cast<const float4*>(&cs[warp][4 * el]);
+        const float4 y = *reinterpret_cast<const float4*>(&cs[warp][4 * el + 2]);
+        tc[0] = f32x2(x.x, x.z);
+        tc[1] = f32x2(y.x, y.z);
+        ts[0] = f32x2(x.y, x.w);
+        ts[1] = f32x2(y.y, y.w);
       }
-      if (!live) continue;
-      if (is_q)
-        *reinterpret_cast<uint4*>(static_cast<T*>(p.q_out) + (row * d.Hq + h) * d.d + e0) = u;
-      else if (page >= 0) {
-        T* pool = static_cast<T*>(is_k ? c.k : c.v) + int64_t(p.layer) * d.n_pages * d.H * d.P * d.d;
-        *reinterpret_cast<uint4*>(pool + paged_row(d, page, hk, pos) * d.d + e0) = u;
+      __syncwarp();   // before the next row's
+    }
+    auto work = [&](F& fa, F& fb, bool norm, const uint64_t (&wt)[4]) {   // by the whole warp
+      uint64_t f[2], g[2];
+      fa.unpack(f);
+      fb.unpack(g);
+      if (norm) {
+        const uint64_t sq2 = ffma_x2(g[1], g[1], ffma_x2(g[0], g[0], ffma_x2(f[1], f[1], fmul_x2(f[0], f[0]))));
+        float ss = __uint_as_float(uint32_t(sq2)) + __uint_as_float(uint32_t(sq2 >> 32));
+#pragma unroll
+        for (int o = kLph / 2; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        const float rs = rsqrtf(fmaf(ss, 1.f / D, d.eps));
+        const uint64_t r2 = f32x2(rs, rs);
+        f[0] = fmul_x2(fmul_x2(f[0], r2), wt[0]);
+        f[1] = fmul_x2(fmul_x2(f[1], r2), wt[1]);
+        g[0] = fmul_x2(fmul_x2(g[0], r2), wt[2]);
+        g[1] = fmul_x2(fmul_x2(g[1], r2), wt[3]);
+      }
+      if (halves) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint64_t u = f[e], v = g[e], ns = ts[e] ^ 0x8000000080000000ull;
+          f[e] = ffma_x2(v, ns, fmul_x2(u, tc[e]));
+          g[e] = ffma_x2(u, ts[e], fmul_x2(v, tc[e]));
+        }
+      } else if (ROT == kRotPairs && turned) {
+        // the pairs of angles 0, 1 are f's, those of 2, 3 g's: (x c - y s, y c + x s)
+        auto turn = [](uint64_t v, float cn, float sn) {
+          const float x = __uint_as_float(uint32_t(v)), y = __uint_as_float(uint32_t(v >> 32));
+          return f32x2(x * cn - y * sn, y * cn + x * sn);
+        };
+        auto lo = [](uint64_t v) { return __uint_as_float(uint32_t(v)); };
+        auto hi = [](uint64_t v) { return __uint_as_float(uint32_t(v >> 32)); };
+        f[0] = turn(f[0], lo(tc[0]), lo(ts[0]));
+        f[1] = turn(f[1], hi(tc[0]), hi(ts[0]));
+        g[0] = turn(g[0], lo(tc[1]), lo(ts[1]));
+        g[1] = turn(g[1], hi(tc[1]), hi(ts[1]));
+      }
+      fa.pack(f);
+      fb.pack(g);
+    };
+    T* q_out = static_cast<T*>(p.q_out) + int64_t(row) * d.Hq * D + off;
+    for (int sb = s0; sb < min(sq, s1); sb += kAppendDepth) {
+      if (sb != s0) load_q(sb);
+#pragma unroll
+      for (int y = 0; y < kAppendDepth; ++y) {
+        const int st = sb + y;
+        if (st >= min(sq, s1)) break;
+        if (ROT != kRotNone || p.q_norm) work(a[y], b[y], p.q_norm != nullptr, wq);
+        if (st * kAtOnce + sub < d.Hq) {
+          *reinterpret_cast<F*>(q_out + st * kStep) = a[y];
+          *reinterpret_cast<F*>(q_out + st * kStep + ab) = b[y];
+        }
+      }
+    }
+    if (s1 <= sq || page < 0) continue;
+    const int64_t pool = ((int64_t(p.layer) * d.n_pages + page) * d.H * d.P + (pos & (d.P - 1))) * D +
+                         (int64_t(sub * D) << d.lp) + eA;
+    const T* k = static_cast<const T*>(p.k) + row * p.k_stride + off;
+    const T* v = static_cast<const T*>(p.v) + row * p.v_stride + off;
+    T* k_out = static_cast<T*>(c.k) + pool;
+    T* v_out = static_cast<T*>(c.v) + pool;
+    constexpr int kPairs = kAppendDepth / 2;   // steps of keys and of values at a time
+    for (int sb = max(s0, sq) - sq; sb < s1 - sq; sb += kPairs) {
+#pragma unroll
+      for (int y = 0; y < kPairs; ++y)
+        if (sb + y < s1 - sq && (sb + y) * kAtOnce + sub < d.H) {
+          a[y] = *reinterpret_cast<const F*>(k + (sb + y) * kStep);
+          b[y] = *reinterpret_cast<const F*>(k + (sb + y) * kStep + ab);
+          a[kPairs + y] = *reinterpret_cast<const F*>(v + (sb + y) * kStep);
+          b[kPairs + y] = *reinterpret_cast<const F*>(v + (sb + y) * kStep + ab);
+        }
+#pragma unroll
+      for (int y = 0; y < kPairs; ++y) {
+        const int st = sb + y;
+        if (st >= s1 - sq) break;
+        if (ROT != kRotNone || p.k_norm) work(a[y], b[y], p.k_norm != nullptr, wk);
+        if (st * kAtOnce + sub < d.H) {
+          const int64_t at = int64_t(st) * pool_step;
+          *reinterpret_cast<F*>(k_out + at) = a[y];
+          *reinterpret_cast<F*>(k_out + at + ab) = b[y];
+          *reinterpret_cast<F*>(v_out + at) = a[kPairs + y];
+          *reinterpret_cast<F*>(v_out + at + ab) = b[kPairs + y];
+        }
       }
     }
   }
+}
+
+template <class T, int D>
+auto append_kernel(const PagedDims& d) {
+  return d.rot == 0 ? paged_append_kernel<T, D, kRotNone>
+                    : d.rot_pairs ? paged_append_kernel<T, D, kRotPairs> : paged_append_kernel<T, D, kRotHalves>;
 }
 
 int grid_of(int64_t items, int num_sms, int per_sm) {
@@ -549,17 +632,17 @@ cudaError_t launch_paged_fork_plan(const PagedDims& d, const PagedCache& c, cons
   return launch_kernel(false, paged_fork_plan_kernel, 1, kPlanThreads, 0, st, d, c, src, dst, n, w);
 }
 cudaError_t launch_paged_fork(const PagedDims& d, const PagedCache& c, const int32_t* src, const int32_t* dst,
-                              int32_t n, const PagedWork& w, cudaStream_t st) {
+                              int32_t n, const PagedWork& w, bool overlap, cudaStream_t st) {
   const int x = grid_of(int64_t(2) * d.L * d.H, 64, 1);
-  return launch_kernel(false, paged_fork_kernel, dim3(x, n), kCopyThreads, 0, st, d, c, src, dst, n, w);
+  return launch_kernel(overlap, paged_fork_kernel, dim3(x, n), kCopyThreads, 0, st, d, c, src, dst, n, w);
 }
 cudaError_t launch_paged_compact_plan(const PagedDims& d, const PagedCache& c, int32_t* live,
                                       const PagedWork& w, cudaStream_t st) {
   return launch_kernel(false, paged_compact_plan_kernel, 1, kPlanThreads, 0, st, d, c, live, w);
 }
 cudaError_t launch_paged_compact(const PagedDims& d, const PagedCache& c, const PagedWork& w, int num_sms,
-                                 cudaStream_t st) {
-  return launch_kernel(false, paged_compact_kernel, num_sms * 8, kCopyThreads, 0, st, d, c, w);
+                                 bool overlap, cudaStream_t st) {
+  return launch_kernel(overlap, paged_compact_kernel, num_sms * 8, kCopyThreads, 0, st, d, c, w);
 }
 cudaError_t launch_paged_copy(const PagedDims& d, const PagedCache& c, const PagedCopy& p, const PagedWork& w,
                               int num_sms, cudaStream_t st) {
@@ -568,9 +651,19 @@ cudaError_t launch_paged_copy(const PagedDims& d, const PagedCache& c, const Pag
 }
 cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const PagedAppend& p,
                                 const PagedWork& w, int num_sms, cudaStream_t st) {
-  const int grid = grid_of((int64_t(p.b.rows) + kAppendRows - 1) / kAppendRows, num_sms, 8);
-  auto kern = d.dtype ? paged_append_kernel<float> : paged_append_kernel<uint16_t>;
-  return launch_kernel(false, kern, grid, kAppendThreads, 0, st, d, c, p, w);
+  // few rows: a row's heads over several warps, all of their loads in flight; many: a warp takes a row, or
+  // some in a row, which share the search for their entry
+  constexpr int kWarps = kAppendThreads / 32;
+  const int at_once = 256 / d.d, steps = (d.Hq + at_once - 1) / at_once + (d.H + at_once - 1) / at_once;
+  const int64_t fill = int64_t(num_sms) * 24;   // warps that are resident
+  const int most = (steps + kAppendDepth - 1) / kAppendDepth;
+  const int parts = p.b.rows >= fill ? 1 : int(fill / p.b.rows < most ? fill / p.b.rows : most);
+  const int rows_each = int((p.b.rows * int64_t(parts) + fill - 1) / fill);
+  const int64_t units = (int64_t(p.b.rows) + rows_each - 1) / rows_each * parts;
+  const int grid = int((units + kWarps - 1) / kWarps);
+  auto kern = d.dtype == 0 ? (d.d == 64 ? append_kernel<uint16_t, 64>(d) : append_kernel<uint16_t, 128>(d))
+                           : (d.d == 64 ? append_kernel<float, 64>(d) : append_kernel<float, 128>(d));
+  return launch_kernel(false, kern, grid, kAppendThreads, 0, st, d, c, p, w, rows_each, parts);
 }
 
 }  // namespace mot

@@ -49,15 +49,16 @@ cudaError_t launch_paged_reserve(const PagedDims& d, const PagedCache& c, const 
 cudaError_t launch_paged_free(const PagedDims& d, const PagedCache& c, const int32_t* seqs, int32_t n,
                               const PagedWork& w, int num_sms, cudaStream_t st);
 // plan: takes the pages and writes the moves (one per fork, from = -1 without a copy); then the
-// copies, with the table rows.
+// copies, with the table rows. overlap: the launch may start before the plan has finished.
 cudaError_t launch_paged_fork_plan(const PagedDims& d, const PagedCache& c, const int32_t* src,
                                    const int32_t* dst, int32_t n, const PagedWork& w, cudaStream_t st);
 cudaError_t launch_paged_fork(const PagedDims& d, const PagedCache& c, const int32_t* src,
-                              const int32_t* dst, int32_t n, const PagedWork& w, cudaStream_t st);
+                              const int32_t* dst, int32_t n, const PagedWork& w, bool overlap,
+                              cudaStream_t st);
 cudaError_t launch_paged_compact_plan(const PagedDims& d, const PagedCache& c, int32_t* live,
                                       const PagedWork& w, cudaStream_t st);
 cudaError_t launch_paged_compact(const PagedDims& d, const PagedCache& c, const PagedWork& w, int num_sms,
-                                 cudaStream_t st);
+                                 bool overlap, cudaStream_t st);
 // Contiguous [n_layers][B][H][S][d] <-> the pages of layers first ..; store: into the pages.
 struct PagedCopy {
   const int32_t* seqs;
