@@ -1980,7 +1980,7 @@ mot_status mot_paged_fork(mot_handle h, const mot_paged_cache* cache, const int3
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   MOT_CUDA_TRY(timed(h, "paged_fork_plan", st,
                      [&] { return launch_paged_fork_plan(h->pd, c, src, dst, n, h->pw, st); }));
-  MOT_CUDA_TRY(timed(h, "paged_fork", st, [&] { return launch_paged_fork(h->pd, c, src, dst, n, h->pw, !h->profile, st); }));
+  MOT_CUDA_TRY(timed(h, "paged_fork", st, [&] { return launch_paged_fork(h->pd, c, src, dst, n, h->pw, h->num_sms, !h->profile, st); }));
   return MOT_OK;
 }
 

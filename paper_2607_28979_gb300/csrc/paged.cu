@@ -632,8 +632,10 @@ cudaError_t launch_paged_fork_plan(const PagedDims& d, const PagedCache& c, cons
   return launch_kernel(false, paged_fork_plan_kernel, 1, kPlanThreads, 0, st, d, c, src, dst, n, w);
 }
 cudaError_t launch_paged_fork(const PagedDims& d, const PagedCache& c, const int32_t* src, const int32_t* dst,
-                              int32_t n, const PagedWork& w, bool overlap, cudaStream_t st) {
-  const int x = grid_of(int64_t(2) * d.L * d.H, 64, 1);
+                              int32_t n, const PagedWork& w, int num_sms, bool overlap, cudaStream_t st) {
+  // as many blocks as are resident, a block's pieces of a page evenly
+  const int64_t pieces = int64_t(2) * d.L * d.H, most = (int64_t(num_sms) * 8 + n - 1) / n;
+  const int x = int(pieces < most ? pieces : most);
   return launch_kernel(overlap, paged_fork_kernel, dim3(x, n), kCopyThreads, 0, st, d, c, src, dst, n, w);
 }
 cudaError_t launch_paged_compact_plan(const PagedDims& d, const PagedCache& c, int32_t* live,

@@ -135,111 +135,27 @@ struct PagedCursor {
   int32_t coarse;        // units of a piece; 0: runs
   int32_t i, hk, rt, kt; // the next unit
   // runs: the CTA that unit x belongs to
-  __device__ __forceinline__ int owner(int64_t x) const { return int(((x + 1) * C - 1) / W); }
+  __device__ __forceinline__ int owner(int64_t x) const;
 };
 
-// The share of CTA blockIdx.x: a run of `least` units at least where there are as many, or a piece of
-// `least` to `most` units. Called by all threads; `sh` and `out` are shared. False: no work.
-template <int BM, int TK>
-__device__ bool paged_begin(const PagedAttnArgs& a, int least, int most, int64_t* sh, PagedCursor* out,
-                            PagedCursor& c) {
-  using S = PagedSplit<BM, TK>;
-  const int G = a.d.Hq / a.d.H, H = a.d.H, T = blockDim.x, tid = threadIdx.x;
-  const int n = a.b.n;
-  // all entries' units, in pieces of f; `at`, `mine`: of this thread's entry among the last T entries
-  int64_t mine = 0, at = 0;
-  PagedSeq ms{-1, 0, 0, 0};
-  if (n <= T && tid < n) ms = paged_seq(a.d, a.b, a.lens, a.status, tid);
-  auto total = [&](int f) -> int64_t {
-    int64_t W = 0;
-    for (int i0 = 0; i0 < n; i0 += T) {
-      if (n > T) {   // more entries than threads: a piece at a time
-        ms.m = 0;
-        if (i0 + tid < n) ms = paged_seq(a.d, a.b, a.lens, a.status, i0 + tid);
-      }
-      mine = ms.m ? H * S::head_units(ms, G, f) : 0;
-      int64_t t;
-      at = W + block_scan(mine, sh, t);
-      W += t;
-    }
-    return W;
-  };
-  int64_t W = total(1);
-  if (W == 0) return false;
-  const int64_t grid = gridDim.x;
-  // the items of the batch: pieces of f units make W / f + items of them at most
-  const int64_t items = int64_t(H) * (int64_t(a.max_chunk) * G <= BM ? n : int64_t(a.b.rows) * G / BM + n);
-  int f = 0;
-  if (items < grid) {
-    const int64_t need = (W + grid - items - 1) / (grid - items);
-    if (need <= most) {
-      f = need < least ? least : int(need);
-      if (f > 1) W = total(f);
-      if (W > grid) {   // max_chunk was no bound: runs
-        f = 0;
-        W = total(1);
-      }
-    }
-  }
-  int C;
-  int64_t u, u_end;
-  if (f) {
-    C = int(W);
-    u = blockIdx.x;
-    u_end = u + 1;
-  } else {
-    const int64_t runs = (W + least - 1) / least;
-    C = runs < grid ? int(runs) : int(grid);
-    u = W * int(blockIdx.x) / C;
-    u_end = W * (int(blockIdx.x) + 1) / C;
-  }
-  if (int(blockIdx.x) >= C) return false;
-  const int ff = f ? f : 1;
-  int64_t carry = 0;
-  for (int i0 = 0; i0 < n; i0 += T) {
-    if (n > T) {
-      ms.m = 0;
-      if (i0 + tid < n) ms = paged_seq(a.d, a.b, a.lens, a.status, i0 + tid);
-      mine = ms.m ? H * S::head_units(ms, G, ff) : 0;
-      int64_t t;
-      at = carry + block_scan(mine, sh, t);
-      carry += t;
-    }
-    if (u >= at && u < at + mine) {
-      PagedCursor o;
-      o.i = i0 + tid;
-      o.s = ms;
-      o.W = W;
-      o.C = C;
-      o.coarse = f;
-      o.u = u;
-      o.u_end = u_end;
-      const int64_t head_u = mine / H;
-      int64_t r = u - at;
-      o.hk = int(r / head_u);
-      r -= o.hk * head_u;
-      int lo = 0, hi = S::row_tiles(o.s.m, G) - 1;   // the last rt with before(rt) <= r
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (S::before(o.s, G, mid, ff) <= r) lo = mid;
-        else hi = mid - 1;
-      }
-      o.rt = lo;
-      o.kt = int(r - S::before(o.s, G, lo, ff)) * ff;
-      *out = o;
-    }
-    if (n > T && carry > u) break;
-  }
-  __syncthreads();
-  c = *out;
-  return true;
+// a / b for a, b >= 0, in 32 bits where they fit (a 64-bit division takes some hundred cycles).
+__device__ __forceinline__ int64_t div_fast(int64_t a, int64_t b) {
+  return uint64_t(a | b) >> 32 ? a / b : int64_t(uint32_t(a) / uint32_t(b));
 }
+
+__device__ __forceinline__ int PagedCursor::owner(int64_t x) const { return int(div_fast((x + 1) * C - 1, W)); }
 
 // One piece of a share: units [kt, kt + n) of the item's `units`.
 struct PagedPiece {
   int32_t kt, n, units;
   bool whole;
   int32_t c0, c1;   // the item's CTAs, in order
+};
+// A share in shared memory: in registers it would be spilled by the loops that it stands around.
+struct PagedShare {
+  PagedCursor c;
+  PagedPiece p;
+  int32_t work;   // whether this CTA has a share, or is not through it
 };
 template <int BM, int TK>
 __device__ __forceinline__ PagedPiece paged_piece(const PagedCursor& c, int G) {
@@ -263,7 +179,7 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedCursor& c, int G) {
   }
   return p;
 }
-// Behind a piece; loads the next entry where the run goes on to it. Uniform over the CTA.
+// Behind a piece; loads the next entry where the run goes on to it.
 template <int BM, int TK>
 __device__ __forceinline__ void paged_next(const PagedAttnArgs& a, PagedCursor& c, const PagedPiece& p) {
   using S = PagedSplit<BM, TK>;
@@ -278,6 +194,116 @@ __device__ __forceinline__ void paged_next(const PagedAttnArgs& a, PagedCursor& 
   do {   // ends: units are left, so an entry with rows follows
     c.s = paged_seq(a.d, a.b, a.lens, a.status, ++c.i);
   } while (c.s.m == 0 && c.i + 1 < a.b.n);
+}
+// The same on a share, in one thread.
+template <int BM, int TK>
+__device__ __forceinline__ void paged_step(const PagedAttnArgs& a, PagedShare& st) {
+  paged_next<BM, TK>(a, st.c, st.p);
+  st.work = st.c.u < st.c.u_end;
+  if (st.work) st.p = paged_piece<BM, TK>(st.c, a.d.Hq / a.d.H);
+}
+
+// The share of CTA blockIdx.x, with its first piece: a run of `least` units at least where there are as
+// many, or a piece of `least` to `most` units. Called by all threads, which see st (in shared memory, as
+// sh) behind it. Up to 32 entries are one warp's, an entry per lane, without a barrier between.
+template <int BM, int TK>
+__device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, int most, int64_t* sh, PagedShare& st) {
+  using S = PagedSplit<BM, TK>;
+  const int G = a.d.Hq / a.d.H, H = a.d.H, n = a.b.n;
+  const bool by_warp = n <= 32;
+  const int T = by_warp ? 32 : int(blockDim.x), me = threadIdx.x;
+  if (threadIdx.x == 0) st.work = 0;
+  if (!by_warp) __syncthreads();
+  if (!by_warp || threadIdx.x < 32) {
+    auto scan = [&](int64_t v, int64_t& t) -> int64_t {
+      if (!by_warp) return block_scan(v, sh, t);
+      int64_t x = v;
+      for (int o = 1; o < n; o <<= 1) {   // the lanes from n on have nothing
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (me >= o) x += y;
+      }
+      t = __shfl_sync(0xffffffffu, x, n - 1);
+      return x - v;
+    };
+    // all entries' units, in pieces of f; `at`, `mine`: of this thread's entry among the last T entries
+    int64_t mine = 0, at = 0;
+    PagedSeq ms{-1, 0, 0, 0};
+    if (n <= T && me < n) ms = paged_seq(a.d, a.b, a.lens, a.status, me);
+    auto total = [&](int f) -> int64_t {
+      int64_t W = 0;
+      for (int i0 = 0; i0 < n; i0 += T) {
+        if (n > T) {   // more entries than threads: a piece at a time
+          ms.m = 0;
+          if (i0 + me < n) ms = paged_seq(a.d, a.b, a.lens, a.status, i0 + me);
+        }
+        mine = ms.m ? H * S::head_units(ms, G, f) : 0;
+        int64_t t;
+        at = W + scan(mine, t);
+        W += t;
+      }
+      return W;
+    };
+    int64_t W = total(1);
+    const int64_t grid = gridDim.x;
+    // the items of the batch: pieces of f units make W / f + items of them at most
+    const int64_t items = int64_t(H) * (int64_t(a.max_chunk) * G <= BM ? n : int64_t(a.b.rows) * G / BM + n);
+    int f = 0;
+    if (items < grid && W > 0) {
+      const int64_t need = div_fast(W + grid - items - 1, grid - items);
+      if (need <= most) {
+        f = need < least ? least : int(need);
+        if (f > 1) W = total(f);
+        if (W > grid) {   // max_chunk was no bound: runs
+          f = 0;
+          W = total(1);
+        }
+      }
+    }
+    const int64_t runs = div_fast(W + least - 1, least);
+    const int C = f || runs < grid ? int(f ? W : runs) : int(grid);
+    if (int(blockIdx.x) < C) {
+      const int64_t u = f ? int64_t(blockIdx.x) : div_fast(W * int(blockIdx.x), C);
+      const int ff = f ? f : 1;
+      int64_t carry = 0;
+      for (int i0 = 0; i0 < n; i0 += T) {
+        if (n > T) {
+          ms.m = 0;
+          if (i0 + me < n) ms = paged_seq(a.d, a.b, a.lens, a.status, i0 + me);
+          mine = ms.m ? H * S::head_units(ms, G, ff) : 0;
+          int64_t t;
+          at = carry + scan(mine, t);
+          carry += t;
+        }
+        if (u >= at && u < at + mine) {
+          PagedCursor o;
+          o.i = i0 + me;
+          o.s = ms;
+          o.W = W;
+          o.C = C;
+          o.coarse = f;
+          o.u = u;
+          o.u_end = f ? u + 1 : div_fast(W * (int(blockIdx.x) + 1), C);
+          const int64_t head_u = div_fast(mine, H);
+          int64_t r = u - at;
+          o.hk = int(div_fast(r, head_u));
+          r -= o.hk * head_u;
+          int lo = 0, hi = S::row_tiles(o.s.m, G) - 1;   // the last rt with before(rt) <= r
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (S::before(o.s, G, mid, ff) <= r) lo = mid;
+            else hi = mid - 1;
+          }
+          o.rt = lo;
+          o.kt = int(r - S::before(o.s, G, lo, ff)) * ff;
+          st.c = o;
+          st.p = paged_piece<BM, TK>(o, G);
+          st.work = 1;
+        }
+        if (n > T && carry > u) break;
+      }
+    }
+  }
+  __syncthreads();
 }
 
 // Partial results of a piece: rows [BM][D] of sum_j 2^(s_j - m) v_j, then [BM] m and [BM] l = sum_j

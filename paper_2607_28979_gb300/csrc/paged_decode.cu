@@ -45,26 +45,31 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
 
+// CTAs per SM: as many as have their registers without spilling (16 warps of D = 128 that spill: 91 us
+// for two contexts of 131,072 and 70,001, 12 that do not: 78).
 template <int D, int NT>
-__global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_kernel(const PagedAttnArgs a) {
+constexpr int kResident = (D == 64 ? 5 : 4) - NT;
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kDecThreads, kResident<D, NT>) paged_decode_kernel(const __grid_constant__ PagedAttnArgs a) {
   constexpr int BM = 8 * NT, TK = kDecTK, kI = D / 32, kH = D / 64;
   constexpr int kLd = D + 4;
   __shared__ int64_t scan[33];
-  __shared__ PagedCursor s_cur;
+  __shared__ PagedShare st;
   __shared__ PagedJoinShared s_join;
   __shared__ __align__(16) float so[kWarps][BM][kLd];   // read and written 16 bytes at a time
   __shared__ float sm[kWarps][BM], sl[kWarps][BM];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int H = a.d.H, G = a.d.Hq / H;
-  PagedCursor c;
-  if (!paged_begin<BM, TK>(a, kLeast, kMost, scan, &s_cur, c)) return;
+  paged_begin<BM, TK>(a, kLeast, kMost, scan, st);
+  const PagedCursor& c = st.c;
+  const PagedPiece& p = st.p;
   const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
   const uint16_t* kp = static_cast<const uint16_t*>(a.k);
   const uint16_t* vp = static_cast<const uint16_t*>(a.v);
 
-  while (c.u < c.u_end) {
-    const PagedPiece p = paged_piece<BM, TK>(c, G);
-    const int r0 = c.rt * BM, n_rows = min(BM, c.s.m * G - r0), len = c.s.len;
+  while (st.work) {
+    const int r0 = c.rt * BM, n_rows = min(BM, c.s.m * G - r0), len = c.s.len, hk = c.hk, slot = c.s.slot;
     uint4 q[NT][kI];
     int pos[NT][2];   // rows 8 nt + 2 t, + 1 see the keys 0 .. pos
 #pragma unroll
@@ -97,17 +102,17 @@ __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_ker
         for (int e = 0; e < 16; ++e) o[n][h][e >> 2][e & 3] = 0.f;
 
     // lane l holds the page of this warp's block in tile `base` + l
-    int base = p.kt, held = 0;
-    const int kt_end = p.kt + p.n;
+    const int kt_begin = p.kt, kt_end = kt_begin + p.n;
+    int base = kt_begin, held = 0;
     auto hold = [&](int kt) {
       base = kt;
       const int k = (kt + lane) * TK + 16 * warp;
-      held = kt + lane < kt_end && k < len ? paged_page(a.d, a.table, a.status, c.s.slot, k) : 0;
+      held = kt + lane < kt_end && k < len ? paged_page(a.d, a.table, a.status, slot, k) : 0;
     };
-    hold(p.kt);
+    hold(kt_begin);
     auto row_of = [&](int kt) -> int64_t {   // pool row of the block's first key
       if (kt - base >= 32) hold(kt);
-      return paged_row(a.d, __shfl_sync(0xffffffffu, held, kt - base), c.hk, kt * TK + 16 * warp);
+      return paged_row(a.d, __shfl_sync(0xffffffffu, held, kt - base), hk, kt * TK + 16 * warp);
     };
     uint4 kr[2][kI], vr[4][kH];
     auto load_k = [&](int kt, int64_t row) {
@@ -131,10 +136,10 @@ __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_ker
         for (int h = 0; h < kH; ++h) vr[e][h] = in ? ld_stream(src + 64 * h) : make_uint4(0u, 0u, 0u, 0u);
       }
     };
-    int64_t row = row_of(p.kt);
-    load_k(p.kt, row);
-    load_v(p.kt, row);
-    for (int kt = p.kt; kt < kt_end; ++kt) {
+    int64_t row = row_of(kt_begin);
+    load_k(kt_begin, row);
+    load_v(kt_begin, row);
+    for (int kt = kt_begin; kt < kt_end; ++kt) {
       const int k0 = kt * TK + 16 * warp;
       float s[NT][4];
 #pragma unroll
@@ -247,7 +252,7 @@ __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_ker
           }
         }
       if (odd) {
-        const int64_t at = paged_row(a.d, paged_page(a.d, a.table, a.status, c.s.slot, k0), c.hk, k0);
+        const int64_t at = paged_row(a.d, paged_page(a.d, a.table, a.status, slot, k0), hk, k0);
         for (int j = 0; j < 16 && k0 + j < len; ++j)
 #pragma unroll
           for (int h = 0; h < kH; ++h)
@@ -314,14 +319,15 @@ __global__ void __launch_bounds__(kDecThreads, NT == 1 ? 4 : 3) paged_decode_ker
       }
     }
     if (part) paged_finish<uint16_t, BM, D>(a, c, p, s_join, tid, kDecThreads);
-    __syncthreads();   // so and s_join are read
-    paged_next<BM, TK>(a, c, p);
+    __syncthreads();   // st, so and s_join are read
+    if (tid == 0) paged_step<BM, TK>(a, st);
+    __syncthreads();
   }
 }
 
 template <int D, int NT>
 cudaError_t launch_decode(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
-  return launch_kernel(false, paged_decode_kernel<D, NT>, num_sms * (NT == 1 ? 4 : 3), kDecThreads, 0, st, a);
+  return launch_kernel(false, paged_decode_kernel<D, NT>, num_sms * kResident<D, NT>, kDecThreads, 0, st, a);
 }
 
 }  // namespace

@@ -52,7 +52,6 @@ struct PfShared {
   uint32_t tmem;
   int32_t abort;
   PagedJoinShared join;
-  int32_t pieces;            // pieces finished
   uint32_t notes[4][4][4];   // [piece & 3][tile of the masked ones][128 keys]: values that are not finite
 };
 static_assert(sizeof(PfShared) <= 1024, "barrier block");
@@ -129,7 +128,7 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCur
 template <int D>
 __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     paged_fmha_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                      const PagedAttnArgs a) {
+                      const __grid_constant__ PagedAttnArgs a) {
   using F = Pf<D>;
   constexpr int kHalves = D / 64;
   extern __shared__ uint8_t smem_raw[];
@@ -140,14 +139,15 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
   uint8_t* sV = sK + F::kNK * F::kTile;     // kNV tiles
   PfShared& sh = *reinterpret_cast<PfShared*>(sV + F::kNV * F::kTile);
   __shared__ int64_t scan[33];
-  __shared__ PagedCursor s_cur;
+  __shared__ PagedShare share;   // the softmax warps'
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = a.d.H, G = a.d.Hq / H;
   const long long wl = a.wait_limit;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(&sh.abort);
-  PagedCursor c;
-  if (!paged_begin<F::kBM, F::kTK>(a, kLeast, kMost, scan, &s_cur, c)) return;   // uniform over the CTA
+  paged_begin<F::kBM, F::kTK>(a, kLeast, kMost, scan, share);
+  if (!share.work) return;   // uniform over the CTA
+  PagedCursor c = share.c;   // of the other roles, each for itself
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -166,7 +166,6 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     }
     mbar_init(&sh.drain, 1);
     sh.abort = 0;
-    sh.pieces = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
@@ -365,8 +364,10 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
     uint32_t t = 0;   // tiles of this stream
     bool ok = true;
-    for (int piece = 0; ok && c.u < c.u_end; ++piece) {
-      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+    const PagedCursor& c = share.c;
+    const PagedPiece& p = share.p;
+    for (int piece = 0;; ++piece) {
+      const int kt_end = p.kt + p.n;
       const int row = c.rt * F::kBM + i * 128 + r, n_rows = c.s.m * G;
       const bool active = n_rows - c.rt * F::kBM > i * 128;   // the stream has rows
       const bool valid = row < n_rows;
@@ -386,7 +387,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_ready[i]);
-        for (int kt = p.kt; kt < p.kt + p.n; ++kt, ++t) {
+        for (int kt = p.kt; kt < kt_end; ++kt, ++t) {
           if (!wait(&sh.s_full[i], t & 1u)) {
             ok = false;
             break;
@@ -539,8 +540,10 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
           }
         }
       }
-      if (tid == 128) *reinterpret_cast<volatile int32_t*>(&sh.pieces) = piece + 1;
-      paged_next<F::kBM, F::kTK>(a, c, p);
+      asm volatile("bar.sync 1, 256;" ::: "memory");   // everyone has read the share
+      if (tid == 128) paged_step<F::kBM, F::kTK>(a, share);
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (!share.work) break;
     }
   }
 
@@ -566,12 +569,8 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
       }
     }
     if (tid == 128) {   // the arrivals that are still owed, so that the counters are zero for the next call
-      PagedCursor w = s_cur;
-      for (int piece = 0; w.u < w.u_end; ++piece) {
-        const PagedPiece p = paged_piece<F::kBM, F::kTK>(w, G);
-        if (piece >= sh.pieces && !p.whole) paged_arrive_owed(a, p);
-        paged_next<F::kBM, F::kTK>(a, w, p);
-      }
+      for (; share.work; paged_step<F::kBM, F::kTK>(a, share))   // from the piece that was not finished
+        if (!share.p.whole) paged_arrive_owed(a, share.p);
       atomicOr(a.status, kStatusTimeout);
     }
     __syncthreads();

@@ -53,8 +53,8 @@ cudaError_t launch_paged_free(const PagedDims& d, const PagedCache& c, const int
 cudaError_t launch_paged_fork_plan(const PagedDims& d, const PagedCache& c, const int32_t* src,
                                    const int32_t* dst, int32_t n, const PagedWork& w, cudaStream_t st);
 cudaError_t launch_paged_fork(const PagedDims& d, const PagedCache& c, const int32_t* src,
-                              const int32_t* dst, int32_t n, const PagedWork& w, bool overlap,
-                              cudaStream_t st);
+                              const int32_t* dst, int32_t n, const PagedWork& w, int num_sms,
+                              bool overlap, cudaStream_t st);
 cudaError_t launch_paged_compact_plan(const PagedDims& d, const PagedCache& c, int32_t* live,
                                       const PagedWork& w, cudaStream_t st);
 cudaError_t launch_paged_compact(const PagedDims& d, const PagedCache& c, const PagedWork& w, int num_sms,

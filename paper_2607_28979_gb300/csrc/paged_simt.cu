@@ -27,7 +27,7 @@ __device__ __forceinline__ bool finite4(const float4& v) {
 }
 
 template <int D, int BM>
-__global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_constant__ PagedAttnArgs a) {
   using P = Simt<D, BM>;
   constexpr int kR = BM / 16;     // rows of a thread
   constexpr int kC = D / 64;      // float4 columns of a thread
@@ -37,16 +37,16 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
   float* sv = sk + kTK * P::kLd;
   float* sp = sv + kTK * D;
   __shared__ int64_t sh[33];
-  __shared__ PagedCursor s_cur;
+  __shared__ PagedShare st;
   __shared__ PagedJoinShared s_join;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int H = a.d.H, G = a.d.Hq / H;
-  PagedCursor c;
-  if (!paged_begin<BM, kTK>(a, kLeast, kMost, sh, &s_cur, c)) return;
+  paged_begin<BM, kTK>(a, kLeast, kMost, sh, st);
+  const PagedCursor& c = st.c;
+  const PagedPiece& p = st.p;
   const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
 
-  while (c.u < c.u_end) {
-    const PagedPiece p = paged_piece<BM, kTK>(c, G);
+  while (st.work) {
     const int r0 = c.rt * BM, n_rows = min(BM, c.s.m * G - r0);
     // the rows' queries
     for (int x = tid; x < BM * (D / 4); x += kSimtThreads) {
@@ -70,8 +70,9 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
 #pragma unroll
       for (int e = 0; e < 4 * kC; ++e) o[i][e] = 0.f;
     }
-    for (int kt = p.kt; kt < p.kt + p.n; ++kt) {
-      const int k0 = kt * kTK, n_keys = min(kTK, c.s.len - k0);
+    const int len = c.s.len, kt_end = p.kt + p.n;
+    for (int kt = p.kt; kt < kt_end; ++kt) {
+      const int k0 = kt * kTK, n_keys = min(kTK, len - k0);
       bool odd = false;   // an infinite or NaN value in a tile that is masked for some rows
       for (int x = tid; x < kTK * (D / 4); x += kSimtThreads) {
         const int j = x / (D / 4), col = (x - j * (D / 4)) * 4;
@@ -205,8 +206,9 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedAtt
       }
       paged_finish<float, BM, D>(a, c, p, s_join, tid, kSimtThreads);
     }
-    paged_next<BM, kTK>(a, c, p);
-    __syncthreads();   // s_join and the queries are read
+    __syncthreads();   // st, s_join and the queries are read
+    if (tid == 0) paged_step<BM, kTK>(a, st);
+    __syncthreads();
   }
 }
 
@@ -215,7 +217,7 @@ cudaError_t launch_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
   static SmemOptIn opt_in;
   auto kern = paged_simt_kernel<D, BM>;
   if (cudaError_t e = opt_in(kern, Simt<D, BM>::kSmem)) return e;
-  const int per_sm = BM == 16 ? 2 : 1;
+  const int per_sm = BM == 16 ? 2 : 1;   // 64 rows at D = 64 fit twice, but make twice the pieces: 24.8 -> 28.6 us
   return launch_kernel(false, kern, num_sms * per_sm, kSimtThreads, Simt<D, BM>::kSmem, st, a);
 }
 

@@ -377,10 +377,11 @@ def mot_paged_load(h: Handle, cache: mot_paged_cache, seqs, n: int, dst_k, dst_v
 
 
 def _row_stride(x, what: str) -> int:
-    stride, shape = x.stride(), x.shape
-    if len(shape) != 3 or stride[2] != 1 or stride[1] != shape[2]:
-        raise ValueError(f"{what}: [rows][heads][head_dim] with contiguous rows is wanted")
-    return stride[0] if shape[0] > 1 else max(stride[0], shape[1] * shape[2])
+    if x.dim() == 3:
+        rows, heads, last = x.stride()
+        if last == 1 and heads == x.size(2):
+            return rows if x.size(0) > 1 else max(rows, x.size(1) * heads)
+    raise ValueError(f"{what}: [rows][heads][head_dim] with contiguous rows is wanted")
 
 
 def mot_paged_append(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, k, v, q_out,
