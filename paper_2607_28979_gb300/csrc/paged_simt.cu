@@ -4,7 +4,10 @@
 //                       query head of the group) of one key/value head at a time, in tiles of 64
 //                       keys: scores, running maximum and sum (base 2), and the output rows in
 //                       registers, 16 x 16 threads; keys, values and probabilities of the tile in
-//                       shared memory. The work is dealt to the CTAs as paged_common.cuh says.
+//                       shared memory, the next tile's copies under way. Bound by the FMAs' issue, so
+//                       both products run on pairs of fp32: a score sums the even and the odd
+//                       dimensions apart, an output pair takes its probability doubled from shared
+//                       memory. The work is dealt to the CTAs as paged_common.cuh says.
 #include "paged_common.cuh"
 
 namespace mot {
@@ -17,14 +20,22 @@ constexpr int kLeast = 1, kMost = 8;   // units of a share
 template <int D, int BM>
 struct Simt {
   static constexpr int kLd = D + 4;    // floats from a query or key row to the next: 16-byte rows, spread over banks
-  static constexpr int kLp = kTK + 4;  // of a probability row
-  static constexpr int kSmem = 4 * (BM * kLd + kTK * kLd + kTK * D + BM * kLp);
+  static constexpr int kLp = 2 * kTK + 4;          // of a row of doubled probabilities
+  static constexpr int kTile = kTK * (kLd + D);    // keys and values
+  static constexpr int kSmem = 4 * (BM * kLd + 2 * kTile + BM * kLp);
 };
 
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+// 16 bytes from global to shared memory, or zeros.
+__device__ __forceinline__ void cp_async_16_or_0(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ bool finite4(const float4& v) {
   return isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w);
 }
+__device__ __forceinline__ float lo_f(uint64_t x) { return __uint_as_float(uint32_t(x)); }
+__device__ __forceinline__ float hi_f(uint64_t x) { return __uint_as_float(uint32_t(x >> 32)); }
+// Four floats of shared memory as two pairs.
+__device__ __forceinline__ ulonglong2 pairs(const float* p) { return *reinterpret_cast<const ulonglong2*>(p); }
 
 template <int D, int BM>
 __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_constant__ PagedAttnArgs a) {
@@ -33,9 +44,8 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_c
   constexpr int kC = D / 64;      // float4 columns of a thread
   extern __shared__ float4 smem4[];
   float* sq = reinterpret_cast<float*>(smem4);
-  float* sk = sq + BM * P::kLd;
-  float* sv = sk + kTK * P::kLd;
-  float* sp = sv + kTK * D;
+  float* stage = sq + BM * P::kLd;      // two tiles: keys [kTK][kLd], values [kTK][D]
+  float* sp = stage + 2 * P::kTile;
   __shared__ int64_t sh[33];
   __shared__ PagedShare st;
   __shared__ PagedJoinShared s_join;
@@ -52,7 +62,8 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_c
     for (int x = tid; x < BM * (D / 4); x += kSimtThreads) {
       const int r = x / (D / 4), col = (x - r * (D / 4)) * 4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < n_rows) v = load4(static_cast<const float*>(a.q) + paged_out_row(c, H, G, r0 + r) * D + col);
+      if (r < n_rows)
+        v = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + paged_out_row(c, H, G, r0 + r) * D + col);
       *reinterpret_cast<float4*>(sq + r * P::kLd + col) = v;
     }
     int pos[kR];   // a row sees the keys 0 .. pos
@@ -62,61 +73,75 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_c
       pos[i] = r < n_rows ? c.s.len - c.s.m + (r0 + r) / G : -1;
     }
     const int first_pos = c.s.len - c.s.m + r0 / G;
-    float m[kR], l[kR], o[kR][4 * kC];
+    float m[kR], l[kR];
+    uint64_t o[kR][2 * kC];   // columns 64 h + 4 tx + 2 e, + 1 in o[i][2 h + e]
 #pragma unroll
     for (int i = 0; i < kR; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4 * kC; ++e) o[i][e] = 0.f;
+      for (int e = 0; e < 2 * kC; ++e) o[i][e] = 0ull;
     }
-    const int len = c.s.len, kt_end = p.kt + p.n;
+    const int len = c.s.len, kt_end = p.kt + p.n, slot = c.s.slot, hk = c.hk;
+    constexpr int kVecs = kTK * (D / 4) / kSimtThreads;   // of a thread, in keys and in values
+    auto fetch = [&](int kt) {
+      float* sk = stage + (kt & 1) * P::kTile;
+      float* sv = sk + kTK * P::kLd;
+#pragma unroll
+      for (int y = 0; y < kVecs; ++y) {
+        const int x = tid + y * kSimtThreads, j = x / (D / 4), col = (x - j * (D / 4)) * 4, pos_j = kt * kTK + j;
+        const bool in = pos_j < len;
+        const int64_t row =
+            in ? paged_row(a.d, paged_page(a.d, a.table, a.status, slot, pos_j), hk, pos_j) * D + col : 0;
+        cp_async_16_or_0(smem_u32(sk + j * P::kLd + col), static_cast<const float*>(a.k) + row, in);
+        cp_async_16_or_0(smem_u32(sv + j * D + col), static_cast<const float*>(a.v) + row, in);
+      }
+      cp_async_commit();
+    };
+    fetch(p.kt);
     for (int kt = p.kt; kt < kt_end; ++kt) {
       const int k0 = kt * kTK, n_keys = min(kTK, len - k0);
-      bool odd = false;   // an infinite or NaN value in a tile that is masked for some rows
-      for (int x = tid; x < kTK * (D / 4); x += kSimtThreads) {
-        const int j = x / (D / 4), col = (x - j * (D / 4)) * 4;
-        float4 kv = make_float4(0.f, 0.f, 0.f, 0.f), vv = kv;
-        if (j < n_keys) {
-          const int page = paged_page(a.d, a.table, a.status, c.s.slot, k0 + j);
-          const int64_t row = paged_row(a.d, page, c.hk, k0 + j) * D + col;
-          kv = load4(static_cast<const float*>(a.k) + row);
-          vv = load4(static_cast<const float*>(a.v) + row);
-          odd |= !finite4(vv);
-        }
-        *reinterpret_cast<float4*>(sk + j * P::kLd + col) = kv;
-        *reinterpret_cast<float4*>(sv + j * D + col) = vv;
+      const float* sk = stage + (kt & 1) * P::kTile;
+      const float* sv = sk + kTK * P::kLd;
+      if (kt + 1 < kt_end) {
+        fetch(kt + 1);
+        cp_async_wait_group<1>();
+      } else {
+        cp_async_wait_group<0>();
       }
-      odd = __syncthreads_or(odd && first_pos < k0 + n_keys - 1);
-      float s[kR][4];
+      bool odd = false;   // an infinite or NaN value in a tile that is masked for some rows
+      if (first_pos < k0 + n_keys - 1) {
+#pragma unroll
+        for (int y = 0; y < kVecs; ++y) {   // what this thread has copied
+          const int x = tid + y * kSimtThreads, j = x / (D / 4), col = (x - j * (D / 4)) * 4;
+          odd |= !finite4(*reinterpret_cast<const float4*>(sv + j * D + col));
+        }
+      }
+      odd = __syncthreads_or(odd);
+      uint64_t s2[kR][4];
 #pragma unroll
       for (int i = 0; i < kR; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+        for (int j = 0; j < 4; ++j) s2[i][j] = 0ull;
 #pragma unroll 4
       for (int e = 0; e < D; e += 4) {
-        float4 q4[kR], k4[4];
+        ulonglong2 q4[kR], k4[4];
 #pragma unroll
-        for (int i = 0; i < kR; ++i) q4[i] = *reinterpret_cast<const float4*>(sq + (ty * kR + i) * P::kLd + e);
+        for (int i = 0; i < kR; ++i) q4[i] = pairs(sq + (ty * kR + i) * P::kLd + e);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(sk + (tx + 16 * j) * P::kLd + e);
+        for (int j = 0; j < 4; ++j) k4[j] = pairs(sk + (tx + 16 * j) * P::kLd + e);
 #pragma unroll
         for (int i = 0; i < kR; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            s[i][j] = fmaf(q4[i].x, k4[j].x, s[i][j]);
-            s[i][j] = fmaf(q4[i].y, k4[j].y, s[i][j]);
-            s[i][j] = fmaf(q4[i].z, k4[j].z, s[i][j]);
-            s[i][j] = fmaf(q4[i].w, k4[j].w, s[i][j]);
-          }
+          for (int j = 0; j < 4; ++j) s2[i][j] = ffma_x2(q4[i].y, k4[j].y, ffma_x2(q4[i].x, k4[j].x, s2[i][j]));
       }
 #pragma unroll
       for (int i = 0; i < kR; ++i) {
-        float mx = m[i];
+        float mx = m[i], s[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          s[i][j] *= sl2;
-          if (k0 + tx + 16 * j <= pos[i]) mx = fmaxf(mx, s[i][j]);
+          s[j] = (lo_f(s2[i][j]) + hi_f(s2[i][j])) * sl2;
+          if (k0 + tx + 16 * j <= pos[i]) mx = fmaxf(mx, s[j]);
         }
 #pragma unroll
         for (int w = 8; w; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
@@ -126,55 +151,49 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_c
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float pr = k0 + tx + 16 * j <= pos[i] ? exp2f(s[i][j] - ms) : 0.f;
+          const float pr = k0 + tx + 16 * j <= pos[i] ? exp2f(s[j] - ms) : 0.f;
           sum += pr;
-          sp[(ty * kR + i) * P::kLp + tx + 16 * j] = pr;
+          *reinterpret_cast<float2*>(sp + (ty * kR + i) * P::kLp + 2 * (tx + 16 * j)) = make_float2(pr, pr);
         }
 #pragma unroll
         for (int w = 8; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
         l[i] = fmaf(l[i], f, sum);
+        const uint64_t f2 = f32x2(f, f);
 #pragma unroll
-        for (int e = 0; e < 4 * kC; ++e) o[i][e] *= f;
+        for (int e = 0; e < 2 * kC; ++e) o[i][e] = fmul_x2(o[i][e], f2);
       }
       __syncwarp();   // a row's probabilities are written and read by one half-warp
       if (!odd) {
-#pragma unroll 2
-        for (int j = 0; j < kTK; j += 4) {
-          float4 p4[kR];
+#pragma unroll 4
+        for (int j = 0; j < kTK; j += 2) {
+          ulonglong2 p2[kR];
 #pragma unroll
-          for (int i = 0; i < kR; ++i) p4[i] = *reinterpret_cast<const float4*>(sp + (ty * kR + i) * P::kLp + j);
+          for (int i = 0; i < kR; ++i) p2[i] = pairs(sp + (ty * kR + i) * P::kLp + 2 * j);
 #pragma unroll
-          for (int jj = 0; jj < 4; ++jj)
+          for (int h = 0; h < kC; ++h) {
+            const ulonglong2 v0 = pairs(sv + j * D + 64 * h + 4 * tx), v1 = pairs(sv + (j + 1) * D + 64 * h + 4 * tx);
 #pragma unroll
-            for (int h = 0; h < kC; ++h) {
-              const float4 v = *reinterpret_cast<const float4*>(sv + (j + jj) * D + 64 * h + 4 * tx);
-#pragma unroll
-              for (int i = 0; i < kR; ++i) {
-                const float pr = jj == 0 ? p4[i].x : jj == 1 ? p4[i].y : jj == 2 ? p4[i].z : p4[i].w;
-                o[i][4 * h] = fmaf(pr, v.x, o[i][4 * h]);
-                o[i][4 * h + 1] = fmaf(pr, v.y, o[i][4 * h + 1]);
-                o[i][4 * h + 2] = fmaf(pr, v.z, o[i][4 * h + 2]);
-                o[i][4 * h + 3] = fmaf(pr, v.w, o[i][4 * h + 3]);
-              }
+            for (int i = 0; i < kR; ++i) {
+              o[i][2 * h] = ffma_x2(p2[i].y, v1.x, ffma_x2(p2[i].x, v0.x, o[i][2 * h]));
+              o[i][2 * h + 1] = ffma_x2(p2[i].y, v1.y, ffma_x2(p2[i].x, v0.y, o[i][2 * h + 1]));
             }
+          }
         }
       } else {   // a masked key adds nothing, where 0 times its value would be NaN
         for (int j = 0; j < n_keys; ++j)
 #pragma unroll
           for (int i = 0; i < kR; ++i)
             if (k0 + j <= pos[i]) {
-              const float pr = sp[(ty * kR + i) * P::kLp + j];
+              const uint64_t pr = *reinterpret_cast<const uint64_t*>(sp + (ty * kR + i) * P::kLp + 2 * j);
 #pragma unroll
               for (int h = 0; h < kC; ++h) {
-                const float4 v = *reinterpret_cast<const float4*>(sv + j * D + 64 * h + 4 * tx);
-                o[i][4 * h] = fmaf(pr, v.x, o[i][4 * h]);
-                o[i][4 * h + 1] = fmaf(pr, v.y, o[i][4 * h + 1]);
-                o[i][4 * h + 2] = fmaf(pr, v.z, o[i][4 * h + 2]);
-                o[i][4 * h + 3] = fmaf(pr, v.w, o[i][4 * h + 3]);
+                const ulonglong2 v = pairs(sv + j * D + 64 * h + 4 * tx);
+                o[i][2 * h] = ffma_x2(pr, v.x, o[i][2 * h]);
+                o[i][2 * h + 1] = ffma_x2(pr, v.y, o[i][2 * h + 1]);
               }
             }
       }
-      __syncthreads();   // the tile is read; the next one may come
+      __syncthreads();   // the tile is read; the copies after the next may come
     }
     if (p.whole) {
 #pragma unroll
@@ -185,7 +204,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_c
         float* dst = static_cast<float*>(a.out) + paged_out_row(c, H, G, r0 + r) * D;
 #pragma unroll
         for (int h = 0; h < kC; ++h) {
-          const float t[4] = {o[i][4 * h], o[i][4 * h + 1], o[i][4 * h + 2], o[i][4 * h + 3]};
+          const float t[4] = {lo_f(o[i][2 * h]), hi_f(o[i][2 * h]), lo_f(o[i][2 * h + 1]), hi_f(o[i][2 * h + 1])};
           paged_store4(dst + 64 * h + 4 * tx, t, f);
         }
       }
@@ -198,7 +217,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_c
 #pragma unroll
         for (int h = 0; h < kC; ++h)
           *reinterpret_cast<float4*>(part + r * D + 64 * h + 4 * tx) =
-              make_float4(o[i][4 * h], o[i][4 * h + 1], o[i][4 * h + 2], o[i][4 * h + 3]);
+              make_float4(lo_f(o[i][2 * h]), hi_f(o[i][2 * h]), lo_f(o[i][2 * h + 1]), hi_f(o[i][2 * h + 1]));
         if (tx == 0) {
           part[BM * D + r] = m[i];
           part[BM * (D + 1) + r] = l[i];
@@ -217,7 +236,7 @@ cudaError_t launch_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st) {
   static SmemOptIn opt_in;
   auto kern = paged_simt_kernel<D, BM>;
   if (cudaError_t e = opt_in(kern, Simt<D, BM>::kSmem)) return e;
-  const int per_sm = BM == 16 ? 2 : 1;   // 64 rows at D = 64 fit twice, but make twice the pieces: 24.8 -> 28.6 us
+  const int per_sm = BM == 16 && D == 64 ? 2 : 1;   // by shared memory
   return launch_kernel(false, kern, num_sms * per_sm, kSimtThreads, Simt<D, BM>::kSmem, st, a);
 }
 
