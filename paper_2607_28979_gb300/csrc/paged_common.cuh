@@ -80,7 +80,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedDims& d, const PagedBat
 // The partial results of an item in several pieces are joined by the CTA that finishes last, in order.
 
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0, by the steps of Euclid's algorithm.
-__device__ inline int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+__device__ __noinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
   int64_t s = 0;
   while (n > 0) {
     s += n * (n - 1) / 2 * (a / m) + n * (b / m);

@@ -64,41 +64,52 @@ __device__ __forceinline__ int first_masked(const PagedSeq& s, int G, int row0) 
 
 // Joins a group's places in order, a thread per row: to the output, or into its first place. Here the
 // partial rows lie by fours of columns, [D / 4][256 rows][4], so that the threads of a warp write and
-// read whole lines.
+// read whole lines. 32 columns at a time, two places with all their loads in flight, under a running
+// maximum.
 template <int D>
 __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCursor& c, const PagedGroup& g, int r) {
   constexpr int BM = Pf<D>::kBM;
   const int G = a.d.Hq / a.d.H, row = c.rt * BM + r;
   if (row >= c.s.m * G) return;
-  float high = -INFINITY, l = 0.f;
-#pragma unroll 8
-  for (int k = 0; k < g.n; ++k) high = fmaxf(high, __ldcg(paged_place<BM, D>(a, g, k) + BM * D + r));
-  const float m = high == -INFINITY ? 0.f : high;
-#pragma unroll 8
-  for (int k = 0; k < g.n; ++k) {
-    const float* pk = paged_place<BM, D>(a, g, k);
-    l = fmaf(exp2f(__ldcg(pk + BM * D + r) - m), __ldcg(pk + BM * (D + 1) + r), l);
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
   uint16_t* dst = static_cast<uint16_t*>(a.out) + paged_out_row(c, a.d.H, G, row) * D;
   float* to = paged_place<BM, D>(a, g, 0);
+  float m = -INFINITY, l = 0.f;
 #pragma unroll 1
-  for (int e = 0; e < D / 32; ++e) {   // 32 columns at a time
+  for (int e = 0; e < D / 32; ++e) {
     float o[32];
 #pragma unroll
     for (int k = 0; k < 32; ++k) o[k] = 0.f;
-#pragma unroll 2
-    for (int k = 0; k < g.n; ++k) {
-      const float* pk = paged_place<BM, D>(a, g, k);
-      const float f = exp2f(__ldcg(pk + BM * D + r) - m);
-      const float4* src = reinterpret_cast<const float4*>(pk) + 8 * e * BM + r;
+    m = -INFINITY;   // the same in every pass
+    l = 0.f;
+#pragma unroll 1
+    for (int k0 = 0; k0 < g.n; k0 += 2) {
+      float mk[2], lk[2];
+      float4 v[2][8];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float* pk = paged_place<BM, D>(a, g, min(k0 + k, g.n - 1));
+        mk[k] = __ldcg(pk + BM * D + r);
+        lk[k] = __ldcg(pk + BM * (D + 1) + r);
+        const float4* src = reinterpret_cast<const float4*>(pk) + 8 * e * BM + r;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[k][x] = __ldcg(src + x * BM);
+      }
+      if (k0 + 1 >= g.n) mk[1] = -INFINITY;
+      const float up = fmax3(m, mk[0], mk[1]), ms = up == -INFINITY ? 0.f : up;
+      const float f = exp2f(m - ms), f0 = exp2f(mk[0] - ms), f1 = exp2f(mk[1] - ms);
+      const bool both = k0 + 1 < g.n;
+      m = up;
+      l = fmaf(f0, lk[0], l * f);
+      if (both) l = fmaf(f1, lk[1], l);
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
-        const float4 v = __ldcg(src + x * BM);
-        o[4 * x] = fmaf(f, v.x, o[4 * x]);
-        o[4 * x + 1] = fmaf(f, v.y, o[4 * x + 1]);
-        o[4 * x + 2] = fmaf(f, v.z, o[4 * x + 2]);
-        o[4 * x + 3] = fmaf(f, v.w, o[4 * x + 3]);
+        const float* u = reinterpret_cast<const float*>(&v[0][x]);
+        const float* w = reinterpret_cast<const float*>(&v[1][x]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          o[4 * x + y] = fmaf(f0, u[y], o[4 * x + y] * f);
+          if (both) o[4 * x + y] = fmaf(f1, w[y], o[4 * x + y]);
+        }
       }
     }
     if (!g.final) {
@@ -108,6 +119,7 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCur
                make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]));
       continue;
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint32_t w[4];
@@ -120,7 +132,7 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCur
     }
   }
   if (!g.final) {   // the row's own thread alone reads these
-    __stcg(to + BM * D + r, high);
+    __stcg(to + BM * D + r, m);
     __stcg(to + BM * (D + 1) + r, l);
   }
 }
@@ -145,11 +157,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
   const int H = a.d.H, G = a.d.Hq / H;
   const long long wl = a.wait_limit;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(&sh.abort);
-  paged_begin<F::kBM, F::kTK>(a, kLeast, kMost, scan, share);
-  if (!share.work) return;   // uniform over the CTA
-  PagedCursor c = share.c;   // of the other roles, each for itself
-
-  if (tid == 0) {
+  if (tid == 128) {   // while warp 0 deals out the work
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_ready[i], 4);
       mbar_init(&sh.s_full[i], 1);
@@ -174,10 +182,16 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     tmem_alloc(&sh.tmem, 512);
     tmem_relinquish();
   }
+  paged_begin<F::kBM, F::kTK>(a, kLeast, kMost, scan, share);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
+  if (!share.work) {   // uniform over the CTA
+    if (warp == 2) tmem_dealloc(tmem, 512);
+    return;
+  }
+  PagedCursor c = share.c;   // of the other roles, each for itself
   // Every lane of a warp waits, and all of them go on or none does.
   auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, wl));
