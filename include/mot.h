@@ -460,7 +460,7 @@ mot_status mot_replay_select(mot_handle h, const void* guide, const int32_t* seq
  * A batch (mot_paged_batch) names n distinct slots and their new rows: entry i
  * has the rows starts[i] .. starts[i + 1] - 1 (ascending, within 0 .. rows) of
  * the call's row buffers, its last m = starts[i + 1] - starts[i] positions in
- * order: row r is position lens - m + (r - starts[i]). `rows` (at most 2^26)
+ * order: row r is position lens - m + (r - starts[i]), rows there may be none. `rows` (at most 2^26)
  * and `max_chunk` (the most rows of an entry; rows where it is not known) are
  * host numbers that bound the work.
  *
@@ -496,9 +496,9 @@ typedef struct {
   int32_t max_pages;   /* entries of a slot's table row */
   int32_t rot_dim;     /* leading dimensions of a head that mot_paged_append rotates; 0: none */
   int32_t rot_pairs;   /* 0: dimension i with i + rot_dim / 2; 1: 2 i with 2 i + 1 */
-  float rot_base;      /* pair i turns by position * rot_base^(-2 i / rot_dim) */
-  float norm_eps;
   mot_dtype dtype;
+  float norm_eps;
+  double rot_base;     /* pair i turns by position * rot_base^(-2 i / rot_dim) */
 } mot_paged_config;
 
 typedef struct {

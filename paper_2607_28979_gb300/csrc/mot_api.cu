@@ -1836,7 +1836,7 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
       c.n_pages <= 0 || c.max_seqs <= 0 || c.max_pages <= 0 || c.q_heads % c.kv_heads ||
       c.rot_dim < 0 || c.rot_dim > c.head_dim || c.rot_pairs < 0 || c.rot_pairs > 1 ||
       !(c.norm_eps >= 0.f) || !std::isfinite(c.norm_eps) ||
-      (c.rot_dim > 0 && (!(c.rot_base >= 1.f) || !std::isfinite(c.rot_base))) ||
+      (c.rot_dim > 0 && (!(c.rot_base >= 1.0) || !std::isfinite(c.rot_base))) ||
       (c.dtype != MOT_BF16 && c.dtype != MOT_FP32))
     return MOT_ERR_INVALID_ARG;
   if ((c.head_dim != 64 && c.head_dim != 128) || c.page < 16 || c.page > 128 || (c.page & (c.page - 1)) ||

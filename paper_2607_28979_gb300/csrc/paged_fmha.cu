@@ -199,176 +199,182 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
   // for the drain after a timeout: loads that have been issued, by ring place
   uint32_t k_issued = 0, k_par = 0, v_issued = 0, v_par = 0;
 
-  if (warp == 0) {
-    // ------------------------------------------------ TMA producer
-    uint32_t t = 0;   // tiles so far
-    bool ok = a.stall_test == 0 || blockIdx.x != 0;   // test hook: CTA 0 loads nothing
-    const int pages = F::kTK >> a.d.lp;                       // of a tile
-    const int x = lane / kHalves, half = lane % kHalves;      // this lane's page and half
-    while (ok && c.u < c.u_end) {
-      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
-      // this lane's table entry of a tile, read a tile ahead
-      auto entry = [&](int kt) -> int {
-        const int at = kt * F::kTK + (x << a.d.lp);
-        return lane < pages * kHalves && kt < p.kt + p.n && at < c.s.len
-                   ? a.table[int64_t(c.s.slot) * a.d.max_pages + (at >> a.d.lp)]
-                   : 0;
-      };
-      int next = entry(p.kt);
-      for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
-        const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0);
-        const bool mine = lane < pages * kHalves && k0 + (x << a.d.lp) < c.s.len;
-        int page = next;
-        next = entry(kt + 1);
-        if (mine && (page < 0 || page >= a.d.n_pages)) {   // held inside the pool
-          page = 0;
-          atomicOr(a.status, kStatusPageUse);
-        }
-        const int row = (page * H + c.hk) << a.d.lp;
-        const uint32_t bytes =
-            n_keys <= 0 ? 0u : static_cast<uint32_t>((n_keys + a.d.P - 1) >> a.d.lp) * a.d.P * 128 * kHalves;
-        auto fetch = [&](bool v, uint32_t st, uint32_t use) -> bool {
-          uint64_t* full = v ? &sh.v_full[st] : &sh.k_full[st];
-          if (!wait(v ? &sh.v_empty[st] : &sh.k_empty[st], (use & 1u) ^ 1u)) return false;
-          if (lane == 0) mbar_arrive_expect_tx(full, bytes);
-          __syncwarp();
-          if (mine)
-            tma_load_2d((v ? sV : sK) + st * F::kTile + half * F::kBlk + (x << a.d.lp) * 128, v ? &tmV : &tmK, full,
-                        half * 64, row);
-          uint32_t& issued = v ? v_issued : k_issued;
-          uint32_t& par = v ? v_par : k_par;
-          issued |= 1u << st;
-          par = (par & ~(1u << st)) | ((use & 1u) << st);
-          return true;
-        };
-        ok = fetch(false, t % F::kNK, t / F::kNK) && fetch(true, t % F::kNV, t / F::kNV);
-      }
-      paged_next<F::kBM, F::kTK>(a, c, p);
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------ MMA issuer: one thread
-    if (elect_one()) {
-      const uint32_t idS = idesc_bf16_f32(128, 128), idPV = idesc_bf16_f32_bmn(128, D);
-      uint32_t t = 0, n_q[2] = {0, 0}, n_s[2] = {0, 0};   // tiles; items and tiles of each stream
-      bool ok = true;
-      auto wait1 = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, wl); };
-      auto issue_s = [&](int i, uint32_t st) -> bool {   // S_i of the keys in place st
-        // P_i of the tile before lies where S_i goes: its product has to be done
-        if (n_s[i] && !wait1(&sh.pv_done[i], (n_s[i] - 1) & 1u)) return false;
-        tc_fence_after();
-#pragma unroll
-        for (int kb = 0; kb < kHalves; ++kb) {
-          const uint64_t ad = sdesc_k_sw128(smem_u32(sQ + i * F::kTile + kb * F::kBlk));
-          const uint64_t bd = sdesc_k_sw128(smem_u32(sK + st * F::kTile + kb * F::kBlk));
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            umma_bf16(tmem + i * 128, ad + 2 * k, bd + 2 * k, idS, (kb | k) != 0);
-        }
-        umma_commit(&sh.s_full[i]);
-        return true;
-      };
-      auto issue_pv = [&](int i, uint32_t st, int steps, bool first) -> bool {   // O_i += P_i V
-        const uint32_t tO = tmem + F::kO + i * D, tP = tmem + i * 128;
-        const uint64_t bd = sdesc_mn_sw128(smem_u32(sV + st * F::kTile), F::kBlk);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!wait1(&sh.p_half[i][h], n_s[i] & 1u)) return false;
-          tc_fence_after();
-#pragma unroll
-          for (int k = 4 * h; k < 4 * h + 4; ++k)
-            if (k < steps) umma_bf16_ts(tO, tP + 8 * k, bd + 128 * k, idPV, !(first && k == 0));
-        }
-        umma_commit(&sh.pv_done[i]);
-        ++n_s[i];
-        return true;
-      };
+  if (warp < 4) {
+    // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; at 168 the softmax spilled (1,196 -> 1,137 us for
+    // 4,096 tokens on 32,768 positions)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 0) {
+      // ------------------------------------------------ TMA producer
+      uint32_t t = 0;   // tiles so far
+      bool ok = a.stall_test == 0 || blockIdx.x != 0;   // test hook: CTA 0 loads nothing
+      const int pages = F::kTK >> a.d.lp;                       // of a tile
+      const int x = lane / kHalves, half = lane % kHalves;      // this lane's page and half
       while (ok && c.u < c.u_end) {
         const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
-        const int n_str = c.s.m * G - c.rt * F::kBM > 128 ? 2 : 1;
-        for (int i = 0; ok && i < n_str; ++i) {
-          ok = wait1(&sh.q_ready[i], n_q[i]++ & 1u);
-          if (ok && i == 0) ok = wait1(&sh.k_full[t % F::kNK], (t / F::kNK) & 1u);
-          ok = ok && issue_s(i, t % F::kNK);
+        // this lane's table entry of a tile, read a tile ahead
+        auto entry = [&](int kt) -> int {
+          const int at = kt * F::kTK + (x << a.d.lp);
+          return lane < pages * kHalves && kt < p.kt + p.n && at < c.s.len
+                     ? a.table[int64_t(c.s.slot) * a.d.max_pages + (at >> a.d.lp)]
+                     : 0;
+        };
+        int next = entry(p.kt);
+        for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
+          const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0);
+          const bool mine = lane < pages * kHalves && k0 + (x << a.d.lp) < c.s.len;
+          int page = next;
+          next = entry(kt + 1);
+          if (mine && (page < 0 || page >= a.d.n_pages)) {   // held inside the pool
+            page = 0;
+            atomicOr(a.status, kStatusPageUse);
+          }
+          const int row = (page * H + c.hk) << a.d.lp;
+          const uint32_t bytes =
+              n_keys <= 0 ? 0u : static_cast<uint32_t>((n_keys + a.d.P - 1) >> a.d.lp) * a.d.P * 128 * kHalves;
+          auto fetch = [&](bool v, uint32_t st, uint32_t use) -> bool {
+            uint64_t* full = v ? &sh.v_full[st] : &sh.k_full[st];
+            if (!wait(v ? &sh.v_empty[st] : &sh.k_empty[st], (use & 1u) ^ 1u)) return false;
+            if (lane == 0) mbar_arrive_expect_tx(full, bytes);
+            __syncwarp();
+            if (mine)
+              tma_load_2d((v ? sV : sK) + st * F::kTile + half * F::kBlk + (x << a.d.lp) * 128, v ? &tmV : &tmK, full,
+                          half * 64, row);
+            uint32_t& issued = v ? v_issued : k_issued;
+            uint32_t& par = v ? v_par : k_par;
+            issued |= 1u << st;
+            par = (par & ~(1u << st)) | ((use & 1u) << st);
+            return true;
+          };
+          ok = fetch(false, t % F::kNK, t / F::kNK) && fetch(true, t % F::kNV, t / F::kNV);
         }
-        if (ok) umma_commit(&sh.k_empty[t % F::kNK]);
-        for (int j = 0; ok && j < p.n; ++j, ++t) {
-          const uint32_t vs = t % F::kNV, ks = (t + 1) % F::kNK;
-          const int n_keys = min(F::kTK, c.s.len - (p.kt + j) * F::kTK);
-          const int steps = n_keys <= 0 ? 0 : (n_keys + 15) >> 4;
-          const bool more = j + 1 < p.n;
-          ok = wait1(&sh.v_ready[vs], (t / F::kNV) & 1u);
+        paged_next<F::kBM, F::kTK>(a, c, p);
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------ MMA issuer: one thread
+      if (elect_one()) {
+        const uint32_t idS = idesc_bf16_f32(128, 128), idPV = idesc_bf16_f32_bmn(128, D);
+        uint32_t t = 0, n_q[2] = {0, 0}, n_s[2] = {0, 0};   // tiles; items and tiles of each stream
+        bool ok = true;
+        auto wait1 = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, wl); };
+        auto issue_s = [&](int i, uint32_t st) -> bool {   // S_i of the keys in place st
+          // P_i of the tile before lies where S_i goes: its product has to be done
+          if (n_s[i] && !wait1(&sh.pv_done[i], (n_s[i] - 1) & 1u)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int kb = 0; kb < kHalves; ++kb) {
+            const uint64_t ad = sdesc_k_sw128(smem_u32(sQ + i * F::kTile + kb * F::kBlk));
+            const uint64_t bd = sdesc_k_sw128(smem_u32(sK + st * F::kTile + kb * F::kBlk));
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              umma_bf16(tmem + i * 128, ad + 2 * k, bd + 2 * k, idS, (kb | k) != 0);
+          }
+          umma_commit(&sh.s_full[i]);
+          return true;
+        };
+        auto issue_pv = [&](int i, uint32_t st, int steps, bool first) -> bool {   // O_i += P_i V
+          const uint32_t tO = tmem + F::kO + i * D, tP = tmem + i * 128;
+          const uint64_t bd = sdesc_mn_sw128(smem_u32(sV + st * F::kTile), F::kBlk);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (!wait1(&sh.p_half[i][h], n_s[i] & 1u)) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 4 * h; k < 4 * h + 4; ++k)
+              if (k < steps) umma_bf16_ts(tO, tP + 8 * k, bd + 128 * k, idPV, !(first && k == 0));
+          }
+          umma_commit(&sh.pv_done[i]);
+          ++n_s[i];
+          return true;
+        };
+        while (ok && c.u < c.u_end) {
+          const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+          const int n_str = c.s.m * G - c.rt * F::kBM > 128 ? 2 : 1;
           for (int i = 0; ok && i < n_str; ++i) {
-            ok = issue_pv(i, vs, steps, j == 0);
-            if (ok && i == n_str - 1) umma_commit(&sh.v_empty[vs]);
-            if (ok && more) {
-              if (i == 0) ok = wait1(&sh.k_full[ks], ((t + 1) / F::kNK) & 1u);
-              ok = ok && issue_s(i, ks);
-              if (ok && i == n_str - 1) umma_commit(&sh.k_empty[ks]);
+            ok = wait1(&sh.q_ready[i], n_q[i]++ & 1u);
+            if (ok && i == 0) ok = wait1(&sh.k_full[t % F::kNK], (t / F::kNK) & 1u);
+            ok = ok && issue_s(i, t % F::kNK);
+          }
+          if (ok) umma_commit(&sh.k_empty[t % F::kNK]);
+          for (int j = 0; ok && j < p.n; ++j, ++t) {
+            const uint32_t vs = t % F::kNV, ks = (t + 1) % F::kNK;
+            const int n_keys = min(F::kTK, c.s.len - (p.kt + j) * F::kTK);
+            const int steps = n_keys <= 0 ? 0 : (n_keys + 15) >> 4;
+            const bool more = j + 1 < p.n;
+            ok = wait1(&sh.v_ready[vs], (t / F::kNV) & 1u);
+            for (int i = 0; ok && i < n_str; ++i) {
+              ok = issue_pv(i, vs, steps, j == 0);
+              if (ok && i == n_str - 1) umma_commit(&sh.v_empty[vs]);
+              if (ok && more) {
+                if (i == 0) ok = wait1(&sh.k_full[ks], ((t + 1) / F::kNK) & 1u);
+                ok = ok && issue_s(i, ks);
+                if (ok && i == n_str - 1) umma_commit(&sh.k_empty[ks]);
+              }
             }
           }
+          paged_next<F::kBM, F::kTK>(a, c, p);
+        }
+      }
+      __syncwarp();
+    } else if (warp == 2) {
+      // ------------------------------------------------ values before the second product
+      uint32_t t = 0;
+      bool ok = true;
+      for (int piece = 0; ok && c.u < c.u_end; ++piece) {
+        const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+        const int masked = first_masked(c.s, G, c.rt * F::kBM);
+        uint32_t (*notes)[4] = sh.notes[piece & 3];
+        // the notes of four pieces ago are read: this piece's values were loaded behind products that
+        // the softmax warps started after them
+        bool cleared = false;
+        for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
+          const uint32_t st = t % F::kNV;
+          ok = wait(&sh.v_full[st], (t / F::kNV) & 1u);
+          if (!ok) break;
+          if (!cleared) {
+            cleared = true;
+            if (lane < 16) notes[lane >> 2][lane & 3] = 0;
+            __syncwarp();
+          }
+          if (kt >= masked) {
+            const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0), rows = n_keys <= 0 ? 0 : (n_keys + 15) & ~15;
+            uint8_t* tile = sV + st * F::kTile;
+            // lane: 16 bytes of a row, 4 rows at a time
+            const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+            for (int b = 0; b < kHalves; ++b)
+#pragma unroll 4
+              for (int r = lane >> 3; r < rows; r += 4) {
+                const uint32_t at = smem_u32(tile + b * F::kBlk + r * 128 + (lane & 7) * 16);
+                if (r >= n_keys) {
+                  st_shared_v4(at, 0u, 0u, 0u, 0u);
+                  continue;
+                }
+                uint4 v = ld_shared_v4(at);
+                __nv_bfloat162 x = zero;   // NaN where a value is not finite: 0 times it
+                x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.x), zero, x);
+                x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.y), zero, x);
+                x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.z), zero, x);
+                x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.w), zero, x);
+                const uint32_t bits = *reinterpret_cast<uint32_t*>(&x);
+                if ((bits & 0x7FFF7FFFu) == 0) continue;
+                uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
+                  if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+                }
+                st_shared_v4(at, u[0], u[1], u[2], u[3]);
+                atomicOr(&notes[min(kt - masked, 3)][r >> 5], 1u << (r & 31));
+              }
+            fence_proxy_async_smem();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.v_ready[st]);
         }
         paged_next<F::kBM, F::kTK>(a, c, p);
       }
     }
-    __syncwarp();
-  } else if (warp == 2) {
-    // ------------------------------------------------ values before the second product
-    uint32_t t = 0;
-    bool ok = true;
-    for (int piece = 0; ok && c.u < c.u_end; ++piece) {
-      const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
-      const int masked = first_masked(c.s, G, c.rt * F::kBM);
-      uint32_t (*notes)[4] = sh.notes[piece & 3];
-      // the notes of four pieces ago are read: this piece's values were loaded behind products that
-      // the softmax warps started after them
-      bool cleared = false;
-      for (int kt = p.kt; ok && kt < p.kt + p.n; ++kt, ++t) {
-        const uint32_t st = t % F::kNV;
-        ok = wait(&sh.v_full[st], (t / F::kNV) & 1u);
-        if (!ok) break;
-        if (!cleared) {
-          cleared = true;
-          if (lane < 16) notes[lane >> 2][lane & 3] = 0;
-          __syncwarp();
-        }
-        if (kt >= masked) {
-          const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0), rows = n_keys <= 0 ? 0 : (n_keys + 15) & ~15;
-          uint8_t* tile = sV + st * F::kTile;
-          // lane: 16 bytes of a row, 4 rows at a time
-          const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
-          for (int b = 0; b < kHalves; ++b)
-#pragma unroll 4
-            for (int r = lane >> 3; r < rows; r += 4) {
-              const uint32_t at = smem_u32(tile + b * F::kBlk + r * 128 + (lane & 7) * 16);
-              if (r >= n_keys) {
-                st_shared_v4(at, 0u, 0u, 0u, 0u);
-                continue;
-              }
-              uint4 v = ld_shared_v4(at);
-              __nv_bfloat162 x = zero;   // NaN where a value is not finite: 0 times it
-              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.x), zero, x);
-              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.y), zero, x);
-              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.z), zero, x);
-              x = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&v.w), zero, x);
-              const uint32_t bits = *reinterpret_cast<uint32_t*>(&x);
-              if ((bits & 0x7FFF7FFFu) == 0) continue;
-              uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
-                if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
-              }
-              st_shared_v4(at, u[0], u[1], u[2], u[3]);
-              atomicOr(&notes[min(kt - masked, 3)][r >> 5], 1u << (r & 31));
-            }
-          fence_proxy_async_smem();
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.v_ready[st]);
-      }
-      paged_next<F::kBM, F::kTK>(a, c, p);
-    }
-  } else if (warp >= 4) {
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------ softmax: warps 4 + 4 i + q, stream i, lane quarter q
     constexpr float kTau = 8.f;
     const int i = (warp - 4) >> 2, quarter = warp & 3;
@@ -378,9 +384,9 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
     const float sl2 = rsqrtf(float(D)) * 1.4426950408889634f;   // log2(e) / sqrt(d)
     uint32_t t = 0;   // tiles of this stream
     bool ok = true;
-    const PagedCursor& c = share.c;
-    const PagedPiece& p = share.p;
     for (int piece = 0;; ++piece) {
+      const PagedCursor c = share.c;
+      const PagedPiece p = share.p;
       const int kt_end = p.kt + p.n;
       const int row = c.rt * F::kBM + i * 128 + r, n_rows = c.s.m * G;
       const bool active = n_rows - c.rt * F::kBM > i * 128;   // the stream has rows

@@ -71,8 +71,8 @@ class mot_paged_config(ctypes.Structure):
                 ("page", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("max_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("rot_dim", ctypes.c_int32), ("rot_pairs", ctypes.c_int32),
-                ("rot_base", ctypes.c_float), ("norm_eps", ctypes.c_float),
-                ("dtype", ctypes.c_int32)]
+                ("dtype", ctypes.c_int32), ("norm_eps", ctypes.c_float),
+                ("rot_base", ctypes.c_double)]
 
 
 class mot_paged_cache(ctypes.Structure):
@@ -299,8 +299,8 @@ def mot_replay_select(h: Handle, guide, seq_lens, batch: int, sel, stream=None) 
 def make_paged_config(n_layers, q_heads, kv_heads, head_dim, page, n_pages, max_seqs, max_pages,
                       rot_dim=0, rot_pairs=False, rot_base=1e4, norm_eps=1e-6, dtype="bf16"):
     return mot_paged_config(n_layers, q_heads, kv_heads, head_dim, page, n_pages, max_seqs,
-                            max_pages, rot_dim, int(bool(rot_pairs)), rot_base, norm_eps,
-                            MOT_BF16 if dtype in ("bf16", MOT_BF16) else MOT_FP32)
+                            max_pages, rot_dim, int(bool(rot_pairs)),
+                            MOT_BF16 if dtype in ("bf16", MOT_BF16) else MOT_FP32, norm_eps, rot_base)
 
 
 def paged_cache(k, v, table, lens, refs) -> mot_paged_cache:

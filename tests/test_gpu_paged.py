@@ -383,6 +383,41 @@ def test_attention_of_a_long_context(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new,n", [(1, 3000), (1, 9001), (20, 3000), (20, 20011), (70, 8200)])
+def test_attention_of_few_rows_in_many_pieces(dtype, new, n):
+    """Items that up to eight, up to 64 and more CTAs share: joins in one level and in two."""
+    c = _filled([n, 40], None, q_heads=4, kv_heads=2, d=64, page=128, dtype=dtype, seed=n)
+    q, out = _attend(c, [0, 1], [new, 1])
+    again = torch.zeros_like(out)
+    M.mot_paged_attention(c.h, 0, c.c, c.batch([0, 1], [new, 1]), q, again)
+    assert torch.equal(again[:new + 1], out[:new + 1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [33, 500])
+def test_attention_of_many_chunks(dtype, n):
+    """More entries than a warp has lanes, and than a CTA has threads, with chunks of several sizes."""
+    lens = [(i * 53) % 150 for i in range(n)]
+    new = [min(x, (i * 11) % 31) for i, x in enumerate(lens)]
+    c = _filled(lens, None, q_heads=4, kv_heads=2, d=64, dtype=dtype, seed=n)
+    seqs = np.random.default_rng(n).permutation(n).tolist()
+    _attend(c, seqs, [new[s] for s in seqs])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_max_chunk_is_only_a_hint(dtype):
+    """Entries with more rows than max_chunk says are computed all the same."""
+    c = _filled([300, 90, 64], None, q_heads=6, kv_heads=2, d=128, page=32, dtype=dtype)
+    q = c.normal(150 + 3 + 64, 6, 128)
+    for hint in (0, 1, 10 ** 6):
+        out = torch.full_like(q, 9.0)
+        b = M.paged_batch(i32([0, 1, 2]), i32([0, 150, 153, 217]), 3, 217, hint)
+        M.mot_paged_attention(c.h, 0, c.c, b, q, out)
+        assert c.status() == M.MOT_OK
+        P.check_attention(c, [0, 1, 2], [150, 3, 64], q, out)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_attention_of_a_long_chunk(dtype):
     """A chunk of 700 on 1,600 positions, checked at some rows; every layer of the pool is its own."""
     c = _filled([2300], None, layers=3, q_heads=4, kv_heads=2, d=64, page=64, dtype=dtype)
@@ -540,6 +575,24 @@ def test_offsets_beyond_32_bits(new):
     c.c = M.paged_cache(c.k, c.v, c.table, c.lens, c.refs)
     c.h = M.mot_create_paged(M.make_paged_config(1, 8, H, d, page, n_pages, 1, 8))
     _attend(c, [0], [new])
+    # the append, the copies and a compaction reach there too
+    x = c.normal(new, 8 + 2 * H, d)
+    q = torch.zeros((new, 8, d), dtype=torch.bfloat16, device="cuda")
+    M.mot_paged_append(c.h, 0, c.c, c.batch([0], [new]), x[:, :8], x[:, 8:8 + H], x[:, 8 + H:], q)
+    flat = [torch.zeros((1, 1, H, 700, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    M.mot_paged_load(c.h, c.c, i32([0]), 1, *flat)
+    assert c.status() == M.MOT_OK
+    for f, stored, k in zip(flat, c.rows(0), (x[:, 8:8 + H], x[:, 8 + H:])):
+        assert torch.equal(f[0, 0, :, 700 - new:].transpose(0, 1), k)
+        assert torch.equal(f[0, 0].double(), stored)
+    M.mot_paged_store(c.h, c.c, i32([0]), 1, flat[1], flat[0])
+    c.refs[c.t[0]] = 1
+    M.mot_paged_compact(c.h, c.c)
+    assert c.status() == M.MOT_OK
+    c.t[0] = c.table[0, :6].tolist()
+    assert sorted(c.t[0]) == list(range(6))
+    for f, stored in zip((flat[1], flat[0]), c.rows(0)):
+        assert torch.equal(f[0, 0].double(), stored)
 
 
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right():
@@ -593,18 +646,88 @@ def test_a_step_is_captured_and_replayed_on_another_stream():
     assert c.status() == M.MOT_OK
 
 
+def test_forks_compaction_and_chunks_are_captured_and_replayed():
+    """A turn of an agents' loop in a graph: branches end, the pool is compacted, new branches start and
+    take a prompt. Every replay is another turn."""
+    c = P.Cache(layers=2, q_heads=6, kv_heads=2, d=64, page=16, n_pages=40, max_pages=12, rot_dim=64)
+    c.reserve([0, 1], [70, 33])
+    c.fork([0, 1, 0], [2, 3, 4])
+    rows, new = 60, [40, 15, 5]
+    x = c.normal(rows, 10, 64)
+    q, out = (torch.zeros((rows, 6, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dst, src, b = i32([2, 3, 4]), i32([0, 1, 0]), c.batch([2, 3, 4], new)
+
+    def turn():
+        M.mot_paged_free(c.h, c.c, dst, 3)
+        M.mot_paged_compact(c.h, c.c)
+        M.mot_paged_fork(c.h, c.c, src, dst, 3)
+        M.mot_paged_reserve(c.h, c.c, b)
+        M.mot_paged_append(c.h, 1, c.c, b, x[:, :6], x[:, 6:8], x[:, 8:], q)
+        M.mot_paged_attention(c.h, 1, c.c, b, q, out)
+
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        turn()
+    for _ in range(4):
+        x.copy_(c.normal(rows, 10, 64))
+        graph.replay()
+        torch.cuda.synchronize()
+        for s in (2, 3, 4):   # the same on the lists
+            for p in c.t[s]:
+                c.r[p] -= 1
+            c.t[s], c.n[s] = [], 0
+        used = sum(r > 0 for r in c.r)
+        to = dict(zip([p for p in range(used, c.n_pages) if c.r[p]], [p for p in range(used) if not c.r[p]]))
+        for a, e in to.items():
+            c.r[e], c.r[a] = c.r[a], 0
+        c.t = [[to.get(p, p) for p in row] for row in c.t]
+        for s, e in ((0, 2), (1, 3), (0, 4)):
+            full, part = divmod(c.n[s], 16)
+            c.t[e], c.n[e] = c.t[s][:full], c.n[s]
+            for p in c.t[e]:
+                c.r[p] += 1
+            if part:
+                c.t[e] = c.t[e] + c.take(1)
+        for s, m in zip((2, 3, 4), new):
+            c.t[s] = c.t[s] + c.take(c.pages(c.n[s] + m) - c.pages(c.n[s]))
+            c.n[s] += m
+        c.check()
+        P.check_attention(c, [2, 3, 4], new, q, out, 1)
+    assert c.status() == M.MOT_OK
+
+
+def test_two_handles_at_once():
+    """Two handles have workspaces of their own: their calls may run side by side on two streams."""
+    caches = [_filled([6000, 500], None, q_heads=4, kv_heads=2, d=64, page=64, seed=s) for s in (1, 2)]
+    streams = [torch.cuda.Stream() for _ in caches]
+    qs = [c.normal(33, 4, 64) for c in caches]
+    outs = [torch.zeros_like(q) for q in qs]
+    batches = [(c.batch([0, 1], [32, 1]), c.batch([0, 1], [1, 1])) for c in caches]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for c, st, q, o, (chunk, step) in zip(caches, streams, qs, outs, batches):
+            M.mot_paged_attention(c.h, 0, c.c, chunk, q, o, stream=st)
+            M.mot_paged_attention(c.h, 0, c.c, step, q[31:], o[31:], stream=st)
+            M.mot_paged_attention(c.h, 0, c.c, chunk, q, o, stream=st)
+    torch.cuda.synchronize()
+    for c, q, o in zip(caches, qs, outs):
+        assert c.status() == M.MOT_OK
+        P.check_attention(c, [0, 1], [32, 1], q, o)
+
+
 def test_calls_follow_the_given_stream():
     c = _filled([500], None, q_heads=4, kv_heads=2, d=64)
     q = c.normal(1, 4, 64)
     out = torch.zeros_like(q)
-    side = torch.cuda.Stream()
+    side, b = torch.cuda.Stream(), c.batch([0], [1])
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
         big = torch.randn((4096, 4096), device="cuda")
         for _ in range(20):
             big = big @ big / 4096
         q.mul_(2)   # behind the products: the call has to wait for it
-    M.mot_paged_attention(c.h, 0, c.c, c.batch([0], [1]), q, out, stream=side)
+    M.mot_paged_attention(c.h, 0, c.c, b, q, out, stream=side)
     assert M.mot_get_device_status(c.h, side) == M.MOT_OK
     P.check_attention(c, [0], [1], q, out)
 

@@ -1,6 +1,8 @@
 """The paged cache's entry points without a GPU: bad configs and NULL handles are refused before any
-CUDA call."""
+CUDA call; the kernels that start under their predecessor, read from the sources."""
 import ctypes
+import os
+import re
 
 import pytest
 
@@ -73,3 +75,14 @@ def test_null_handles_and_arguments():
     assert L.mot_paged_append(None, 0, c, b, 64, 64, 64, 64, 64, 64, None, None, 64, None) == bad
     assert L.mot_paged_attention(None, 0, c, b, 64, 64, None) == bad
     assert M.mot_status_string(M.MOT_ERR_PAGES) == "MOT_ERR_PAGES"
+
+
+def test_overlapped_kernels_wait_before_they_read_or_leave():
+    """The second kernels of a fork and of a compaction start while the plan before them runs: each
+    waits for it first of all."""
+    src = open(os.path.join(os.path.dirname(mot_build.__file__), "csrc", "paged.cu")).read()
+    names = re.findall(r"launch_kernel\(overlap, (\w+)", src)
+    assert sorted(names) == ["paged_compact_kernel", "paged_fork_kernel"]
+    for name in names:
+        body = src[src.index("{", src.index(name + "(")):]
+        assert body[1:].lstrip().startswith("pdl_enter();"), name
