@@ -72,7 +72,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity,
   }
 }
 
-// mbar_wait for the attention kernels' TMA producers and the softmax warps' lane-0
+// mbar_wait for the replay attention kernel's TMA producer and its softmax warps' lane-0
 // waits: each poll may suspend the thread (up to 0.5 us, ended early when the
 // phase completes), so waiting warps leave their sub-partition's issue slots to
 // the softmax warps. The MMA issuer keeps the polling mbar_wait.
