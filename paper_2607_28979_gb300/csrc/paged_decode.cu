@@ -272,6 +272,47 @@ __global__ void __launch_bounds__(kDecThreads, kResident<D, NT>) paged_decode_ke
       }
       if (more) load_v(kt + 1, row);
     }
+    // An infinite value that is seen: its weight's second part may be 0 or negative, which makes NaN of
+    // the sum. Where a sum is not finite the piece's values are gone through again, and those that are
+    // not finite and seen are the sum (an infinity, or NaN). Looked for once a piece, not in the loop.
+    bool spoilt = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int h = 0; h < kH; ++h)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) spoilt |= !isfinite(o[n][h][e >> 2][e & 3]);
+    if (__any_sync(0xffffffffu, spoilt)) {
+#pragma unroll
+      for (int h = 0; h < kH; ++h)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float add[NT][2];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) add[n][0] = add[n][1] = 0.f;
+#pragma unroll 1
+          for (int kt = kt_begin; kt < kt_end; ++kt) {
+            const int k0 = kt * TK + 16 * warp;
+            if (k0 >= len) break;
+            const int64_t at = paged_row(a.d, paged_page(a.d, a.table, a.status, slot, k0), hk, k0);
+#pragma unroll 1
+            for (int j = 0; j < 16 && k0 + j < len; ++j) {
+              const float x = __uint_as_float(uint32_t(vp[(at + j) * D + 64 * h + 8 * g + e]) << 16);
+              if (isfinite(x)) continue;
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+                  if (k0 + j <= pos[n][b]) add[n][b] += x;
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+              if (add[n][b] != 0.f) o[n][h][e >> 1][b + 2 * (e & 1)] = add[n][b];   // NaN too
+        }
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll

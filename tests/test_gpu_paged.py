@@ -501,6 +501,32 @@ def test_an_infinite_value_that_is_seen(dtype, new):
     assert bool(inf[:, 2:, 7].all()) and int(inf.sum()) == 2 * new and not bool(torch.isnan(out).any())
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 2, 3])
+def test_infinite_values_that_are_seen_by_few_rows(d, new):
+    """The same at many positions: whatever a weight's two bf16 parts are (the second one may be 0 or
+    negative), they give the infinity and no NaN; a NaN and both infinities in a column give NaN."""
+    c = _filled([600], None, q_heads=8, kv_heads=2, d=d, page=32)
+    q = c.normal(new, 8, d)
+    b, clean = c.batch([0], [new]), c.v.clone()
+    out = torch.zeros_like(q)
+    for j in range(0, 600 - new, 13):
+        sign = -1 if j % 2 else 1
+        c.v.copy_(clean)
+        page, at = c.t[0][j // 32], j % 32
+        c.v[0, page, 0, at, 9] = sign * math.inf
+        c.v[0, page, 1, at, 3] = math.nan
+        c.v[0, page, 1, at, 40] = math.inf
+        c.v[0, c.t[0][0], 1, 31, 40] = -math.inf
+        M.mot_paged_attention(c.h, 0, c.c, b, q, out)
+        odd = torch.zeros_like(out, dtype=torch.bool)
+        odd[:, :4, 9] = True
+        odd[:, 4:, 3] = odd[:, 4:, 40] = True
+        assert bool((out[:, :4, 9] == sign * math.inf).all()), j
+        assert bool(torch.isnan(out[:, 4:, 3]).all()) and bool(torch.isnan(out[:, 4:, 40]).all()), j
+        assert bool(torch.isfinite(out[~odd]).all()), j
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("gain", [0.05, 2.0, -2.0])
 @pytest.mark.parametrize("new", [1, 50])
