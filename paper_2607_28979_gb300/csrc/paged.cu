@@ -64,8 +64,10 @@ __global__ void __launch_bounds__(kPlanThreads)
     const int i = i0 + tid;
     int need = 0;
     if (i < b.n) {
-      const int s = b.seqs[i], m = b.starts[i + 1] - b.starts[i];
-      if (!mark_slot(marks, s, d.max_seqs) || m < 0) {
+      // ascending starts within the rows: the new positions of all entries together are b.rows at most,
+      // so that no sum of pages here leaves 32 bits
+      const int s = b.seqs[i], from = b.starts[i], to = b.starts[i + 1], m = to - from;
+      if (!mark_slot(marks, s, d.max_seqs) || from < 0 || to < from || to > b.rows) {
         bad = true;
       } else {
         const int len = c.lens[s];
@@ -78,7 +80,7 @@ __global__ void __launch_bounds__(kPlanThreads)
     int t;
     const int at = block_scan(need, sh, t);
     if (i < b.n && total + at <= d.n_pages) w.first[i] = int(total) + at;
-    total += t;   // a piece adds 1024 x 2^26 at most
+    total += t;
     if (total > d.n_pages) bad = true;
   }
   if (__syncthreads_or(bad) || !take_lowest(d, c.refs, int(total), w.take, sh)) {

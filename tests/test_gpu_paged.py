@@ -129,6 +129,19 @@ def test_refused_changes_change_nothing_until_the_status_is_read():
     assert c.status() == M.MOT_ERR_PAGES   # that one is a source and a destination: refused as well
 
 
+def test_reserve_refuses_starts_outside_its_rows():
+    """starts below 0 or beyond the batch's rows, in the first entry, a middle one and the last."""
+    c = P.Cache(n_pages=20, max_seqs=5, max_pages=4, page=16)
+    c.reserve([0], [5])
+    for starts, rows in (([0, 4, 9], 8), ([-1, 2, 3], 8), ([0, 9, 9], 8), ([9, 9, 12], 8), ([3, 5, 4], 8)):
+        M.mot_paged_reserve(c.h, c.c, M.paged_batch(i32([1, 2]), i32(starts), 2, rows))
+        c.check(f"{starts}")
+        assert c.status() == M.MOT_ERR_PAGES, starts
+    c.reserve([1, 2], [4, 4])
+    c.check()
+    assert c.status() == M.MOT_OK
+
+
 def test_store_and_append_do_nothing_behind_a_refused_change():
     c = P.Cache(n_pages=4, max_pages=4, page=16)
     c.reserve([0], [20])
