@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kCopyThreads)
   pdl_enter();   // behind the plan
   const int n = w.count[0], used = w.count[1];
   if (n == 0) return;
-  const int vecs = d.H * d.P * d.d * elem_bytes(d) / 16;   // of a page in one layer
+  const int vecs = d.H * d.P * (d.d * elem_bytes(d) / 16);   // of a page in one layer; its bytes may pass 2^31
   constexpr int kPiece = 4 * kCopyThreads;
   const int pieces = (vecs + kPiece - 1) / kPiece;
   const int64_t items = int64_t(n) * d.L * 2 * pieces;
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kCopyThreads)
 __global__ void __launch_bounds__(kCopyThreads)
     paged_copy_kernel(const PagedDims d, const PagedCache c, const PagedCopy p, const PagedWork w) {
   if (p.store && refused(w.status)) return;
-  const int per_seq = (p.S + d.P - 1) >> d.lp;
+  const int per_seq = ((p.S - 1) >> d.lp) + 1;
   const int64_t items = int64_t(per_seq) * p.n * p.n_layers;
   const int es = elem_bytes(d);
   const int dv = d.d * es / 16;                       // vectors of a row: a power of two
@@ -650,7 +650,7 @@ cudaError_t launch_paged_compact(const PagedDims& d, const PagedCache& c, const 
 }
 cudaError_t launch_paged_copy(const PagedDims& d, const PagedCache& c, const PagedCopy& p, const PagedWork& w,
                               int num_sms, cudaStream_t st) {
-  const int64_t items = int64_t((p.S + d.P - 1) / d.P) * p.n * p.n_layers;
+  const int64_t items = int64_t((p.S - 1) / d.P + 1) * p.n * p.n_layers;
   return launch_kernel(false, paged_copy_kernel, grid_of(items, num_sms, 8), kCopyThreads, 0, st, d, c, p, w);
 }
 cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const PagedAppend& p,

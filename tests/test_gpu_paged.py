@@ -142,6 +142,21 @@ def test_reserve_refuses_starts_outside_its_rows():
     assert c.status() == M.MOT_OK
 
 
+def test_compaction_of_very_wide_pages():
+    """A page of one layer has 2^31 bytes."""
+    H = 32768
+    c = P.Cache(q_heads=H, kv_heads=H, d=128, page=128, n_pages=2, max_seqs=2, max_pages=1, dtype="fp32")
+    c.reserve([0, 1], [128, 100])
+    c.free([0])
+    before = [x[0, 1].clone() for x in (c.k, c.v)]
+    c.compact()
+    c.check()
+    assert c.t[1] == [0]
+    for x, y in zip((c.k, c.v), before):
+        assert torch.equal(x[0, 0], y)
+    assert c.status() == M.MOT_OK
+
+
 def test_store_and_append_do_nothing_behind_a_refused_change():
     c = P.Cache(n_pages=4, max_pages=4, page=16)
     c.reserve([0], [20])
