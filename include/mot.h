@@ -579,7 +579,9 @@ mot_status mot_paged_load(mot_handle h, const mot_paged_cache* cache, int32_t fi
  *     (a cos t - b sin t, b cos t + a sin t), t as in mot_paged_config,
  * in fp32 with angles exact for any position, and rounded once. q goes to
  * q_out [rows][q_heads][head_dim] (which may be q itself where its rows are
- * contiguous), k and v into the pages. Rows of no entry give nothing.
+ * contiguous), k and v into the pages, which the sequence has to hold alone (as
+ * it does those that mot_paged_reserve took and a fork's copied one). Rows of
+ * no entry, and rows before position 0, give nothing.
  */
 mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cache,
                             const mot_paged_batch* batch, const void* q, int64_t q_stride,
@@ -594,7 +596,8 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
  * q, out: [rows][q_heads][head_dim], 16-byte aligned. A row before position 0
  * (a sequence shorter than its rows) sees nothing and is written as zeros;
  * rows of no entry are not written. Positions behind p add nothing, whatever
- * they hold, NaN and infinities included. One row per entry is a decoding
+ * they hold, NaN and infinities included; an infinite value that is seen gives
+ * an infinite result, and a row whose scores are all -inf zeros. One row per entry is a decoding
  * step; any mixture with longer chunks is one call.
  */
 mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cache* cache,

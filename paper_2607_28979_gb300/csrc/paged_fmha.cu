@@ -27,8 +27,8 @@
 //                       against the kernel of its day (4,096 tokens on 32,768 positions): two buffers of
 //                       64 keys per stream instead of one of 128 (1,402 us for 1,214: twice the steps),
 //                       two softmax threads per row (1,243 for 1,219), an issuing warp per stream (1,620
-//                       for 1,452), P in three quarters and one or as a whole (1,163 and 1,200 for 1,141). The waits poll without a sleep: a sleeping thread wakes up to a
-//                       microsecond late.
+//                       for 1,452), P in three quarters and one or as a whole (1,163 and 1,200 for 1,141).
+//                       The waits poll without a sleep: a sleeping thread wakes up to a microsecond late.
 //                       Every wait is bounded; on a timeout the roles unwind, copies and MMAs in flight
 //                       are drained, TMEM is freed and kStatusTimeout is raised.
 #include "paged_common.cuh"

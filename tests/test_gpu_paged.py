@@ -556,6 +556,21 @@ def test_infinite_values_that_are_seen_by_few_rows(d, new):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new", [1, 40])
+def test_rows_whose_scores_are_all_minus_infinity_are_zeros(dtype, new):
+    c = _filled([90], None, q_heads=4, kv_heads=2, d=64, dtype=dtype)
+    c.k[0, c.t[0], 1] = -math.inf   # the second key/value head's keys, all positions
+    q = c.normal(new, 4, 64).abs() + 0.5
+    out = torch.full_like(q, math.nan)
+    M.mot_paged_attention(c.h, 0, c.c, c.batch([0], [new]), q, out)
+    assert not bool(out[:, 2:].any()) and bool(torch.isfinite(out).all())
+    K, V = c.rows(0)
+    ref, absv, slop = P.attention(q[:, :2], K[:1], V[:1])
+    half = P.HALF[dtype]
+    P.assert_close(out[:, :2], ref, half * (ref.abs() + (absv if dtype == "bf16" else 0)) + slop, "the other head")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("gain", [0.05, 2.0, -2.0])
 @pytest.mark.parametrize("new", [1, 50])
 def test_scores_that_rise_or_fall_along_the_context(dtype, gain, new):
