@@ -16,7 +16,7 @@
 //                         second product as two bf16 parts (2^-17): it has the tensor pipe to itself,
 //                         and the result is that of 32-bit weights. Per warp a running maximum and
 //                         sum; the four warps meet at the end of a piece. Measured, 28 heads on 4:
-//                         64 sequences of 16,384 positions 6.0 TB/s, of 100 to 16,384 5.1; two blocks
+//                         64 sequences of 16,384 positions 6.0 TB/s, of 100 to 16,384 5.2; two blocks
 //                         ahead instead of one: 73 us for 77 with two contexts
 //                         of 131,072 and 70,001, but 85 for 82 with the 64.
 #include "paged_common.cuh"
