@@ -106,10 +106,11 @@ __global__ void __launch_bounds__(kPlanThreads)
 __global__ void __launch_bounds__(kCopyThreads)
     paged_free_kernel(const PagedDims d, const PagedCache c, const int32_t* seqs, int n, const PagedWork w) {
   __shared__ uint32_t marks[kPagedMaxSeqs / 32];
-  if (refused(w.status)) return;
   const int tid = threadIdx.x, T = blockDim.x;
   for (int i = tid; i < (d.max_seqs + 31) / 32; i += T) marks[i] = 0;
-  __syncthreads();
+  // another CTA of this launch may be setting the bit: one decision for the whole CTA, which then either
+  // leaves (the batch is refused) or checks all of it
+  if (__syncthreads_or(refused(w.status))) return;
   bool bad = false;
   for (int i = tid; i < n; i += T) bad |= !mark_slot(marks, seqs[i], d.max_seqs);
   if (__syncthreads_or(bad)) {

@@ -1,0 +1,49 @@
+"""What no run shows reliably in the paged cache's kernels, read from the sources: decisions that a
+whole CTA has to take alike, and the order of its writes to shared memory."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_28979_gb300", "csrc")
+
+
+def _source(name):
+    return re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+
+
+def _body(src, name):
+    """The braces of the function that is defined as `name`(."""
+    for m in re.finditer(r"\b%s\(" % name, src):
+        i, depth = m.end(), 1
+        while depth:
+            depth += {"(": 1, ")": -1}.get(src[i], 0)
+            i += 1
+        rest = src[i:].lstrip()
+        if not rest.startswith("{"):
+            continue
+        at = src.index("{", i)
+        depth, i = 1, at + 1
+        while depth:
+            depth += {"{": 1, "}": -1}.get(src[i], 0)
+            i += 1
+        return src[at:i]
+    raise AssertionError(name)
+
+
+def _kernels(src):
+    return {m.group(1): _body(src, m.group(1)) for m in re.finditer(r"\b(paged_\w+_kernel)\(const PagedDims", src)}
+
+
+def test_a_refusal_that_another_cta_may_set_is_read_by_the_cta_as_one():
+    """A kernel of several CTAs that sets the refusal bit also meets it while it is being set: threads
+    that read it one by one would disagree, and those that stay would act on a batch that is not checked."""
+    src = _source("paged.cu")
+    kernels = _kernels(src)
+    sets = {name for name, body in kernels.items() if "kStatusPages)" in body}
+    assert {"paged_reserve_kernel", "paged_free_kernel", "paged_fork_plan_kernel"} <= sets
+    several = {name for name in sets if not re.search(r"launch_kernel\(\w+, %s, 1, " % name, src)}
+    assert several == {"paged_free_kernel"}
+    for name in several:
+        reads = re.findall(r"[^;{}]*\brefused\([^;]*;", kernels[name])
+        assert len(reads) == 1 and "if (__syncthreads_or(refused(w.status))) return;" in reads[0], (name, reads)
