@@ -213,7 +213,9 @@ __device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, i
   const bool by_warp = n <= 32;
   const int T = by_warp ? 32 : int(blockDim.x), me = threadIdx.x;
   if (threadIdx.x == 0) st.work = 0;
-  if (!by_warp) __syncthreads();
+  // before another thread sets it (shuffles order no memory)
+  if (by_warp) __syncwarp();
+  else __syncthreads();
   if (!by_warp || threadIdx.x < 32) {
     auto scan = [&](int64_t v, int64_t& t) -> int64_t {
       if (!by_warp) return block_scan(v, sh, t);

@@ -47,3 +47,13 @@ def test_a_refusal_that_another_cta_may_set_is_read_by_the_cta_as_one():
     for name in several:
         reads = re.findall(r"[^;{}]*\brefused\([^;]*;", kernels[name])
         assert len(reads) == 1 and "if (__syncthreads_or(refused(w.status))) return;" in reads[0], (name, reads)
+
+
+def test_a_share_is_cleared_before_another_thread_may_set_it():
+    """Thread 0 clears st.work, the thread of the entry that the share lies in sets it: in both ways of
+    dealing the work (by one warp, by the CTA) a barrier that orders memory stands between."""
+    body = _body(_source("paged_common.cuh"), "paged_begin")
+    cleared, found = body.index("st.work = 0;"), body.index("st.work = 1;")
+    between = body[cleared:found]
+    dealt = between[:between.index("shfl")]   # before anything that the warp does together
+    assert "by_warp" in dealt and "__syncwarp();" in dealt and "__syncthreads();" in dealt
