@@ -479,7 +479,8 @@ mot_status mot_replay_select(mot_handle h, const void* guide, const int32_t* seq
  *     free, compact, store, append) until the status has been read;
  *   - lengths, starts, slots and table entries out of their ranges are held
  *     inside them by the calls that read them: nothing outside the buffers is
- *     touched, and the results of the entries concerned mean nothing.
+ *     touched, no page is written or counted through such an entry (a fork takes
+ *     it over as it is), and the results of the entries concerned mean nothing.
  * Errors: MOT_ERR_INVALID_ARG (NULL or misaligned pointers, sizes out of
  * range, overlapping buffers, a handle of another kind), MOT_ERR_CUDA.
  *

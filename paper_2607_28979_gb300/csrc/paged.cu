@@ -135,7 +135,8 @@ __global__ void __launch_bounds__(kCopyThreads)
   }
 }
 
-// Checks a fork and takes the pages of its partly filled last pages; moves[i]: what is copied.
+// Checks a fork and takes the pages of its partly filled last pages; moves[i]: what is copied (from < 0:
+// nothing).
 __global__ void __launch_bounds__(kPlanThreads)
     paged_fork_plan_kernel(const PagedDims d, const PagedCache c, const int32_t* src, const int32_t* dst, int n,
                            const PagedWork w) {
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kPlanThreads)
     if (f >= 0) {
       mv.y = w.take[f];
       c.refs[mv.y] = 1;
-      mv.x = paged_page(d, c.table, w.status, src[i], c.lens[src[i]]);
+      mv.x = paged_entry(d, c.table, w.status, src[i], c.lens[src[i]]);
     }
     w.moves[i] = mv;
   }
@@ -216,14 +217,17 @@ __global__ void __launch_bounds__(kCopyThreads)
   const int pages = pages_of(d, len), full = len >> d.lp, part = len & (d.P - 1);
   for (int j = blockIdx.x * kCopyThreads + tid; j < pages; j += gridDim.x * kCopyThreads) {
     int p = mv.y;
-    if (j < full) {
-      p = paged_page(d, c.table, w.status, a, j << d.lp);
-      atomicAdd(&c.refs[p], 1);
+    if (j < full) {   // an entry out of range is taken over as it is
+      p = c.table[int64_t(a) * d.max_pages + j];
+      if (p >= 0 && p < d.n_pages)
+        atomicAdd(&c.refs[p], 1);
+      else
+        atomicOr(w.status, kStatusPageUse);
     }
     c.table[int64_t(b) * d.max_pages + j] = p;
   }
   if (blockIdx.x == 0 && tid == 0) c.lens[b] = len;
-  if (!part) return;
+  if (!part || mv.x < 0) return;
   const int es = elem_bytes(d), run = d.P * d.d * es / 16, n_vec = part * d.d * es / 16;
   for (int x = blockIdx.x; x < 2 * d.L * d.H; x += gridDim.x) {
     uint4* pool = static_cast<uint4*>(x & 1 ? c.v : c.k);
@@ -333,7 +337,8 @@ __global__ void __launch_bounds__(kCopyThreads)
     if (j == 0 && threadIdx.x == 0 && (len < 0 || len > cap)) atomicOr(w.status, kStatusPageUse);
     const int rows = min(min(len, cap) - (j << d.lp), d.P);
     if (rows <= 0) continue;
-    const int page = paged_page(d, c.table, w.status, s, j << d.lp);
+    const int page = paged_entry(d, c.table, w.status, s, j << d.lp);
+    if (page < 0) continue;   // nothing is copied: whatever page it fell on would be another sequence's
     const int64_t pool = ((int64_t(p.first + l) * d.n_pages + page) * d.H << d.lp) * dv;
     const int64_t flat = ((int64_t(l) * p.B + i) * d.H * p.S + (j << d.lp)) * dv;
     const int n_vec = 2 * d.H << lrun;
@@ -500,11 +505,7 @@ __global__ void __launch_bounds__(kAppendThreads, 6)
       continue;
     }
     if (fresh || (pos & (d.P - 1)) == 0) {
-      page = c.table[int64_t(slot) * d.max_pages + (pos >> d.lp)];
-      if (page < 0 || page >= d.n_pages) {
-        page = -1;
-        if (lane == 0) atomicOr(w.status, kStatusPageUse);
-      }
+      page = paged_entry(d, c.table, w.status, slot, pos);
     }
     uint64_t tc[2] = {}, ts[2] = {};   // cos and sin of the lane's four angles, in pairs
     if (ROT != kRotNone) {

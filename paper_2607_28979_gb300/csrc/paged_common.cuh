@@ -459,13 +459,18 @@ __device__ __forceinline__ void paged_finish(const PagedAttnArgs& a, const Paged
 __device__ __forceinline__ int64_t paged_row(const PagedDims& d, int page, int hk, int pos) {
   return (int64_t(page) * d.H + hk) * d.P + (pos & (d.P - 1));
 }
-// A table entry, held inside the pool.
-__device__ __forceinline__ int paged_page(const PagedDims& d, const int32_t* table, int32_t* status,
-                                          int slot, int pos) {
+// A table entry; -1, and the status says so, where it is outside the pool.
+__device__ __forceinline__ int paged_entry(const PagedDims& d, const int32_t* table, int32_t* status, int slot,
+                                           int pos) {
   const int p = table[int64_t(slot) * d.max_pages + (pos >> d.lp)];
   if (p >= 0 && p < d.n_pages) return p;
   atomicOr(status, kStatusPageUse);
-  return 0;
+  return -1;
+}
+// The same held inside the pool, for what only reads.
+__device__ __forceinline__ int paged_page(const PagedDims& d, const int32_t* table, int32_t* status,
+                                          int slot, int pos) {
+  return max(paged_entry(d, table, status, slot, pos), 0);
 }
 
 }  // namespace

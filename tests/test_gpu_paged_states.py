@@ -32,3 +32,51 @@ def test_a_refused_free_of_many_slots_changes_nothing(wrong):
     c.free(list(range(0, n, 3)))
     c.check()
     assert c.status() == M.MOT_OK
+
+
+def _torn(dtype="bf16"):
+    """Slot 0 holds pages 0 and 1, slot 1 pages 2 .. 5 with its entries 1 and 3 (the last, partly filled)
+    out of range."""
+    c = P.Cache(layers=2, kv_heads=2, q_heads=4, page=16, n_pages=12, max_seqs=4, max_pages=5, dtype=dtype)
+    c.reserve([0, 1], [30, 55])
+    c.check()
+    c.t[1][1], c.t[1][3] = -1, c.n_pages
+    c.table[1, 1], c.table[1, 3] = -1, c.n_pages
+    return c
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_store_through_a_bad_table_entry_writes_no_page(dtype):
+    c = _torn(dtype)
+    want = [x.clone() for x in (c.k, c.v)]
+    flat = [c.normal(c.L, 1, c.H, 64, c.d) for _ in range(2)]
+    M.mot_paged_store(c.h, c.c, i32([1]), 1, *flat)
+    assert c.status() == M.MOT_ERR_PAGES
+    for x, y, f in zip(want, (c.k, c.v), flat):
+        for j in (0, 2):   # the entries in range
+            x[:, c.t[1][j]] = f[:, 0, :, 16 * j:16 * j + 16]
+        assert torch.equal(x, y)
+    # what a load finds there stays as it was
+    out = [torch.full_like(f, 7.0) for f in flat]
+    M.mot_paged_load(c.h, c.c, i32([1]), 1, *out)
+    assert c.status() == M.MOT_ERR_PAGES
+    for o, f in zip(out, flat):
+        for j in (0, 2):
+            assert torch.equal(o[:, 0, :, 16 * j:16 * j + 16], f[:, 0, :, 16 * j:16 * j + 16])
+        assert bool((o[:, 0, :, 16:32] == 7).all()) and bool((o[:, 0, :, 48:] == 7).all())
+
+
+def test_a_fork_of_a_bad_table_entry_counts_and_copies_no_page():
+    c = _torn()
+    want = [x.clone() for x in (c.k, c.v)]
+    M.mot_paged_fork(c.h, c.c, i32([1, 0]), i32([2, 3]), 2)
+    assert c.status() == M.MOT_ERR_PAGES
+    last = [c.take(1)[0] for _ in range(2)]
+    c.t[2], c.n[2] = [c.t[1][0], -1, c.t[1][2], last[0]], 55
+    c.t[3], c.n[3] = [c.t[0][0], last[1]], 30
+    for p in (c.t[1][0], c.t[1][2], c.t[0][0]):
+        c.r[p] += 1
+    c.check()
+    for x, y in zip(want, (c.k, c.v)):
+        x[:, last[1], :, :14] = x[:, c.t[0][1], :, :14]
+        assert torch.equal(x, y)
