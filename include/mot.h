@@ -137,7 +137,8 @@ mot_status mot_translate_host(mot_handle h, const void* src_k, const void* src_v
 /*
  * Synchronise `stream`, then report and clear the sticky device status word:
  * MOT_ERR_SEQ_LEN, MOT_ERR_TIMEOUT, MOT_ERR_PAGES, or MOT_OK. MOT_ERR_CUDA if
- * the stream reports an error.
+ * the stream reports an error. MOT_ERR_PAGES comes last: where another is
+ * reported first, the next call reports it.
  */
 mot_status mot_get_device_status(mot_handle h, mot_stream_t stream);
 
@@ -481,6 +482,7 @@ mot_status mot_replay_select(mot_handle h, const void* guide, const int32_t* seq
  *     inside them by the calls that read them: nothing outside the buffers is
  *     touched, no page is written or counted through such an entry (a fork takes
  *     it over as it is), and the results of the entries concerned mean nothing.
+ * mot_paged_cause tells the two apart.
  * Errors: MOT_ERR_INVALID_ARG (NULL or misaligned pointers, sizes out of
  * range, overlapping buffers, a handle of another kind), MOT_ERR_CUDA.
  *
@@ -520,6 +522,15 @@ typedef struct {
 } mot_paged_batch;
 
 mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out);
+
+/*
+ * What the last mot_get_device_status of a paged handle found, both or either
+ * where it returned MOT_ERR_PAGES, 0 where it did not: a change was refused,
+ * and those behind it did nothing; something out of range was held inside, and
+ * every call was carried out.
+ */
+enum { MOT_PAGES_REFUSED = 1, MOT_PAGES_HELD = 2 };
+mot_status mot_paged_cause(mot_handle h, int32_t* cause);
 
 /*
  * Room for new positions: entry i's sequence becomes m_i longer, and the pages

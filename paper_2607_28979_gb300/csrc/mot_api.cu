@@ -177,6 +177,7 @@ struct mot_ctx {
   uint64_t* pfreq = nullptr;   // [rot_dim / 2] turns per position, in units of 2^-64
   float* ppart = nullptr;      // partial results of the attention's split items
   int32_t* pcount = nullptr;   // its arrival counters, zero between calls
+  int32_t pages_cause = 0;     // what the last read of the status word found
   // Top-K routing (tensor-core path, 0 < top_k < E): token buckets per expert
   bool sparse_ok = false;   // the shapes support it
   int routing = 0;          // 0 dense compute with a zeroed gate, 1 token buckets
@@ -1366,10 +1367,16 @@ mot_status mot_get_device_status(mot_handle h, mot_stream_t stream) {
   MOT_CUDA_TRY(cudaStreamSynchronize(st));
   int32_t v = 0;
   MOT_CUDA_TRY(cudaMemcpy(&v, h->status, 4, cudaMemcpyDeviceToHost));
-  MOT_CUDA_TRY(cudaMemset(h->status, 0, 4));
+  // One cause is reported. What was found of a paged cache stays in the word until it is the one: a refused
+  // change goes on holding back the changes behind it.
+  const int32_t pages = v & (kStatusPages | kStatusPageUse);
+  const bool other = (v & (kStatusTimeout | kStatusSeqLen)) != 0;
+  const int32_t rest = other ? pages : 0;
+  MOT_CUDA_TRY(cudaMemcpy(h->status, &rest, 4, cudaMemcpyHostToDevice));
+  h->pages_cause = other ? 0 : (pages & kStatusPages ? MOT_PAGES_REFUSED : 0) | (pages & kStatusPageUse ? MOT_PAGES_HELD : 0);
   if (v & kStatusTimeout) return MOT_ERR_TIMEOUT;
   if (v & kStatusSeqLen) return MOT_ERR_SEQ_LEN;
-  if (v & (kStatusPages | kStatusPageUse)) return MOT_ERR_PAGES;
+  if (pages) return MOT_ERR_PAGES;
   return MOT_OK;
 }
 
@@ -1954,6 +1961,12 @@ mot_status paged_copy(mot_handle h, const mot_paged_cache* cache, const PagedCop
 }
 
 }  // namespace
+
+mot_status mot_paged_cause(mot_handle h, int32_t* cause) {
+  if (!h || h->kind != 4 || !cause) return MOT_ERR_INVALID_ARG;
+  *cause = h->pages_cause;
+  return MOT_OK;
+}
 
 mot_status mot_paged_reserve(mot_handle h, const mot_paged_cache* cache, const mot_paged_batch* batch,
                              mot_stream_t stream) {

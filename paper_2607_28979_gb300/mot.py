@@ -32,6 +32,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 MOT_OK, MOT_ERR_INVALID_ARG, MOT_ERR_UNSUPPORTED, MOT_ERR_NO_WEIGHTS, MOT_ERR_WEIGHTS_SIZE, \
     MOT_ERR_OOM, MOT_ERR_CUDA, MOT_ERR_SEQ_LEN, MOT_ERR_TIMEOUT, MOT_ERR_PAGES = range(10)
 MOT_BF16, MOT_FP32 = 0, 1
+MOT_PAGES_REFUSED, MOT_PAGES_HELD = 1, 2
 
 
 class mot_config(ctypes.Structure):
@@ -129,6 +130,7 @@ _SIGS = {
     "mot_replay_attention": [_H, ctypes.c_int32, _P, _P, _P, _P, _P, ctypes.c_int32, _P, _P],
     "mot_replay_select": [_H, _P, _P, ctypes.c_int32, _P, _P],
     "mot_create_paged": [ctypes.POINTER(mot_paged_config), ctypes.POINTER(ctypes.c_void_p)],
+    "mot_paged_cause": [_H, ctypes.POINTER(ctypes.c_int32)],
     "mot_paged_reserve": [_H, _CACHE, _BATCH, _P],
     "mot_paged_fork": [_H, _CACHE, _P, _P, _I, _P],
     "mot_paged_free": [_H, _CACHE, _P, _I, _P],
@@ -325,6 +327,13 @@ def mot_create_paged(cfg: mot_paged_config) -> Handle:
     out = ctypes.c_void_p()
     _check(_lib.mot_create_paged(ctypes.byref(cfg), ctypes.byref(out)), "mot_create_paged")
     return Handle(out.value, 0)
+
+
+def mot_paged_cause(h: Handle) -> int:
+    """MOT_PAGES_REFUSED and / or MOT_PAGES_HELD: what the last mot_get_device_status found."""
+    out = ctypes.c_int32()
+    _check(_lib.mot_paged_cause(h.ptr, ctypes.byref(out)), "mot_paged_cause")
+    return out.value
 
 
 def mot_paged_reserve(h: Handle, cache: mot_paged_cache, batch: mot_paged_batch, stream=None) -> None:

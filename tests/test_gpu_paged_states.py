@@ -80,3 +80,52 @@ def test_a_fork_of_a_bad_table_entry_counts_and_copies_no_page():
     for x, y in zip(want, (c.k, c.v)):
         x[:, last[1], :, :14] = x[:, c.t[0][1], :, :14]
         assert torch.equal(x, y)
+
+
+def test_a_refusal_is_still_reported_behind_a_timeout():
+    """A step whose reserve is refused and whose attention runs out of time (its first CTA loads nothing,
+    under a limit of some 10 ms) reports both, one a call, and changes are held back until both are read."""
+    c = P.Cache(q_heads=8, kv_heads=2, d=128, page=32, n_pages=40, max_seqs=3, max_pages=39)
+    c.reserve([0], [1100])
+    before = [x.clone() for x in (c.k, c.v)]
+    q = c.normal(100, 8, 128)
+    out, k = torch.zeros_like(q), c.normal(100, 2, 128)
+    b = c.batch([0], [100])
+    c.reserve([1], [500], ok=False)   # 16 pages of the 5 that are left
+    M.mot_debug_set(c.h, True, 20_000_000)
+    M.mot_paged_attention(c.h, 0, c.c, b, q, out)
+    M.mot_debug_set(c.h, False)
+    assert c.status() == M.MOT_ERR_TIMEOUT
+    M.mot_paged_append(c.h, 0, c.c, b, q, k, k, out)
+    c.reserve([1], [5], ok=False)
+    c.check("behind the refused reserve")
+    assert c.status() == M.MOT_ERR_PAGES
+    for x, y in zip(before, (c.k, c.v)):
+        assert torch.equal(x, y)
+    assert c.status() == M.MOT_OK
+    c.reserve([1], [5])
+    c.check()
+    assert c.status() == M.MOT_OK
+
+
+def test_a_refused_change_and_a_value_held_in_range_are_told_apart():
+    c = _torn()
+    flat = [c.normal(c.L, 1, c.H, 64, c.d) for _ in range(2)]
+
+    def load():
+        M.mot_paged_load(c.h, c.c, i32([1]), 1, *flat)
+
+    def refused():
+        c.free([0, 0], ok=False)
+
+    for calls, cause in (((), 0), ((load,), M.MOT_PAGES_HELD), ((refused,), M.MOT_PAGES_REFUSED),
+                         ((refused, load), M.MOT_PAGES_REFUSED | M.MOT_PAGES_HELD), ((), 0)):
+        for call in calls:
+            call()
+        assert c.status() == (M.MOT_ERR_PAGES if calls else M.MOT_OK)
+        assert M.mot_paged_cause(c.h) == cause
+    c.check()
+    other = M.mot_create_replay(M.mot_replay_config(4, 2, 64, 1, 64, 16, 1))
+    with pytest.raises(M.MotError) as e:
+        M.mot_paged_cause(other)
+    assert e.value.status == M.MOT_ERR_INVALID_ARG
