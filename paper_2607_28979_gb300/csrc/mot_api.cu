@@ -1363,16 +1363,20 @@ mot_status mot_translate_host(mot_handle h, const void* src_k, const void* src_v
 
 mot_status mot_get_device_status(mot_handle h, mot_stream_t stream) {
   if (!h) return MOT_ERR_INVALID_ARG;
+  if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  MOT_CUDA_TRY(cudaStreamSynchronize(st));
   int32_t v = 0;
-  MOT_CUDA_TRY(cudaMemcpy(&v, h->status, 4, cudaMemcpyDeviceToHost));
+  MOT_CUDA_TRY(cudaMemcpyAsync(&v, h->status, 4, cudaMemcpyDeviceToHost, st));
+  MOT_CUDA_TRY(cudaStreamSynchronize(st));
   // One cause is reported. What was found of a paged cache stays in the word until it is the one: a refused
   // change goes on holding back the changes behind it.
   const int32_t pages = v & (kStatusPages | kStatusPageUse);
   const bool other = (v & (kStatusTimeout | kStatusSeqLen)) != 0;
   const int32_t rest = other ? pages : 0;
-  MOT_CUDA_TRY(cudaMemcpy(h->status, &rest, 4, cudaMemcpyHostToDevice));
+  if (rest != v) {   // written before this returns: the handle's next call may be on any stream
+    MOT_CUDA_TRY(cudaMemcpyAsync(h->status, &rest, 4, cudaMemcpyHostToDevice, st));
+    MOT_CUDA_TRY(cudaStreamSynchronize(st));
+  }
   h->pages_cause = other ? 0 : (pages & kStatusPages ? MOT_PAGES_REFUSED : 0) | (pages & kStatusPageUse ? MOT_PAGES_HELD : 0);
   if (v & kStatusTimeout) return MOT_ERR_TIMEOUT;
   if (v & kStatusSeqLen) return MOT_ERR_SEQ_LEN;

@@ -57,3 +57,16 @@ def test_a_share_is_cleared_before_another_thread_may_set_it():
     between = body[cleared:found]
     dealt = between[:between.index("shfl")]   # before anything that the warp does together
     assert "by_warp" in dealt and "__syncwarp();" in dealt and "__syncthreads();" in dealt
+
+
+def test_the_status_word_is_cleared_before_its_reader_returns():
+    """A fill of device memory, or a small copy from ordinary host memory, may still be under way when its
+    call returns, and a kernel on a stream that does not wait for the default one would meet the old word
+    (a refused change holds the changes behind it back) or lose what it writes. So the word is changed on
+    the call's stream, and that is waited for."""
+    src = _source("mot_api.cu")
+    body = _body(src, "mot_get_device_status")
+    assert not re.search(r"\bcuda(Memset|Memcpy)\(", body)
+    changed = [m.end() for m in re.finditer(r"Async\(h->status", body)]
+    assert changed and "cudaStreamSynchronize(st)" in body[changed[-1]:body.index("return MOT_ERR_TIMEOUT")]
+    assert body.index("cudaSetDevice(h->device)") < body.index("Async(")
