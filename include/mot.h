@@ -473,8 +473,8 @@ mot_status mot_replay_select(mot_handle h, const void* guide, const int32_t* seq
  * workspace), nor may two calls that change one cache. What the device finds
  * is reported by mot_get_device_status as MOT_ERR_PAGES:
  *   - a change that cannot be made as a whole (reserve, fork, free: a slot
- *     outside the table or named twice, a length beyond max_pages P or
- *     2^30 - 1, not enough free pages; reserve: starts that fall or leave
+ *     outside the table or named twice, a length below 0 or beyond max_pages P
+ *     or 2^30 - 1, not enough free pages; reserve: starts that fall or leave
  *     0 .. rows; and what is said below) changes nothing,
  *     and neither do the calls behind it that change a cache (reserve, fork,
  *     free, compact, store, append) until the status has been read;

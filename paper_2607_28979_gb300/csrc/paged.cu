@@ -27,6 +27,11 @@ __device__ __forceinline__ bool mark_slot(uint32_t* marks, int s, int max_seqs) 
   return (atomicOr(&marks[s >> 5], bit) & bit) == 0;
 }
 
+// Whether a stored length, or one that a sequence is to get, is one that the table holds.
+__device__ __forceinline__ bool len_fits(const PagedDims& d, int64_t len) {
+  return len >= 0 && len <= (int64_t(d.max_pages) << d.lp) && len <= INT32_MAX / 2;
+}
+
 __device__ __forceinline__ int pages_of(const PagedDims& d, int len) { return (len + d.P - 1) >> d.lp; }
 
 // take[0 .. total): the lowest pages with refs <= 0, ascending. False where there are fewer.
@@ -71,7 +76,7 @@ __global__ void __launch_bounds__(kPlanThreads)
         bad = true;
       } else {
         const int len = c.lens[s];
-        if (len < 0 || int64_t(len) + m > (int64_t(d.max_pages) << d.lp) || int64_t(len) + m > INT32_MAX / 2)
+        if (len < 0 || !len_fits(d, int64_t(len) + m))
           bad = true;
         else
           need = pages_of(d, len + m) - pages_of(d, len);
@@ -112,15 +117,15 @@ __global__ void __launch_bounds__(kCopyThreads)
   // leaves (the batch is refused) or checks all of it
   if (__syncthreads_or(refused(w.status))) return;
   bool bad = false;
-  for (int i = tid; i < n; i += T) bad |= !mark_slot(marks, seqs[i], d.max_seqs);
+  for (int i = tid; i < n; i += T)   // a length that another CTA has freed by now is 0
+    bad |= !mark_slot(marks, seqs[i], d.max_seqs) || !len_fits(d, c.lens[seqs[i]]);
   if (__syncthreads_or(bad)) {
     if (tid == 0) atomicOr(w.status, kStatusPages);
     return;
   }
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int s = seqs[i];
-    const int len = c.lens[s];
-    const int pages = len <= 0 ? 0 : min(pages_of(d, min(len, INT32_MAX / 2)), d.max_pages);
+    const int pages = pages_of(d, c.lens[s]);
     int32_t* row = c.table + int64_t(s) * d.max_pages;
     for (int j = tid; j < pages; j += T) {
       const int p = row[j];
@@ -157,7 +162,7 @@ __global__ void __launch_bounds__(kPlanThreads)
         bad = true;
       } else {
         const int len = c.lens[a];
-        if (len < 0 || len > INT32_MAX / 2 || pages_of(d, len) > d.max_pages)
+        if (!len_fits(d, len))
           bad = true;
         else
           need = (len & (d.P - 1)) != 0;

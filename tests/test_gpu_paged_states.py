@@ -129,3 +129,25 @@ def test_a_refused_change_and_a_value_held_in_range_are_told_apart():
     with pytest.raises(M.MotError) as e:
         M.mot_paged_cause(other)
     assert e.value.status == M.MOT_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("length", [-1, -2 ** 31, 4 * 16 + 1, 2 ** 30, 2 ** 31 - 1])
+def test_changes_of_a_sequence_with_a_length_out_of_range_are_refused(length):
+    """A stored length that the table cannot hold: reserve, fork and free of that slot change nothing,
+    alone or among others, and the slot is as it was when its length is put right."""
+    c = P.Cache(n_pages=20, max_seqs=6, max_pages=4, page=16)
+    c.reserve([0, 1, 2], [20, 40, 5])
+    c.check()
+    c.n[1] = c.lens[1] = length
+    for call in (lambda: c.reserve([1], [1], ok=False), lambda: c.reserve([0, 1], [3, 0], ok=False),
+                 lambda: c.fork([1], [3], ok=False), lambda: c.fork([0, 1, 2], [3, 4, 5], ok=False),
+                 lambda: c.fork([0], [1], ok=False), lambda: c.free([1], ok=False), lambda: c.free([0, 2, 1], ok=False)):
+        call()
+        c.check()
+        assert c.status() == M.MOT_ERR_PAGES
+        assert M.mot_paged_cause(c.h) == M.MOT_PAGES_REFUSED
+    c.n[1] = c.lens[1] = 40
+    c.reserve([1, 0], [24, 1])
+    c.free([1])
+    c.check()
+    assert c.status() == M.MOT_OK
