@@ -289,7 +289,8 @@ __global__ void __launch_bounds__(kPlanThreads)
   }
 }
 
-// The moves' pages, all layers; the table's entries at or above the count of pages in use follow.
+// The moves' pages, all layers; the table's entries at or above the count of pages in use follow (without a
+// move the table is not read).
 __global__ void __launch_bounds__(kCopyThreads)
     paged_compact_kernel(const PagedDims d, const PagedCache c, const PagedWork w) {
   pdl_enter();   // behind the plan
@@ -312,11 +313,14 @@ __global__ void __launch_bounds__(kCopyThreads)
   for (int s = blockIdx.x * warps + (threadIdx.x >> 5); s < d.max_seqs; s += gridDim.x * warps) {
     const int len = c.lens[s];
     const int pages = len <= 0 ? 0 : min(pages_of(d, min(len, INT32_MAX / 2)), d.max_pages);
+    bool bad = !len_fits(d, len);
     int32_t* row = c.table + int64_t(s) * d.max_pages;
     for (int j = lane; j < pages; j += 32) {
       const int p = row[j];
+      bad |= p < 0 || p >= d.n_pages;
       if (p >= used && p < d.n_pages) row[j] = w.map[p];
     }
+    if (bad) atomicOr(w.status, kStatusPageUse);
   }
 }
 

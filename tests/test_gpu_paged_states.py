@@ -151,3 +151,23 @@ def test_changes_of_a_sequence_with_a_length_out_of_range_are_refused(length):
     c.free([1])
     c.check()
     assert c.status() == M.MOT_OK
+
+
+@pytest.mark.parametrize("length", [None, -3, 2 ** 30])
+def test_a_compaction_reports_what_it_finds_out_of_range(length):
+    """Bad table entries, and lengths that the table cannot hold; the good entries follow their pages."""
+    c = _torn()
+    c.reserve([2], [20])   # pages 6 and 7
+    if length is not None:
+        c.t[1][1], c.t[1][3] = 3, 5   # the entries are good, the length of slot 2 is not
+        c.table[1, :4] = i32(c.t[1])
+        c.lens[2] = length
+    c.free([0])
+    c.compact()   # six pages are in use: 6 and 7 move to 0 and 1
+    if length is not None:   # a row of no length is not read; one that is too long has its entries up to the table's end
+        c.n[2] = length
+        if length < 0:
+            c.t[2] = [6, 7]
+    c.check()
+    assert c.status() == M.MOT_ERR_PAGES
+    assert M.mot_paged_cause(c.h) == M.MOT_PAGES_HELD
