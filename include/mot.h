@@ -611,6 +611,10 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
  * they hold, NaN and infinities included; an infinite value that is seen gives
  * an infinite result, and a row whose scores are all -inf zeros. One row per entry is a decoding
  * step; any mixture with longer chunks is one call.
+ * Precision: scores, maxima and sums in fp32, the result rounded once. In bf16 with
+ * max_chunk * (q_heads / kv_heads) > 16 the weights enter the sums, numerator and
+ * denominator alike, rounded to bf16 (2^-8 of each); below that in two bf16
+ * parts (2^-17), so that the last bits of a row may differ with the call that it is in.
  */
 mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cache* cache,
                                const mot_paged_batch* batch, const void* q, void* out,

@@ -19,7 +19,11 @@
 //                                    running maximum (base 2; raised, and O and the sum rescaled, only
 //                                    when a tile exceeds it by 2^8) and sum, P as bf16 pairs into TMEM
 //                                    in two halves, so that the second product starts on the first
-//                                    while the other is made; at the end O from TMEM to the output or
+//                                    while the other is made (a second part of each weight, as the
+//                                    few-row kernel has it, would double the second product); the sum
+//                                    is of the rounded weights, 2% of the time more than of the
+//                                    unrounded ones, else one heavy weight's rounding (2^-8) stays in
+//                                    the result; at the end O from TMEM to the output or
 //                                    to the piece's partial results.
 //                       What bounds it: S_i cannot be made again before P_i V is done (P_i lies over it),
 //                       so a stream is a chain of two products, the softmax and the commits and wake-ups
@@ -465,7 +469,8 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
           if (raise) m = mx;
           const float mu = m == -INFINITY ? 0.f : m;
           const uint64_t s2 = f32x2(sl2, sl2), nm2 = f32x2(-mu, -mu);
-          uint64_t sum[2] = {0ull, 0ull};
+          // the sum of the weights as the product takes them: where one of them is most of it, its rounding cancels
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             uint32_t pk[16];
@@ -474,9 +479,9 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
               const uint64_t x = ffma_x2((static_cast<uint64_t>(v[e][2 * k + 1]) << 32) | v[e][2 * k], s2, nm2);
               const float p0 = ex2_fast(__uint_as_float(static_cast<uint32_t>(x)));
               const float p1 = ex2_fast(__uint_as_float(static_cast<uint32_t>(x >> 32)));
-              sum[k & 1] = fadd_x2(sum[k & 1], f32x2(p0, p1));
               __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);
               pk[k] = *reinterpret_cast<uint32_t*>(&pb);
+              add_bf16x2(sum[2 * (k & 1)], sum[2 * (k & 1) + 1], pk[k]);
             }
             tmem_st_32x32b_x16(tS + 16 * e, pk);
             if (e & 1) {
@@ -486,8 +491,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
               if (lane == 0) mbar_arrive(&sh.p_half[i][e >> 1]);
             }
           }
-          const uint64_t s01 = fadd_x2(sum[0], sum[1]);
-          l += __uint_as_float(static_cast<uint32_t>(s01)) + __uint_as_float(static_cast<uint32_t>(s01 >> 32));
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
         ok = ok && wait(&sh.pv_done[i], (t - 1) & 1u);
       }

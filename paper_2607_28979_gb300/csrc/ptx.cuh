@@ -703,6 +703,14 @@ __device__ __forceinline__ uint64_t fadd_x2(uint64_t a, uint64_t b) {
   return d;
 }
 
+// lo += the lower, hi += the upper of a pair of bf16, in fp32 (exact operands, one instruction each).
+__device__ __forceinline__ void add_bf16x2(float& lo, float& hi, uint32_t pair) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+      "add.f32.bf16 %0, a, %0;\n\tadd.f32.bf16 %1, b, %1;\n\t}"
+      : "+f"(lo), "+f"(hi)
+      : "r"(pair));
+}
+
 __device__ __forceinline__ uint32_t tanh_approx_f16x2(uint32_t x) {
   uint32_t y;
   asm("tanh.approx.f16x2 %0, %1;" : "=r"(y) : "r"(x));
