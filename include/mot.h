@@ -608,9 +608,11 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
  * q, out: [rows][q_heads][head_dim], 16-byte aligned. A row before position 0
  * (a sequence shorter than its rows) sees nothing and is written as zeros;
  * rows of no entry are not written. Positions behind p add nothing, whatever
- * they hold, NaN and infinities included; an infinite value that is seen gives
- * an infinite result, and a row whose scores are all -inf zeros. One row per entry is a decoding
- * step; any mixture with longer chunks is one call.
+ * they hold, NaN and infinities included. An infinite value that is seen gives
+ * that infinity where its weight beside the row's largest is 2^-100 or more, and an
+ * infinity or NaN where it is less. A row whose scores are all -inf is zeros,
+ * whatever its values are.
+ * One row per entry is a decoding step; any mixture with longer chunks is one call.
  * Precision: scores, maxima and sums in fp32, the result rounded once. In bf16 with
  * max_chunk * (q_heads / kv_heads) > 16 the weights enter the sums, numerator and
  * denominator alike, rounded to bf16 (2^-8 of each); below that in two bf16

@@ -320,14 +320,19 @@ __device__ __forceinline__ int64_t paged_out_row(const PagedCursor& c, int H, in
   const int t = r / G;
   return (int64_t(c.s.r0 + t) * H + c.hk) * G + (r - t * G);
 }
+// Four columns of a result: the weighted sums over the sum of the weights, and 0 where no weight is above 0
+// (the sums are 0 or, by values that are not finite, NaN then).
 template <class T>
-__device__ __forceinline__ void paged_store4(T* dst, const float (&o)[4], float f) {
+__device__ __forceinline__ void paged_store4(T* dst, const float (&o)[4], float l) {
+  const bool none = l == 0.f;
+  const float f = 1.f / l;
+  const float4 r = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
   if constexpr (sizeof(T) == 2) {
-    __nv_bfloat162 x = __floats2bfloat162_rn(o[0] * f, o[1] * f), y = __floats2bfloat162_rn(o[2] * f, o[3] * f);
+    __nv_bfloat162 x = __floats2bfloat162_rn(r.x, r.y), y = __floats2bfloat162_rn(r.z, r.w);
     *reinterpret_cast<uint2*>(dst) =
         make_uint2(*reinterpret_cast<uint32_t*>(&x), *reinterpret_cast<uint32_t*>(&y));
   } else {
-    *reinterpret_cast<float4*>(dst) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
+    *reinterpret_cast<float4*>(dst) = r;
   }
 }
 
@@ -421,7 +426,7 @@ __device__ __forceinline__ void paged_join(const PagedAttnArgs& a, const PagedCu
     }
     if (g.final) {
       if (x0 + tid < items)
-        paged_store4(static_cast<T*>(a.out) + paged_out_row(c, a.d.H, G, r0 + r) * D + col, o, l == 0.f ? 0.f : 1.f / l);
+        paged_store4(static_cast<T*>(a.out) + paged_out_row(c, a.d.H, G, r0 + r) * D + col, o, l);
     } else {
       float* part = paged_place<BM, D>(a, g, 0);
       __syncthreads();   // a row's maximum and sum have been read by the threads of all its columns

@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kDecThreads, kResident<D, NT>) paged_decode_ke
           part[BM * (D + 1) + r] = ll;
         }
       } else {
-        paged_store4(static_cast<uint16_t*>(a.out) + paged_out_row(c, H, G, r0 + r) * D + col, y, ll == 0.f ? 0.f : 1.f / ll);
+        paged_store4(static_cast<uint16_t*>(a.out) + paged_out_row(c, H, G, r0 + r) * D + col, y, ll);
       }
     }
     if (part) paged_finish<uint16_t, BM, D>(a, c, p, s_join, tid, kDecThreads);

@@ -131,6 +131,10 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const PagedCur
       continue;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (l == 0.f) {   // no weight is above 0 (values that are not finite make NaN of 0)
+#pragma unroll
+      for (int k = 0; k < 32; ++k) o[k] = 0.f;
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint32_t w[4];
@@ -502,6 +506,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
         uint32_t any = 0;   // notes of this piece (uniform over the CTA)
 #pragma unroll
         for (int e = 0; e < 16; ++e) any |= reinterpret_cast<volatile uint32_t*>(sh.notes[piece & 3])[e];
+        const bool seen = pos >= p.kt * F::kTK;   // a key of the piece; else O may not have been written
         const float f = l == 0.f ? 0.f : 1.f / l;
         uint16_t* dst = static_cast<uint16_t*>(a.out) + out_row * D;
 #pragma unroll 1
@@ -509,11 +514,11 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
           uint32_t o[32];
           tmem_ld_32x32b_x32(tO + 32 * e, o);
           tmem_ld_wait(o);
-          if (l == 0.f) {   // no key was seen
+          if (!seen || (l == 0.f && !part)) {   // a result without weights is 0 whatever the values are
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = 0u;
           }
-          if (any) {   // values that are not finite, of keys that this row sees
+          if (any && (l != 0.f || part)) {   // values that are not finite, of keys that this row sees
             for (int kt = max(masked, p.kt); kt < p.kt + p.n; ++kt)
               for (int w = 0; w < 4; ++w)
                 for (uint32_t bits = sh.notes[piece & 3][min(kt - masked, 3)][w]; bits; bits &= bits - 1) {

@@ -200,12 +200,11 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const __grid_c
       for (int i = 0; i < kR; ++i) {
         const int r = ty * kR + i;
         if (r >= n_rows) continue;
-        const float f = l[i] == 0.f ? 0.f : 1.f / l[i];
         float* dst = static_cast<float*>(a.out) + paged_out_row(c, H, G, r0 + r) * D;
 #pragma unroll
         for (int h = 0; h < kC; ++h) {
           const float t[4] = {lo_f(o[i][2 * h]), hi_f(o[i][2 * h]), lo_f(o[i][2 * h + 1]), hi_f(o[i][2 * h + 1])};
-          paged_store4(dst + 64 * h + 4 * tx, t, f);
+          paged_store4(dst + 64 * h + 4 * tx, t, l[i]);
         }
       }
     } else {

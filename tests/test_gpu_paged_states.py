@@ -171,3 +171,79 @@ def test_a_compaction_reports_what_it_finds_out_of_range(length):
     c.check()
     assert c.status() == M.MOT_ERR_PAGES
     assert M.mot_paged_cause(c.h) == M.MOT_PAGES_HELD
+
+
+def _with_keys(n, first, dtype, d=64):
+    """A sequence of n positions whose keys are `first` [n] in their first dimension and 0 in the others,
+    and queries [..][4][d] of ones there: scores of first / sqrt(d)."""
+    c = P.Cache(q_heads=4, kv_heads=2, d=d, page=32, n_pages=-(-n // 32), max_seqs=1, max_pages=-(-n // 32), dtype=dtype)
+    c.reserve([0], [n])
+    flat = [torch.zeros((1, 1, 2, n, d), dtype=P.DT[dtype], device="cuda"), c.normal(1, 1, 2, n, d)]
+    flat[0][0, 0, :, :, 0] = first.to(P.DT[dtype])
+    return c, flat
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 4, 60, 300])
+@pytest.mark.parametrize("n", [640, 20000])
+def test_infinite_values_of_small_and_of_no_weight(n, new, dtype):
+    """The header's sentences: an infinite value comes out as itself while its weight is 2^-90 of the row's
+    largest, and as no finite number where its weight is none in 32 bits; other columns are finite. The
+    keys lie in tiles that every row sees as a whole, in the same CTA's keys as the largest and in others."""
+    c, flat = _with_keys(n, torch.zeros(n, device="cuda"), dtype)
+    small, none = [30, 200], [40, 250]   # in the tiles before the last 300 positions
+    unit = 8 / 1.4426950408889634        # a base-2 step of the scores
+    flat[0][0, 0, :, small, 0] = -90 * unit
+    flat[0][0, 0, :, none, 0] = -400 * unit
+    flat[1][0, 0, :, 30, 3], flat[1][0, 0, :, 200, 5] = float("inf"), float("-inf")
+    flat[1][0, 0, :, 40, 7], flat[1][0, 0, :, 250, 9] = float("inf"), float("-inf")
+    M.mot_paged_store(c.h, c.c, i32([0]), 1, *flat)
+    q = torch.zeros((new, 4, 64), dtype=P.DT[dtype], device="cuda")
+    q[..., 0] = 1
+    out = torch.zeros_like(q)
+    M.mot_paged_attention(c.h, 0, c.c, c.batch([0], [new]), q, out)
+    assert c.status() == M.MOT_OK
+    assert bool((out[..., 3] == float("inf")).all()) and bool((out[..., 5] == float("-inf")).all())
+    assert not bool(torch.isfinite(out[..., [7, 9]]).any())
+    rest = [i for i in range(64) if i not in (3, 5, 7, 9)]
+    assert bool(torch.isfinite(out[..., rest]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 4, 60])
+def test_rows_without_weights_are_zeros_whatever_the_values_are(new, dtype):
+    c, flat = _with_keys(640, torch.full((640,), float("-inf"), device="cuda"), dtype)
+    flat[1][0, 0, :, 30, 3], flat[1][0, 0, :, 500, 5], flat[1][0, 0, :, 200, 7] = float("inf"), float("nan"), float("-inf")
+    flat[0][0, 0, :, :, 1:] = float("-inf")
+    q = torch.ones((new, 4, 64), dtype=P.DT[dtype], device="cuda")
+    M.mot_paged_store(c.h, c.c, i32([0]), 1, *flat)
+    out = torch.zeros_like(q)
+    M.mot_paged_attention(c.h, 0, c.c, c.batch([0], [new]), q, out)
+    assert c.status() == M.MOT_OK
+    assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 4, 60])
+def test_infinite_values_beside_keys_of_no_weight_at_all(new, dtype):
+    """Long stretches of keys whose scores are -inf, each with an infinite value, so that whole CTAs see no
+    weight; the other keys weigh alike. The values' columns are not finite, the others are as the keys with
+    weight have them."""
+    n = 20000
+    first = torch.zeros(n, device="cuda")
+    first[1000:9000] = first[12000:12100] = first[19500:19900] = float("-inf")
+    c, flat = _with_keys(n, first, dtype)
+    for j, col in ((1500, 3), (8000, 5), (12050, 7), (19600, 9)):
+        flat[1][0, 0, :, j, col] = float("inf")
+    flat[1][..., 20] = 3.0
+    M.mot_paged_store(c.h, c.c, i32([0]), 1, *flat)
+    q = torch.zeros((new, 4, 64), dtype=P.DT[dtype], device="cuda")
+    q[..., 0] = 1
+    out = torch.zeros_like(q)
+    M.mot_paged_attention(c.h, 0, c.c, c.batch([0], [new]), q, out)
+    assert c.status() == M.MOT_OK
+    assert not bool(torch.isfinite(out[..., [3, 5, 7, 9]]).any())
+    assert bool(torch.isfinite(out[..., [i for i in range(64) if i not in (3, 5, 7, 9)]]).all())
+    # 12,000 equal weights: sums of n terms are off by n 2^-24 at most on either side
+    P.assert_close(out[..., 20], torch.full((new, 4), 3.0, dtype=torch.float64, device="cuda"),
+                   P.HALF[dtype] * 3 + 2 * n * 2.0 ** -24 * 3)
