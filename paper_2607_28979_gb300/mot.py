@@ -198,6 +198,9 @@ def _stream(s) -> Optional[int]:
 class Handle:
     """Owns one ``mot_handle``; destroyed with ``mot_destroy`` or on GC."""
 
+    paged = None    # the config of a paged handle
+    device = None   # its device, where torch had one when it was made
+
     def __init__(self, ptr: int, n_layers_tgt: int):
         self.ptr = ptr
         self.n_layers_tgt = n_layers_tgt
@@ -305,10 +308,46 @@ def make_paged_config(n_layers, q_heads, kv_heads, head_dim, page, n_pages, max_
                             MOT_BF16 if dtype in ("bf16", MOT_BF16) else MOT_FP32, norm_eps, rot_base)
 
 
+# What the paged calls take as tensors is checked against the handle: contiguous device memory of its type and
+# at least its sizes. Addresses (ints) and None go to the library as they are. A set of types holds their names,
+# and the types themselves as they come.
+_FLOATS = {MOT_BF16: {"torch.bfloat16", "torch.int16", "torch.uint16"},   # the values, or their bits
+           MOT_FP32: {"torch.float32"}}
+_INT32 = {"torch.int32"}
+
+
+def _bad(where: str, what: str) -> MotError:
+    return MotError(MOT_ERR_INVALID_ARG, f"{where}, {what}")
+
+
+def _typed(x, kinds, where: str, what: str, dev) -> None:
+    """Raises unless x is on the GPU (``dev``, where it is known) and of one of the types."""
+    if not getattr(x, "is_cuda", False):
+        raise _bad(where, f"{what} is not a CUDA tensor")
+    if x.dtype not in kinds:
+        if str(x.dtype) not in kinds:
+            raise _bad(where, f"{what} is of type {x.dtype}")
+        kinds.add(x.dtype)
+    if dev is not None and x.get_device() != dev:
+        raise _bad(where, f"{what} is on another device than the handle")
+
+
+def _whole(x, kinds, least: int, where: str, what: str, dev) -> Optional[int]:
+    """The address of x: contiguous, ``least`` elements or more."""
+    if x is None or isinstance(x, int):
+        return x
+    _typed(x, kinds, where, what, dev)
+    if not x.is_contiguous():
+        raise _bad(where, f"{what} is not contiguous")
+    if x.numel() < least:
+        raise _bad(where, f"{what} has {x.numel()} elements, {least} are read or written")
+    return x.data_ptr()
+
+
 def paged_cache(k, v, table, lens, refs) -> mot_paged_cache:
     """The arrays of a paged cache (contiguous device tensors): pools k, v
     [n_layers][n_pages][kv_heads][page][head_dim], int32 table [max_seqs][max_pages], lens
-    [max_seqs] and refs [n_pages]. The struct keeps the tensors."""
+    [max_seqs] and refs [n_pages]. The struct keeps the tensors; the calls check them."""
     c = mot_paged_cache(*[_addr(x) for x in (k, v, table, lens, refs)])
     c._keep = (k, v, table, lens, refs)
     return c
@@ -326,7 +365,47 @@ def paged_batch(seqs, starts, n: int, rows: int, max_chunk: Optional[int] = None
 def mot_create_paged(cfg: mot_paged_config) -> Handle:
     out = ctypes.c_void_p()
     _check(_lib.mot_create_paged(ctypes.byref(cfg), ctypes.byref(out)), "mot_create_paged")
-    return Handle(out.value, 0)
+    h = Handle(out.value, 0)
+    h.paged = mot_paged_config.from_buffer_copy(cfg)
+    torch = sys.modules.get("torch")
+    if torch is not None and torch.cuda.is_initialized():
+        h.device = torch.cuda.current_device()
+    return h
+
+
+def _fits(h: Handle, cache: mot_paged_cache, where: str) -> Optional[mot_paged_config]:
+    """The handle's config (None: no paged handle, which the library refuses); raises where the cache's
+    tensors are not those of such a handle. A cache that fitted is not looked at again."""
+    cfg = h.paged
+    if cfg is None or getattr(cache, "_fitted", None) is cfg:
+        return cfg
+    keep = getattr(cache, "_keep", None)
+    if keep is not None:
+        c = cfg
+        form = (c.n_pages, c.kv_heads, c.page, c.head_dim)
+        for x, what in zip(keep, "kv"):
+            _whole(x, _FLOATS[c.dtype], 0, where, what, h.device)
+            if hasattr(x, "shape") and (tuple(x.shape[1:]) != form or x.shape[0] < c.n_layers):
+                raise _bad(where, f"{what} is {tuple(x.shape)}, the handle's pools are {(c.n_layers,) + form}")
+        table, lens, refs = keep[2:]
+        _whole(table, _INT32, c.max_seqs * c.max_pages, where, "table", h.device)
+        if hasattr(table, "shape") and table.shape[-1] != c.max_pages and table.dim() > 1:
+            raise _bad(where, f"table is {tuple(table.shape)}, the handle's {(c.max_seqs, c.max_pages)}")
+        _whole(lens, _INT32, c.max_seqs, where, "lens", h.device)
+        _whole(refs, _INT32, c.n_pages, where, "refs", h.device)
+    cache._fitted = cfg
+    return cfg
+
+
+def _batch_fits(h: Handle, batch: mot_paged_batch, where: str) -> int:
+    """The batch's rows; raises where its tensors are shorter than its n says."""
+    keep, n = getattr(batch, "_keep", None), batch.n
+    if keep is not None and getattr(batch, "_fitted", None) != n:
+        if 0 < n <= h.paged.max_seqs:   # else nothing is read, or the library refuses it
+            _whole(keep[0], _INT32, n, where, "seqs", h.device)
+            _whole(keep[1], _INT32, n + 1, where, "starts", h.device)
+            batch._fitted = n
+    return batch.rows
 
 
 def mot_paged_cause(h: Handle) -> int:
@@ -337,32 +416,46 @@ def mot_paged_cause(h: Handle) -> int:
 
 
 def mot_paged_reserve(h: Handle, cache: mot_paged_cache, batch: mot_paged_batch, stream=None) -> None:
-    _check(_lib.mot_paged_reserve(h.ptr, ctypes.byref(cache), ctypes.byref(batch), _stream(stream)),
-           "mot_paged_reserve")
+    where = "mot_paged_reserve"
+    if _fits(h, cache, where) is not None:
+        _batch_fits(h, batch, where)
+    _check(_lib.mot_paged_reserve(h.ptr, ctypes.byref(cache), ctypes.byref(batch), _stream(stream)), where)
 
 
 def mot_paged_fork(h: Handle, cache: mot_paged_cache, src, dst, n: int, stream=None) -> None:
-    _check(_lib.mot_paged_fork(h.ptr, ctypes.byref(cache), _addr(src), _addr(dst), int(n),
-                               _stream(stream)), "mot_paged_fork")
+    where = "mot_paged_fork"
+    _fits(h, cache, where)
+    _check(_lib.mot_paged_fork(h.ptr, ctypes.byref(cache), _whole(src, _INT32, n, where, "src", h.device),
+                               _whole(dst, _INT32, n, where, "dst", h.device), int(n), _stream(stream)), where)
 
 
 def mot_paged_free(h: Handle, cache: mot_paged_cache, seqs, n: int, stream=None) -> None:
-    _check(_lib.mot_paged_free(h.ptr, ctypes.byref(cache), _addr(seqs), int(n), _stream(stream)),
-           "mot_paged_free")
+    where = "mot_paged_free"
+    _fits(h, cache, where)
+    _check(_lib.mot_paged_free(h.ptr, ctypes.byref(cache), _whole(seqs, _INT32, n, where, "seqs", h.device), int(n),
+                               _stream(stream)), where)
 
 
 def mot_paged_compact(h: Handle, cache: mot_paged_cache, live=None, stream=None) -> None:
-    _check(_lib.mot_paged_compact(h.ptr, ctypes.byref(cache), _addr(live), _stream(stream)),
-           "mot_paged_compact")
+    where = "mot_paged_compact"
+    _fits(h, cache, where)
+    _check(_lib.mot_paged_compact(h.ptr, ctypes.byref(cache), _whole(live, _INT32, 1, where, "live", h.device),
+                                  _stream(stream)), where)
 
 
-def _contiguous_shape(k, v):
+def _contiguous_shape(h, k, v, where):
     """(n_layers, batch, max_seq) of contiguous caches [n_layers][batch][kv_heads][max_seq][head_dim]."""
     if tuple(k.shape) != tuple(v.shape) or len(k.shape) != 5:
         raise ValueError("contiguous caches are [n_layers][batch][kv_heads][max_seq][head_dim], K and V alike")
     for x in (k, v):
         if hasattr(x, "is_contiguous") and not x.is_contiguous():
             raise ValueError("contiguous caches are wanted")
+    c = h.paged
+    if c is not None:
+        for x, what in ((k, "K"), (v, "V")):
+            _typed(x, _FLOATS[c.dtype], where, what, h.device)
+        if k.shape[2] != c.kv_heads or k.shape[4] != c.head_dim:
+            raise _bad(where, f"{k.shape[2]} heads of {k.shape[4]}, the handle's are {c.kv_heads} of {c.head_dim}")
     return int(k.shape[0]), int(k.shape[1]), int(k.shape[3])
 
 
@@ -370,26 +463,35 @@ def mot_paged_store(h: Handle, cache: mot_paged_cache, seqs, n: int, src_k, src_
                     stream=None) -> None:
     """Tensors src_k, src_v [n_layers][batch][kv_heads][max_seq][head_dim] into the pages of the
     slots ``seqs``, layers first_layer ..."""
-    layers, batch, max_seq = _contiguous_shape(src_k, src_v)
-    _check(_lib.mot_paged_store(h.ptr, ctypes.byref(cache), int(first_layer), layers, _addr(seqs), int(n),
-                                batch, max_seq, _addr(src_k), _addr(src_v), _stream(stream)),
-           "mot_paged_store")
+    where = "mot_paged_store"
+    _fits(h, cache, where)
+    layers, batch, max_seq = _contiguous_shape(h, src_k, src_v, where)
+    _check(_lib.mot_paged_store(h.ptr, ctypes.byref(cache), int(first_layer), layers,
+                                _whole(seqs, _INT32, n, where, "seqs", h.device), int(n), batch, max_seq,
+                                _addr(src_k), _addr(src_v), _stream(stream)), where)
 
 
 def mot_paged_load(h: Handle, cache: mot_paged_cache, seqs, n: int, dst_k, dst_v, first_layer: int = 0,
                    stream=None) -> None:
     """The pages of the slots ``seqs`` into tensors [n_layers][batch][kv_heads][max_seq][head_dim]."""
-    layers, batch, max_seq = _contiguous_shape(dst_k, dst_v)
-    _check(_lib.mot_paged_load(h.ptr, ctypes.byref(cache), int(first_layer), layers, _addr(seqs), int(n),
-                               batch, max_seq, _addr(dst_k), _addr(dst_v), _stream(stream)),
-           "mot_paged_load")
+    where = "mot_paged_load"
+    _fits(h, cache, where)
+    layers, batch, max_seq = _contiguous_shape(h, dst_k, dst_v, where)
+    _check(_lib.mot_paged_load(h.ptr, ctypes.byref(cache), int(first_layer), layers,
+                               _whole(seqs, _INT32, n, where, "seqs", h.device), int(n), batch, max_seq,
+                               _addr(dst_k), _addr(dst_v), _stream(stream)), where)
 
 
-def _row_stride(x, what: str) -> int:
-    if x.dim() == 3:
-        rows, heads, last = x.stride()
-        if last == 1 and heads == x.size(2):
-            return rows if x.size(0) > 1 else max(rows, x.size(1) * heads)
+def _row_stride(x, what: str, least=None, where: str = "") -> int:
+    """The stride of rows [heads][head_dim]; ``least``: (rows, heads, head_dim) that x has to hold."""
+    shape, strides = x.shape, x.stride()
+    if len(shape) == 3:
+        n, heads, d = shape
+        row, head, last = strides
+        if last == 1 and (head == d or heads == 1):
+            if least is not None and (n < least[0] or heads != least[1] or d != least[2]):
+                raise _bad(where, f"{what} is {tuple(shape)}, the handle's is {least}")
+            return row if n > 1 else heads * d   # the stride of a single row, or head, says nothing
     raise ValueError(f"{what}: [rows][heads][head_dim] with contiguous rows is wanted")
 
 
@@ -397,16 +499,35 @@ def mot_paged_append(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_p
                      q_norm=None, k_norm=None, stream=None) -> None:
     """Tensors q, k, v [rows][heads][head_dim], whose rows may lie apart (columns of a fused
     projection); q_out [rows][q_heads][head_dim] contiguous."""
-    _check(_lib.mot_paged_append(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), _addr(q),
-                                 _row_stride(q, "q"), _addr(k), _row_stride(k, "k"), _addr(v),
-                                 _row_stride(v, "v"), _addr(q_norm), _addr(k_norm), _addr(q_out),
-                                 _stream(stream)), "mot_paged_append")
+    where = "mot_paged_append"
+    c, dev = _fits(h, cache, where), h.device
+    if c is None:
+        strides = [_row_stride(x, what) for x, what in ((q, "q"), (k, "k"), (v, "v"))]
+    else:
+        rows, kinds, hq, d = _batch_fits(h, batch, where), _FLOATS[c.dtype], c.q_heads, c.head_dim
+        kv = (rows, c.kv_heads, d)
+        strides = _row_stride(q, "q", (rows, hq, d), where), _row_stride(k, "k", kv, where), _row_stride(v, "v", kv, where)
+        for x, what in ((q, "q"), (k, "k"), (v, "v")):
+            _typed(x, kinds, where, what, dev)
+        q_out = _whole(q_out, kinds, rows * hq * d, where, "q_out", dev)
+        q_norm, k_norm = _whole(q_norm, kinds, d, where, "q_norm", dev), _whole(k_norm, kinds, d, where, "k_norm", dev)
+    _check(_lib.mot_paged_append(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), _addr(q), strides[0],
+                                 _addr(k), strides[1], _addr(v), strides[2], _addr(q_norm), _addr(k_norm),
+                                 _addr(q_out), _stream(stream)), where)
 
 
 def mot_paged_attention(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, out,
                         stream=None) -> None:
-    _check(_lib.mot_paged_attention(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), _addr(q),
-                                    _addr(out), _stream(stream)), "mot_paged_attention")
+    """Tensors q, out [rows][q_heads][head_dim], contiguous."""
+    where = "mot_paged_attention"
+    c, dev = _fits(h, cache, where), h.device
+    if c is None:
+        q, out = _addr(q), _addr(out)
+    else:
+        least, kinds = _batch_fits(h, batch, where) * c.q_heads * c.head_dim, _FLOATS[c.dtype]
+        q, out = _whole(q, kinds, least, where, "q", dev), _whole(out, kinds, least, where, "out", dev)
+    _check(_lib.mot_paged_attention(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), q, out,
+                                    _stream(stream)), where)
 
 
 def mot_create(cfg: mot_config) -> Handle:
