@@ -1914,34 +1914,64 @@ size_t paged_es(const PagedDims& d) { return d.dtype ? 4 : 2; }
 size_t paged_layer_bytes(const PagedDims& d) { return size_t(d.n_pages) * d.H * d.P * d.d * paged_es(d); }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
+struct PagedSpan {
+  const void* p;
+  size_t n;
+};
+void paged_spans(const PagedDims& d, const PagedCache& c, PagedSpan (&s)[5]) {
+  const size_t pool = paged_layer_bytes(d) * d.L;
+  s[0] = {c.k, pool};
+  s[1] = {c.v, pool};
+  s[2] = {c.table, size_t(d.max_seqs) * d.max_pages * 4};
+  s[3] = {c.lens, size_t(d.max_seqs) * 4};
+  s[4] = {c.refs, size_t(d.n_pages) * 4};
+}
+
 mot_status paged_args(mot_handle h, const mot_paged_cache* c, PagedCache& pc) {
   if (!h || h->kind != 4 || !c) return MOT_ERR_INVALID_ARG;
   if (!c->k || !c->v || !c->table || !c->lens || !c->refs || !aligned16(c->k) || !aligned16(c->v) ||
       !aligned4(c->table) || !aligned4(c->lens) || !aligned4(c->refs))
     return MOT_ERR_INVALID_ARG;
-  const size_t bytes = paged_layer_bytes(h->pd) * h->pd.L;
-  if (overlap(c->k, bytes, c->v, bytes)) return MOT_ERR_INVALID_ARG;
   pc = PagedCache{c->k, c->v, c->table, c->lens, c->refs};
+  PagedSpan s[5];
+  paged_spans(h->pd, pc, s);
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(s[i].p, s[i].n, s[j].p, s[j].n)) return MOT_ERR_INVALID_ARG;
   return MOT_OK;
 }
 
-// Whether [p, p + n) meets the pools.
+// Whether [p, p + n) meets the pools, or any of the cache's arrays.
 bool meets_pools(const mot_ctx* h, const PagedCache& c, const void* p, size_t n) {
   const size_t bytes = paged_layer_bytes(h->pd) * h->pd.L;
   return overlap(p, n, c.k, bytes) || overlap(p, n, c.v, bytes);
 }
+bool meets_cache(const mot_ctx* h, const PagedCache& c, const void* p, size_t n) {
+  PagedSpan s[5];
+  paged_spans(h->pd, c, s);
+  for (const PagedSpan& x : s)
+    if (overlap(p, n, x.p, x.n)) return true;
+  return false;
+}
+// Whether [p, p + n), which a call writes, meets the batch's arrays.
+bool meets_batch(const PagedBatch& b, const void* p, size_t n) {
+  return overlap(p, n, b.seqs, size_t(b.n) * 4) || overlap(p, n, b.starts, (size_t(b.n) + 1) * 4);
+}
 
-mot_status paged_batch_args(mot_handle h, const mot_paged_batch* b, PagedBatch& pb) {
+mot_status paged_batch_args(mot_handle h, const PagedCache& c, const mot_paged_batch* b, PagedBatch& pb) {
   if (!b || b->n < 0 || b->n > h->pd.max_seqs || b->rows < 0 || b->rows > (1 << 26) || b->max_chunk < 0)
     return MOT_ERR_INVALID_ARG;
   if (b->n > 0 && (!b->seqs || !b->starts || !aligned4(b->seqs) || !aligned4(b->starts)))
     return MOT_ERR_INVALID_ARG;
   pb = PagedBatch{b->seqs, b->starts, b->n, b->rows};
+  if (b->n > 0 && (meets_cache(h, c, b->seqs, size_t(b->n) * 4) || meets_cache(h, c, b->starts, (size_t(b->n) + 1) * 4)))
+    return MOT_ERR_INVALID_ARG;
   return MOT_OK;
 }
 
-mot_status paged_slots(mot_handle h, const int32_t* seqs, int32_t n) {
-  if (n < 0 || n > h->pd.max_seqs || (n > 0 && (!seqs || !aligned4(seqs)))) return MOT_ERR_INVALID_ARG;
+mot_status paged_slots(mot_handle h, const PagedCache& c, const int32_t* seqs, int32_t n) {
+  if (n < 0 || n > h->pd.max_seqs || (n > 0 && (!seqs || !aligned4(seqs) || meets_cache(h, c, seqs, size_t(n) * 4))))
+    return MOT_ERR_INVALID_ARG;
   return MOT_OK;
 }
 
@@ -1950,13 +1980,19 @@ mot_status paged_copy(mot_handle h, const mot_paged_cache* cache, const PagedCop
   mot_status r = paged_args(h, cache, c);
   if (r != MOT_OK) return r;
   const PagedDims& d = h->pd;
-  if ((r = paged_slots(h, p.seqs, p.n)) != MOT_OK) return r;
+  if ((r = paged_slots(h, c, p.seqs, p.n)) != MOT_OK) return r;
   if (p.first < 0 || p.n_layers <= 0 || p.first > d.L - p.n_layers || p.B < p.n || p.B <= 0 || p.S <= 0)
     return MOT_ERR_INVALID_ARG;
   if (!p.k || !p.v || !aligned16(p.k) || !aligned16(p.v)) return MOT_ERR_INVALID_ARG;
   const size_t bytes = size_t(p.n_layers) * p.B * d.H * size_t(p.S) * d.d * paged_es(d);
   if (overlap(p.k, bytes, p.v, bytes) || meets_pools(h, c, p.k, bytes) || meets_pools(h, c, p.v, bytes))
     return MOT_ERR_INVALID_ARG;
+  if (!p.store) {   // writes them
+    const size_t sb = size_t(p.n) * 4;
+    if (meets_cache(h, c, p.k, bytes) || meets_cache(h, c, p.v, bytes) || overlap(p.k, bytes, p.seqs, sb) ||
+        overlap(p.v, bytes, p.seqs, sb))
+      return MOT_ERR_INVALID_ARG;
+  }
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   if (p.n == 0) return MOT_OK;
   MOT_CUDA_TRY(timed(h, p.store ? "paged_store" : "paged_load", st,
@@ -1978,7 +2014,7 @@ mot_status mot_paged_reserve(mot_handle h, const mot_paged_cache* cache, const m
   PagedCache c;
   PagedBatch b;
   mot_status r = paged_args(h, cache, c);
-  if (r != MOT_OK || (r = paged_batch_args(h, batch, b)) != MOT_OK) return r;
+  if (r != MOT_OK || (r = paged_batch_args(h, c, batch, b)) != MOT_OK) return r;
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   if (b.n == 0) return MOT_OK;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -1991,7 +2027,7 @@ mot_status mot_paged_fork(mot_handle h, const mot_paged_cache* cache, const int3
   NvtxRange range("mot_paged_fork");
   PagedCache c;
   mot_status r = paged_args(h, cache, c);
-  if (r != MOT_OK || (r = paged_slots(h, src, n)) != MOT_OK || (r = paged_slots(h, dst, n)) != MOT_OK) return r;
+  if (r != MOT_OK || (r = paged_slots(h, c, src, n)) != MOT_OK || (r = paged_slots(h, c, dst, n)) != MOT_OK) return r;
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   if (n == 0) return MOT_OK;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -2006,7 +2042,7 @@ mot_status mot_paged_free(mot_handle h, const mot_paged_cache* cache, const int3
   NvtxRange range("mot_paged_free");
   PagedCache c;
   mot_status r = paged_args(h, cache, c);
-  if (r != MOT_OK || (r = paged_slots(h, seqs, n)) != MOT_OK) return r;
+  if (r != MOT_OK || (r = paged_slots(h, c, seqs, n)) != MOT_OK) return r;
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   if (n == 0) return MOT_OK;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -2020,7 +2056,7 @@ mot_status mot_paged_compact(mot_handle h, const mot_paged_cache* cache, int32_t
   PagedCache c;
   mot_status r = paged_args(h, cache, c);
   if (r != MOT_OK) return r;
-  if (!aligned4(live)) return MOT_ERR_INVALID_ARG;
+  if (!aligned4(live) || (live && meets_cache(h, c, live, 4))) return MOT_ERR_INVALID_ARG;
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   MOT_CUDA_TRY(timed(h, "paged_compact_plan", st,
@@ -2055,7 +2091,7 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
   PagedCache c;
   PagedAppend p{};
   mot_status r = paged_args(h, cache, c);
-  if (r != MOT_OK || (r = paged_batch_args(h, batch, p.b)) != MOT_OK) return r;
+  if (r != MOT_OK || (r = paged_batch_args(h, c, batch, p.b)) != MOT_OK) return r;
   const PagedDims& d = h->pd;
   if (layer < 0 || layer >= d.L) return MOT_ERR_INVALID_ARG;
   if (!q || !k || !v || !q_out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
@@ -2071,8 +2107,11 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
   const size_t qb = span(q_stride, qw), kb = span(k_stride, kw), vb = span(v_stride, kw), ob = span(qw, qw);
   if ((overlap(q_out, ob, q, qb) && !(q_out == q && q_stride == qw)) || overlap(q_out, ob, k, kb) ||
       overlap(q_out, ob, v, vb) || meets_pools(h, c, q, qb) || meets_pools(h, c, k, kb) ||
-      meets_pools(h, c, v, vb) || meets_pools(h, c, q_out, ob))
+      meets_pools(h, c, v, vb) || meets_cache(h, c, q_out, ob) || meets_batch(p.b, q_out, ob))
     return MOT_ERR_INVALID_ARG;
+  for (const void* w : {q_norm, k_norm})
+    if (w && (overlap(q_out, ob, w, size_t(d.d) * es) || meets_pools(h, c, w, size_t(d.d) * es)))
+      return MOT_ERR_INVALID_ARG;
   p.layer = layer;
   p.q = q;
   p.k = k;
@@ -2096,11 +2135,11 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   PagedCache c;
   PagedAttnArgs a{};
   mot_status r = paged_args(h, cache, c);
-  if (r != MOT_OK || (r = paged_batch_args(h, batch, a.b)) != MOT_OK) return r;
+  if (r != MOT_OK || (r = paged_batch_args(h, c, batch, a.b)) != MOT_OK) return r;
   const PagedDims& d = h->pd;
   if (layer < 0 || layer >= d.L || !q || !out || !aligned16(q) || !aligned16(out)) return MOT_ERR_INVALID_ARG;
   const size_t qb = size_t(a.b.rows) * d.Hq * d.d * paged_es(d);
-  if (overlap(out, qb, q, qb) || meets_pools(h, c, out, qb)) return MOT_ERR_INVALID_ARG;
+  if (overlap(out, qb, q, qb) || meets_cache(h, c, out, qb) || meets_batch(a.b, out, qb)) return MOT_ERR_INVALID_ARG;
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   if (a.b.rows == 0 || a.b.n == 0) return MOT_OK;
   const size_t at = paged_layer_bytes(d) * size_t(layer);

@@ -247,3 +247,66 @@ def test_infinite_values_beside_keys_of_no_weight_at_all(new, dtype):
     # 12,000 equal weights: sums of n terms are off by n 2^-24 at most on either side
     P.assert_close(out[..., 20], torch.full((new, 4), 3.0, dtype=torch.float64, device="cuda"),
                    P.HALF[dtype] * 3 + 2 * n * 2.0 ** -24 * 3)
+
+
+def test_buffers_that_overlap_are_refused():
+    """What a call writes meets nothing else that it reads, and the cache's arrays do not meet: each pair,
+    by a tensor that holds both."""
+    n_pages, S, W, H, d = 24, 4, 6, 2, 64
+    ints = torch.zeros(4096, dtype=torch.int32, device="cuda")
+    table, lens, refs = ints[:S * W].view(S, W), ints[32:32 + S], ints[64:64 + n_pages]
+    table.fill_(-1)
+    pools = torch.zeros((2, 1, n_pages, H, 16, d), dtype=torch.bfloat16, device="cuda")
+    k, v = pools
+    cfg = M.make_paged_config(1, 4, H, d, 16, n_pages, S, W)
+    h = M.mot_create_paged(cfg)
+    seqs, starts = ints[128:130], ints[160:163]
+    seqs.copy_(i32([0, 1]))
+    starts.copy_(i32([0, 1, 2]))
+    c = M.paged_cache(k, v, table, lens, refs)
+    b = M.paged_batch(seqs, starts, 2, 2)
+    q, kn = torch.zeros((2, 4, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, H, d), dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(1024, dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(q)
+    before = ints.clone()
+
+    def refused(call):
+        with pytest.raises(M.MotError) as e:
+            call()
+        assert e.value.status == M.MOT_ERR_INVALID_ARG
+
+    # the cache's own arrays
+    for bad in (M.paged_cache(k, v, table, table.view(-1)[4:4 + S], refs), M.paged_cache(k, v, table, lens, ints[20:20 + n_pages]),
+                M.paged_cache(k, v, table, lens, ints[33:33 + n_pages]), M.paged_cache(k, k, table, lens, refs),
+                M.paged_cache(k, v, table, k.view(torch.int32).view(-1)[:S], refs)):
+        refused(lambda: M.mot_paged_reserve(h, bad, b))
+    # what a batch and a list of slots lie in
+    for x in (lens, table.view(-1), refs):
+        refused(lambda: M.mot_paged_reserve(h, c, M.paged_batch(x[:2], starts, 2, 2)))
+        refused(lambda: M.mot_paged_reserve(h, c, M.paged_batch(seqs, x[1:4], 2, 2)))
+        refused(lambda: M.mot_paged_free(h, c, x[:2], 2))
+        refused(lambda: M.mot_paged_fork(h, c, x[:1], seqs, 1))
+        refused(lambda: M.mot_paged_fork(h, c, seqs, x[:1], 1))
+        refused(lambda: M.mot_paged_compact(h, c, x[2:3]))
+    # outputs over the cache's arrays and the batch's (addresses: the tensors are of other types)
+    base = ints.data_ptr()
+    for at in (0, 128, 256, 512, 640):   # table, lens, refs, seqs, starts
+        refused(lambda: M.mot_paged_attention(h, 0, c, b, q, base + at))
+        refused(lambda: M.mot_paged_append(h, 0, c, b, q, kn, kn, base + at))
+    flat = torch.zeros((2, 1, 1, H, 16, d), dtype=torch.bfloat16, device="cuda")
+    for x in (ints[:1024].view(torch.bfloat16).view(1, 1, H, 16, d), pools[0, :, :1].view(1, 1, H, 16, d)):
+        refused(lambda: M.mot_paged_load(h, c, seqs[:1], 1, x, flat[0]))
+        refused(lambda: M.mot_paged_load(h, c, seqs[:1], 1, flat[0], x))
+    # norm weights under the output
+    refused(lambda: M.mot_paged_append(h, 0, c, b, q, kn, kn, w[:512].view(2, 4, d), q_norm=w[448:512]))
+    refused(lambda: M.mot_paged_append(h, 0, c, b, q, kn, kn, w[:512].view(2, 4, d), k_norm=w[:64]))
+    assert M.mot_get_device_status(h) == M.MOT_OK
+    assert torch.equal(ints, before)
+    # and none of it where they only stand side by side
+    M.mot_paged_reserve(h, c, b)
+    M.mot_paged_append(h, 0, c, b, q, kn, kn, w[:512].view(2, 4, d), q_norm=w[512:576], k_norm=w[576:640])
+    M.mot_paged_attention(h, 0, c, b, q, out)
+    M.mot_paged_load(h, c, seqs[:1], 1, flat[0], flat[1])
+    M.mot_paged_compact(h, c, ints[31:32])
+    assert M.mot_get_device_status(h) == M.MOT_OK
+    assert int(ints[31]) == 2
