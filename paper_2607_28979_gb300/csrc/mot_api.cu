@@ -1395,19 +1395,19 @@ mot_status mot_destroy(mot_handle h) {
 }
 
 mot_status mot_get_layer_map(mot_handle h, int32_t* out, int32_t n) {
-  if (!h || !out || n != h->d.L_t) return MOT_ERR_INVALID_ARG;
+  if (!h || h->kind == 4 || !out || n != h->d.L_t) return MOT_ERR_INVALID_ARG;
   for (int l = 0; l < n; ++l) out[l] = h->layer_map[l];
   return MOT_OK;
 }
 
 mot_status mot_get_path(mot_handle h, int32_t* path) {
-  if (!h || !path) return MOT_ERR_INVALID_ARG;
+  if (!h || h->kind == 4 || !path) return MOT_ERR_INVALID_ARG;
   *path = h->use_umma ? 1 : 0;
   return MOT_OK;
 }
 
 mot_status mot_set_schedule(mot_handle h, int32_t schedule) {
-  if (!h || schedule < 0 || schedule > 4) return MOT_ERR_INVALID_ARG;
+  if (!h || h->kind == 4 || schedule < 0 || schedule > 4) return MOT_ERR_INVALID_ARG;
   if (schedule == 3 && !(h->use_umma && onchip_supported(h->d))) return MOT_ERR_UNSUPPORTED;
   if (schedule == 4 && !(h->kind == 0 && h->use_umma && wide_supported(h->d)))
     return MOT_ERR_UNSUPPORTED;
@@ -1416,7 +1416,7 @@ mot_status mot_set_schedule(mot_handle h, int32_t schedule) {
 }
 
 mot_status mot_get_schedule(mot_handle h, int32_t* schedule) {
-  if (!h || !schedule) return MOT_ERR_INVALID_ARG;
+  if (!h || h->kind == 4 || !schedule) return MOT_ERR_INVALID_ARG;
   *schedule = h->schedule;
   return MOT_OK;
 }
@@ -1773,7 +1773,7 @@ mot_status mot_replay_attention(mot_handle h, int32_t layer, const void* q, cons
 }
 
 mot_status mot_set_routing(mot_handle h, int32_t routing) {
-  if (!h || routing < 0 || routing > 1) return MOT_ERR_INVALID_ARG;
+  if (!h || h->kind == 4 || routing < 0 || routing > 1) return MOT_ERR_INVALID_ARG;
   const bool bt_top1 = h->kind == 2 && h->bt && h->bt->d.top_k == 1;
   if (routing == 1 && !h->sparse_ok && !bt_top1) return MOT_ERR_UNSUPPORTED;
   h->routing = routing;
@@ -1781,7 +1781,7 @@ mot_status mot_set_routing(mot_handle h, int32_t routing) {
 }
 
 mot_status mot_get_routing(mot_handle h, int32_t* routing) {
-  if (!h || !routing) return MOT_ERR_INVALID_ARG;
+  if (!h || h->kind == 4 || !routing) return MOT_ERR_INVALID_ARG;
   *routing = h->routing;
   return MOT_OK;
 }
@@ -1800,7 +1800,7 @@ mot_status mot_get_expert_counts(mot_handle h, int32_t* counts, int32_t n, mot_s
     }
     return MOT_OK;
   }
-  if (!h || !counts || n != h->d.G * h->d.E) return MOT_ERR_INVALID_ARG;
+  if (!h || h->kind == 4 || !counts || n != h->d.G * h->d.E) return MOT_ERR_INVALID_ARG;
   if (!(h->sparse_ok && h->routing == 1 && h->counts_valid)) return MOT_ERR_UNSUPPORTED;
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

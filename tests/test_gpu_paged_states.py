@@ -310,3 +310,38 @@ def test_buffers_that_overlap_are_refused():
     M.mot_paged_compact(h, c, ints[31:32])
     assert M.mot_get_device_status(h) == M.MOT_OK
     assert int(ints[31]) == 2
+
+
+def test_a_paged_handle_takes_no_calls_of_other_kinds():
+    """Each call with arguments that are good for a handle of its own kind, or would pass as such."""
+    import ctypes
+    c = P.Cache()
+    L, h, n = M._lib, c.h.ptr, ctypes.c_int32(7)
+    x = torch.zeros(4096, dtype=torch.int32, device="cuda").data_ptr()
+    out = (ctypes.c_int32 * 4)()
+    bad = M.MOT_ERR_INVALID_ARG
+    assert L.mot_load_weights(h, x, 0) == bad
+    assert L.mot_translate(h, x, x, x, 0, x, x, None) == bad
+    assert L.mot_translate_host(h, x, x, x, 0, x, x, None) == bad
+    assert L.mot_translate_h(h, x, x, 0, x, x, None) == bad
+    assert L.mot_translate_bt(h, x, x, x, 0, x, x, None) == bad
+    assert L.mot_replay_attention(h, 0, x, x, x, x, x, 0, x, None) == bad
+    assert L.mot_replay_select(h, x, x, 0, x, None) == bad
+    assert L.mot_get_layer_map(h, out, 0) == bad
+    assert L.mot_get_path(h, ctypes.byref(n)) == bad
+    assert L.mot_set_schedule(h, 0) == bad and L.mot_get_schedule(h, ctypes.byref(n)) == bad
+    assert L.mot_set_routing(h, 0) == bad and L.mot_get_routing(h, ctypes.byref(n)) == bad
+    assert L.mot_get_expert_counts(h, out, 0, None) == bad
+    assert L.mot_debug_fixed_gate(h, None) == bad
+    assert n.value == 7
+    # and those that it does
+    count = ctypes.c_int64()
+    assert L.mot_get_launch_count(h, ctypes.byref(count)) == M.MOT_OK
+    assert L.mot_debug_set(h, 0, 0) == M.MOT_OK
+    assert L.mot_profile_enable(h, 1) == M.MOT_OK
+    c.reserve([0], [5])
+    stats = (M.mot_kernel_stat * 4)()
+    assert L.mot_profile_read(h, stats, 4, ctypes.byref(n)) == M.MOT_OK and n.value == 1
+    assert stats[0].name == b"paged_reserve" and stats[0].launches == 1
+    assert L.mot_profile_enable(h, 0) == M.MOT_OK
+    assert c.status() == M.MOT_OK
