@@ -53,3 +53,33 @@ def test_a_mean_of_equal_values_is_that_value(new, d, dtype):
     assert c.status() == M.MOT_OK
     want = values.double().expand(new, 4, d)
     P.assert_close(out, want, 0 * want if dtype == "bf16" else (2 * n + 16) * 2.0 ** -24 * want)
+
+
+@pytest.mark.parametrize("hq,h,d,new", [(8, 2, 64, 1), (8, 2, 64, 4), (14, 2, 64, 2), (7, 1, 128, 1), (16, 2, 128, 2), (3, 3, 128, 16)])
+def test_few_rows_hold_their_weights_to_17_bits(hq, h, d, new):
+    """Up to 16 rows per key/value head in bf16: the weights enter in two bf16 parts. The first is off by half a
+    step, 2^-8 of the weight's power of two; what is left lies a binade lower or is that tie, which is exact, so
+    the second is off by 2^-17. The result's own rounding and the 32-bit terms of the general bound are all
+    that comes on top. The oracle with the second part left out breaks this bound, so the test can tell."""
+    lens = [777, 130 + new, 61 + new]
+    c = P.Cache(q_heads=hq, kv_heads=h, d=d, page=32, n_pages=40, max_seqs=3, max_pages=25, seed=hq + new)
+    c.reserve([0, 1, 2], lens)
+    q = c.normal(3 * new, hq, d)
+    out = torch.zeros_like(q)
+    M.mot_paged_attention(c.h, 0, c.c, c.batch([0, 1, 2], [new] * 3), q, out)
+    assert c.status() == M.MOT_OK
+    told = 0
+    for i, n in enumerate(lens):
+        K, V = c.rows(i)
+        rows = slice(i * new, (i + 1) * new)
+        ref, absv, slop = P.attention(q[rows], K, V)
+        tol = 2.0 ** -8 * ref.abs() + 2.0 ** -17 * absv + slop
+        P.assert_close(out[rows], ref, tol, f"slot {i}")
+        for r in range(new):   # the mistake, in the oracle
+            p = n - new + r + 1
+            Kr, Vr = (x[:, :p].repeat_interleave(hq // h, 0) for x in (K, V))
+            s = torch.einsum("hd,hnd->hn", q[i * new + r].double(), Kr) / math.sqrt(d)
+            w = torch.exp(s - s.amax(1, keepdim=True))
+            one = torch.einsum("hn,hnd->hd", w.to(torch.bfloat16).double(), Vr) / w.sum(1, keepdim=True)
+            told += int(((one.to(torch.bfloat16).double() - ref[r]).abs() > tol[r]).sum())
+    assert told > 0.02 * out.numel(), told
