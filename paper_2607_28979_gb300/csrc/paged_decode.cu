@@ -27,7 +27,12 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kDecThreads = 32 * kWarps;
 constexpr int kDecTK = 16 * kWarps;
-constexpr int kLeast = 2, kMost = 8;   // units of a share (a join costs about as much as four)
+// Units of a share. A join costs about as much as four tiles: one token on 517 positions, 12 heads of 128 on 2,
+// takes 10.3 us in a graph with two tiles at least, 12.0 with one and 11.9 with four; on 8,000 14.4, 18.2 and
+// 15.4 (on 64 positions one tile is better, 6.1 for 6.7). Pieces against runs (kMost = 0): 10.3 for 12.4 on 517
+// positions, 14.4 for 16.4 on 8,000, 12.3 for 13.8 for 16 tokens of 12 heads of 64 on 500 each. Longer pieces
+// leave CTAs without work: with 16, those 16 on 2,000 positions take 25.5 for 23.7.
+constexpr int kLeast = 2, kMost = 8;
 
 // 16 bytes that are read once
 __device__ __forceinline__ uint4 ld_stream(const void* p) {

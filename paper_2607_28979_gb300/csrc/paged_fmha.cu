@@ -40,7 +40,13 @@
 namespace mot {
 namespace {
 
-constexpr int kLeast = 1, kMost = 16;   // units of a share (a piece's start, end and join cost about as much as eight)
+// Units of a share. A piece's start, end and join cost about as much as eight tiles, and a run often has two of
+// them. Pieces against runs (kMost = 0), us in a graph: 256 new tokens of 12 heads of 128 on 2, on 4,096 and
+// 16,384 positions, 41 for 59 and 55 for 67; 1,024 from nothing, 12 heads of 64, 22 for 29. Longer pieces leave
+// CTAs without work: with 32, 200 tokens of each of six on 3,584 positions take 56 for 42 (with 16, on 2,048, 39
+// for 33: the price of 39 for 51 where 30 chunks of 40 have 60 items). kLeast = 4 gains where an item has few
+// tiles (64 tokens on 2,000 positions, 29 for 35) and loses where it has many rows (1,024 from nothing, 23 for 22).
+constexpr int kLeast = 1, kMost = 16;
 
 template <int D>
 struct Pf {
