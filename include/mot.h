@@ -233,7 +233,8 @@ mot_status mot_profile_read(mot_handle h, mot_kernel_stat* out, int32_t cap, int
 /*
  * Failure-detection test hook. Every device pipeline wait of this handle's
  * kernels gives up after `wait_limit_cycles` SM cycles (0 = the default, about
- * two seconds), sets MOT_ERR_TIMEOUT in the status word and unwinds (copies
+ * two seconds; a limit below 2,000,000, about a millisecond, counts as that:
+ * copies in flight get no longer to end), sets MOT_ERR_TIMEOUT in the status word and unwinds (copies
  * and MMAs in flight are drained, TMEM is freed). With stall_test = 1, the
  * first CTA of the single-SM GEMM1 kernel (schedule 0) never fills its first
  * pipeline stage, so a wait on it runs out: translations then report

@@ -1421,10 +1421,13 @@ mot_status mot_get_schedule(mot_handle h, int32_t* schedule) {
   return MOT_OK;
 }
 
+static constexpr int64_t kLeastWait = 2000000;   // SM cycles, about a millisecond
+
 mot_status mot_debug_set(mot_handle h, int32_t stall_test, int64_t wait_limit_cycles) {
   if (!h || stall_test < 0 || stall_test > 1 || wait_limit_cycles < 0) return MOT_ERR_INVALID_ARG;
   h->stall_test = stall_test;
-  h->wait_limit = wait_limit_cycles > 0 ? wait_limit_cycles : 4000000000LL;
+  // the drains behind a timeout have the same bound, and no copy may outlive its kernel
+  h->wait_limit = wait_limit_cycles > 0 ? std::max<int64_t>(wait_limit_cycles, kLeastWait) : 4000000000LL;
   return MOT_OK;
 }
 

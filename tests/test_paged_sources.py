@@ -70,3 +70,11 @@ def test_the_status_word_is_cleared_before_its_reader_returns():
     changed = [m.end() for m in re.finditer(r"Async\(h->status", body)]
     assert changed and "cudaStreamSynchronize(st)" in body[changed[-1]:body.index("return MOT_ERR_TIMEOUT")]
     assert body.index("cudaSetDevice(h->device)") < body.index("Async(")
+
+
+def test_a_short_wait_limit_leaves_time_for_copies_in_flight():
+    """The limit of the waits bounds what drains copies and products behind a timeout too: a limit of a few
+    cycles would let a CTA leave, and the next one start in its shared memory, with copies still to land."""
+    body = _body(_source("mot_api.cu"), "mot_debug_set")
+    least = int(re.search(r"kLeastWait = (\d+);", _source("mot_api.cu")).group(1))
+    assert "std::max<int64_t>(wait_limit_cycles, kLeastWait)" in body and least >= 1_000_000
