@@ -209,7 +209,8 @@ __device__ __forceinline__ void copy_vecs(uint4* __restrict__ dst, const uint4* 
 __device__ __forceinline__ int elem_bytes(const PagedDims& d) { return d.dtype ? 4 : 2; }
 
 // Block (x, i): fork i's table row (its x-th share) and its copied page, the filled rows of the
-// heads and layers x, x + gridDim.x, ..
+// heads and layers x, x + gridDim.x, .. 16 branches of two prefixes, 44 MB of copies, 19 us with the plan
+// and the free before it (latency of three launches and of pieces of 16 KB).
 __global__ void __launch_bounds__(kCopyThreads)
     paged_fork_kernel(const PagedDims d, const PagedCache c, const int32_t* src, const int32_t* dst, int n,
                       const PagedWork w) {
@@ -324,7 +325,8 @@ __global__ void __launch_bounds__(kCopyThreads)
   }
 }
 
-// Item (layer, entry, page): its heads' rows between the pool and the contiguous caches.
+// Item (layer, entry, page): its heads' rows between the pool and the contiguous caches. 8,192 positions of 28
+// layers of 4 heads of 128: 153 us either way (6.1 TB/s read and written).
 __global__ void __launch_bounds__(kCopyThreads)
     paged_copy_kernel(const PagedDims d, const PagedCache c, const PagedCopy p, const PagedWork w) {
   if (p.store && refused(w.status)) return;
@@ -383,7 +385,8 @@ __global__ void __launch_bounds__(kCopyThreads)
 // but the norm's sum), 8 in a row otherwise. A lane's angles and norm weights are the same for every
 // head; fp32 in packed pairs. Angles: F_i = base^(-2 i / rot) / (2 pi) turns per position as a 64-bit
 // fraction, so the upper half of pos * F_i mod 2^64 is the angle in 2^-32 turns (1.5e-9), for any
-// position below 2^30.
+// position below 2^30. 10,254 rows of 36 heads of 128, normed and rotated, 39.4 us (4.8 TB/s; bound by
+// loads that stand still while a warp works), in fp32 73.5 (5.1 TB/s); one row 4.4.
 constexpr int kAppendThreads = 128;
 constexpr int kAppendDepth = 4;   // steps with their loads in flight
 

@@ -16,9 +16,11 @@
 //                         second product as two bf16 parts (2^-17): it has the tensor pipe to itself,
 //                         and the result is that of 32-bit weights. Per warp a running maximum and
 //                         sum; the four warps meet at the end of a piece. Measured, 28 heads on 4:
-//                         64 sequences of 16,384 positions 6.0 TB/s, of 100 to 16,384 5.2; two blocks
-//                         ahead instead of one: 73 us for 77 with two contexts
-//                         of 131,072 and 70,001, but 85 for 82 with the 64.
+//                         64 sequences of 16,384 positions 321 us (6.7 TB/s), of 100 to 16,384 5.2 TB/s;
+//                         two blocks ahead instead of one, in as many warps as hold them: 72.5 us for
+//                         74.5 with two contexts of 131,072 and 70,001, but 85 for 79 with the 64. One
+//                         token on 517 positions: the work dealt out after 3.6 us, the pieces done after
+//                         7.9, joined after 11.0.
 #include "paged_common.cuh"
 
 namespace mot {
@@ -53,8 +55,8 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
 
-// CTAs per SM: as many as have their registers without spilling (16 warps of D = 128 that spill: 91 us
-// for two contexts of 131,072 and 70,001, 12 that do not: 78).
+// CTAs per SM: as many as have their registers without spilling (16 warps of D = 128 that spill: 84 us
+// for two contexts of 131,072 and 70,001, 12 that do not: 76).
 template <int D, int NT>
 constexpr int kResident = (D == 64 ? 5 : 4) - NT;
 

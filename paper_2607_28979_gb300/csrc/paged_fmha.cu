@@ -8,8 +8,8 @@
 //                                    lane per (page, 64 dimensions), into rings of 2 and 3 tiles;
 //                         warp 1     S_i = Q_i K^T (Q_i and K from shared memory) and O_i += P_i V (P_i
 //                                    from TMEM, over S_i; V's rows are keys, so it is an MN-major
-//                                    operand and needs no transpose), i = 0, 1 in turn. One thread: an
-//                                    election and a warp barrier at each step cost 9% of the whole;
+//                                    operand and needs no transpose), i = 0, 1 in turn, by one thread
+//                                    without an election at each step;
 //                         warp 2     values before the second product: rows behind the sequence's
 //                                    end become zeros, and in tiles that some rows see only in part
 //                                    infinite and NaN values do too (a masked key's weight is 0, and 0
@@ -27,12 +27,11 @@
 //                                    to the piece's partial results.
 //                       What bounds it: S_i cannot be made again before P_i V is done (P_i lies over it),
 //                       so a stream is a chain of two products, the softmax and the commits and wake-ups
-//                       between them; two streams in turn keep the tensor cores 60% busy. Slower were, each
-//                       against the kernel of its day (4,096 tokens on 32,768 positions): two buffers of
-//                       64 keys per stream instead of one of 128 (1,402 us for 1,214: twice the steps),
-//                       two softmax threads per row (1,243 for 1,219), an issuing warp per stream (1,620
-//                       for 1,452), P in three quarters and one or as a whole (1,163 and 1,200 for 1,141).
-//                       The waits poll without a sleep: a sleeping thread wakes up to a microsecond late.
+//                       between them; two streams in turn keep the tensor cores 54% busy (4,096 tokens of
+//                       28 heads on 4 on 32,768 positions: 1,191 to 1,218 us, 1,500 TFLOP/s). Slower there:
+//                       two buffers of 64 keys per stream instead of one of 128 (1,385 us: twice the
+//                       steps), P as a whole (1,223); P in three quarters and one, or one and three, the
+//                       same. The waits poll without a sleep.
 //                       Every wait is bounded; on a timeout the roles unwind, copies and MMAs in flight
 //                       are drained, TMEM is freed and kStatusTimeout is raised.
 #include "paged_common.cuh"
@@ -221,7 +220,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
   uint32_t k_issued = 0, k_par = 0, v_issued = 0, v_par = 0;
 
   if (warp < 4) {
-    // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; at 168 the softmax spilled (1,196 -> 1,137 us for
+    // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; at 168 the softmax spills (1,258 us for 1,205 for
     // 4,096 tokens on 32,768 positions)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 0) {
