@@ -3,8 +3,6 @@ whole CTA has to take alike, and the order of its writes to shared memory."""
 import os
 import re
 
-import pytest
-
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_28979_gb300", "csrc")
 
 
