@@ -603,6 +603,29 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
                             mot_stream_t stream);
 
 /*
+ * Rotation by several positions, of a prompt that holds images or video: a row has
+ * `axes` of them (1 to 4; time, height and width, say), and pair i (i < rot_dim / 2,
+ * paired as rot_pairs says) turns by the one of axis[i], times rates[i] radians
+ * (finite, at most 2^16 either way; NULL: rot_base^(-2 i / rot_dim), as ever). axis
+ * and rates are host arrays [rot_dim / 2], taken over; any assignment of pairs to
+ * axes may be given, and a later call replaces it for the appends behind it.
+ * MOT_ERR_UNSUPPORTED for a handle with rot_dim 0.
+ *
+ * mot_paged_append_at is mot_paged_append with positions int32 [axes][rows] (device;
+ * any values, negative ones too) in the place of the rows' places in their
+ * sequences, for the rotation alone: where keys and values go, and what attention
+ * sees, stays with the sequence. One position for all axes gives what
+ * mot_paged_append gives for that position. MOT_ERR_INVALID_ARG before
+ * mot_paged_set_axes.
+ */
+mot_status mot_paged_set_axes(mot_handle h, int32_t axes, const int32_t* axis, const double* rates);
+mot_status mot_paged_append_at(mot_handle h, int32_t layer, const mot_paged_cache* cache,
+                               const mot_paged_batch* batch, const int32_t* positions,
+                               const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const void* q_norm,
+                               const void* k_norm, void* q_out, mot_stream_t stream);
+
+/*
  * Attention of the batch's rows over one layer's pages: row r at position p of
  * its sequence and query head h (key / value head h / (q_heads / kv_heads))
  *   o = softmax over j <= p of q . k_j / sqrt(head_dim), applied to v_j

@@ -175,6 +175,9 @@ struct mot_ctx {
   PagedDims pd{};
   PagedWork pw{};
   uint64_t* pfreq = nullptr;   // [rot_dim / 2] turns per position, in units of 2^-64
+  PagedAxes paxes{};           // each pair's axis and turn, where n_axes > 0
+  int32_t n_axes = 0;
+  double prot_base = 0;
   float* ppart = nullptr;      // partial results of the attention's split items
   int32_t* pcount = nullptr;   // its arrival counters, zero between calls
   int32_t pages_cause = 0;     // what the last read of the status word found
@@ -1841,6 +1844,13 @@ mot_status mot_expert_usage(const int32_t* counts, int32_t n, double* cv2, doubl
 
 // ---------------------------------------------------------------- paged cache
 
+// An angle in radians as a fraction of a turn, in units of 2^-64 (whole turns fall away).
+static uint64_t turn_of(long double radians) {
+  const long double turns = radians / 6.283185307179586476925286766559005768L;
+  const long double part = std::ldexp(turns - std::floor(turns), 64) + 0.5L;
+  return part >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(part);
+}
+
 mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
   if (!out) return MOT_ERR_INVALID_ARG;
   *out = nullptr;
@@ -1860,6 +1870,7 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
   mot_ctx* h = new (std::nothrow) mot_ctx();
   if (!h) return MOT_ERR_OOM;
   h->kind = 4;
+  h->prot_base = c.rot_base;
   PagedDims& d = h->pd;
   d = PagedDims{c.n_layers, c.q_heads, c.kv_heads, c.head_dim, c.page, 0, c.n_pages, c.max_seqs, c.max_pages,
                 c.rot_dim, c.rot_pairs, c.norm_eps, c.dtype == MOT_BF16 ? 0 : 1};
@@ -1877,13 +1888,9 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
     delete h;
     return MOT_ERR_UNSUPPORTED;
   }
-  // pair i turns by base^(-2 i / rot) / (2 pi) of a turn per position
-  uint64_t freq[64] = {};
-  for (int i = 0; i < d.rot / 2; ++i) {
-    const long double turns = std::pow(static_cast<long double>(c.rot_base), -2.0L * i / d.rot) /
-                              6.283185307179586476925286766559005768L;
-    freq[i] = static_cast<uint64_t>(std::ldexp(turns, 64) + 0.5L);   // at most 1 / (2 pi) of 2^64
-  }
+  // pair i turns by base^(-2 i / rot) per position
+  uint64_t (&freq)[64] = h->paxes.freq;
+  for (int i = 0; i < d.rot / 2; ++i) freq[i] = turn_of(std::pow(static_cast<long double>(c.rot_base), -2.0L * i / d.rot));
   const size_t pages = d.n_pages, counters = size_t(paged_counters(h->num_sms)) * 4;
   if (cudaMalloc(&h->pw.first, (size_t(d.max_seqs) + 1) * 4) != cudaSuccess ||
       cudaMalloc(&h->pw.take, pages * 4) != cudaSuccess || cudaMalloc(&h->pw.map, pages * 4) != cudaSuccess ||
@@ -2086,11 +2093,15 @@ mot_status mot_paged_load(mot_handle h, const mot_paged_cache* cache, int32_t fi
   return paged_copy(h, cache, p, reinterpret_cast<cudaStream_t>(stream));
 }
 
-mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cache,
-                            const mot_paged_batch* batch, const void* q, int64_t q_stride, const void* k,
-                            int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm,
-                            const void* k_norm, void* q_out, mot_stream_t stream) {
-  NvtxRange range("mot_paged_append");
+}  // extern "C"
+
+namespace {
+
+// at: [n_axes][rows] positions; null: a row's place in its sequence.
+mot_status paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cache, const mot_paged_batch* batch,
+                        const int32_t* at, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, void* q_out,
+                        mot_stream_t stream) {
   PagedCache c;
   PagedAppend p{};
   mot_status r = paged_args(h, cache, c);
@@ -2115,6 +2126,10 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
   for (const void* w : {q_norm, k_norm})
     if (w && (overlap(q_out, ob, w, size_t(d.d) * es) || meets_pools(h, c, w, size_t(d.d) * es)))
       return MOT_ERR_INVALID_ARG;
+  const size_t ab = size_t(h->n_axes) * p.b.rows * 4;
+  if (at && (overlap(q_out, ob, at, ab) || meets_pools(h, c, at, ab))) return MOT_ERR_INVALID_ARG;
+  PagedAxes ax = h->paxes;
+  ax.at = at;
   p.layer = layer;
   p.q = q;
   p.k = k;
@@ -2128,8 +2143,46 @@ mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* 
   p.q_out = q_out;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   MOT_CUDA_TRY(timed(h, "paged_append", st,
-                     [&] { return launch_paged_append(d, c, p, h->pw, h->num_sms, st); }));
+                     [&] { return launch_paged_append(d, c, p, h->pw, ax, h->num_sms, st); }));
   return MOT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+mot_status mot_paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cache,
+                            const mot_paged_batch* batch, const void* q, int64_t q_stride, const void* k,
+                            int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm,
+                            const void* k_norm, void* q_out, mot_stream_t stream) {
+  NvtxRange range("mot_paged_append");
+  return paged_append(h, layer, cache, batch, nullptr, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, q_out,
+                      stream);
+}
+
+mot_status mot_paged_set_axes(mot_handle h, int32_t axes, const int32_t* axis, const double* rates) {
+  if (!h || h->kind != 4 || axes < 1 || axes > kPagedMaxAxes || !axis) return MOT_ERR_INVALID_ARG;
+  const int pairs = h->pd.rot / 2;
+  if (pairs == 0) return MOT_ERR_UNSUPPORTED;
+  for (int i = 0; i < pairs; ++i)
+    if (axis[i] < 0 || axis[i] >= axes || (rates && !(std::fabs(rates[i]) <= 65536.0))) return MOT_ERR_INVALID_ARG;
+  for (int i = 0; i < pairs; ++i) {
+    h->paxes.axis[i] = static_cast<uint8_t>(axis[i]);
+    h->paxes.freq[i] = turn_of(rates ? static_cast<long double>(rates[i])
+                                     : std::pow(static_cast<long double>(h->prot_base), -2.0L * i / h->pd.rot));
+  }
+  h->n_axes = axes;
+  return MOT_OK;
+}
+
+mot_status mot_paged_append_at(mot_handle h, int32_t layer, const mot_paged_cache* cache, const mot_paged_batch* batch,
+                               const int32_t* positions, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm,
+                               const void* k_norm, void* q_out, mot_stream_t stream) {
+  NvtxRange range("mot_paged_append_at");
+  if (!h || h->kind != 4 || h->n_axes == 0 || !positions || !aligned4(positions)) return MOT_ERR_INVALID_ARG;
+  return paged_append(h, layer, cache, batch, positions, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, q_out,
+                      stream);
 }
 
 mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cache* cache,

@@ -1,5 +1,5 @@
-// The pages of a paged cache on sm_103a: reserve, fork, free, compact, the copies between pages and
-// contiguous caches, and the append of new keys and values.
+// The pages of a paged cache on sm_103a: reserve, fork, free, compact, and the copies between pages and
+// contiguous caches.
 //
 // The bookkeeping (table, lens, refs) lives on the device and is changed there, so that a step of a
 // serving loop needs no host round trip. A page is in use while refs > 0; what is taken are always
@@ -15,10 +15,6 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kPerThread = 8;     // pages of a thread in one step of a scan over refs
 constexpr int kCopyThreads = 256;
-
-__device__ __forceinline__ bool refused(const int32_t* status) {
-  return (*reinterpret_cast<const volatile int32_t*>(status) & kStatusPages) != 0;
-}
 
 // Marks slot s of the batch; false where it is outside the table or marked already.
 __device__ __forceinline__ bool mark_slot(uint32_t* marks, int s, int max_seqs) {
@@ -377,257 +373,6 @@ __global__ void __launch_bounds__(kCopyThreads)
   }
 }
 
-// ---------------------------------------------------------------- append
-//
-// A warp takes some rows, one after another, in steps of 2 or 4 heads (queries, then keys with their
-// values): d / 8 lanes per head with 8 elements each, in two groups of four: i .. i + 3 and i + rot / 2
-// .. in the half-and-half layout of the rotation, so that a pair's elements are in one lane (no shuffles
-// but the norm's sum), 8 in a row otherwise. A lane's angles and norm weights are the same for every
-// head; fp32 in packed pairs. Angles: F_i = base^(-2 i / rot) / (2 pi) turns per position as a 64-bit
-// fraction, so the upper half of pos * F_i mod 2^64 is the angle in 2^-32 turns (1.5e-9), for any
-// position below 2^30. 10,254 rows of 36 heads of 128, normed and rotated, 39.4 us (4.8 TB/s; bound by
-// loads that stand still while a warp works), in fp32 73.5 (5.1 TB/s); one row 4.4.
-constexpr int kAppendThreads = 128;
-constexpr int kAppendDepth = 4;   // steps with their loads in flight
-
-template <class T>
-struct Four;   // four elements, as two pairs of fp32
-template <>
-struct Four<uint16_t> {
-  uint2 u;
-  __device__ __forceinline__ void unpack(uint64_t (&x)[2]) const {
-    x[0] = (uint64_t(u.x & 0xFFFF0000u) << 32) | (u.x << 16);
-    x[1] = (uint64_t(u.y & 0xFFFF0000u) << 32) | (u.y << 16);
-  }
-  __device__ __forceinline__ void pack(const uint64_t (&x)[2]) {
-    __nv_bfloat162 a = __floats2bfloat162_rn(lo_f(x[0]), hi_f(x[0])), b = __floats2bfloat162_rn(lo_f(x[1]), hi_f(x[1]));
-    u = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
-  }
-  static __device__ __forceinline__ float lo_f(uint64_t x) { return __uint_as_float(uint32_t(x)); }
-  static __device__ __forceinline__ float hi_f(uint64_t x) { return __uint_as_float(uint32_t(x >> 32)); }
-};
-template <>
-struct Four<float> {
-  uint4 u;
-  __device__ __forceinline__ void unpack(uint64_t (&x)[2]) const {
-    x[0] = (uint64_t(u.y) << 32) | u.x;
-    x[1] = (uint64_t(u.w) << 32) | u.z;
-  }
-  __device__ __forceinline__ void pack(const uint64_t (&x)[2]) {
-    u = make_uint4(uint32_t(x[0]), uint32_t(x[0] >> 32), uint32_t(x[1]), uint32_t(x[1] >> 32));
-  }
-};
-
-// The last entry i with starts[i] <= row, by a 32-way search of one warp.
-__device__ __forceinline__ int entry_of(const int32_t* starts, int n, int row) {
-  const int lane = threadIdx.x & 31;
-  int lo = 0, cnt = n;   // the entry is in [lo, lo + cnt)
-  while (cnt > 1) {
-    const int step = (cnt + 31) / 32;
-    const int i = lo + lane * step;
-    const uint32_t le = __ballot_sync(0xffffffffu, lane * step < cnt && (lane == 0 || starts[i] <= row));
-    const int k = 31 - __clz(le);   // lane 0 is always set
-    lo += k * step;
-    cnt = min(step, cnt - k * step);
-  }
-  return lo;
-}
-
-enum { kRotNone = 0, kRotHalves = 1, kRotPairs = 2 };
-
-// cos and sin of t / 2^32 turns: the nearest quarter turn off, then their series to x^10 and x^9 (off by
-// 2^-29 at most on |x| <= pi / 4).
-__device__ __forceinline__ float2 cos_sin_turns(uint32_t t) {
-  const uint32_t quarter = (t + 0x20000000u) >> 30;
-  const float x = float(int32_t(t - (quarter << 30))) * 1.46291807926715968e-9f;   // 2 pi / 2^32
-  const float z = x * x;
-  const float sn = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), x);
-  const float cn =
-      fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800, 1.f / 40320), -1.f / 720), 1.f / 24), -0.5f), 1.f);
-  const float c = quarter & 1u ? sn : cn, s = quarter & 1u ? cn : sn;
-  return make_float2((quarter + 1u) & 2u ? -c : c, quarter & 2u ? -s : s);
-}
-
-template <class T, int D, int ROT>
-__global__ void __launch_bounds__(kAppendThreads, 6)
-    paged_append_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w, int rows_each,
-                        int parts) {
-  using F = Four<T>;
-  constexpr int kLph = D / 8, kAtOnce = 32 / kLph, kStep = kAtOnce * D;   // lanes per head; heads and elements of a step
-  __shared__ __align__(16) float2 cs[kAppendThreads / 32][D / 2];        // cos, sin of a row's angles
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (refused(w.status)) return;
-  const int sub = lane / kLph, el = lane % kLph;           // this lane's head and place in it
-  const int half = d.rot >> 1;
-  const bool turned = ROT != kRotNone && 8 * el < d.rot;   // the lane's elements are rotated
-  const bool halves = ROT == kRotHalves && turned;
-  const int eA = halves ? 4 * el : 8 * el, eB = halves ? half + 4 * el : 8 * el + 4;
-  uint64_t wq[4], wk[4];
-  auto weights = [&](const void* src, uint64_t (&x)[4]) {
-    if (!src) return;
-    uint64_t a[2], b[2];
-    reinterpret_cast<const F*>(static_cast<const T*>(src) + eA)->unpack(a);
-    reinterpret_cast<const F*>(static_cast<const T*>(src) + eB)->unpack(b);
-    x[0] = a[0];
-    x[1] = a[1];
-    x[2] = b[0];
-    x[3] = b[1];
-  };
-  weights(p.q_norm, wq);
-  weights(p.k_norm, wk);
-  // steps 0 .. sq - 1: queries, .. sq + sk - 1: a step of keys and one of values; this warp's: [s0, s1)
-  const int sq = (d.Hq + kAtOnce - 1) / kAtOnce, sk = (d.H + kAtOnce - 1) / kAtOnce, steps = sq + sk;
-  const int unit = blockIdx.x * (kAppendThreads / 32) + warp, part = unit % parts;
-  const int per = (steps + parts - 1) / parts, s0 = part * per, s1 = min(steps, s0 + per);
-  const int row_begin = min(int64_t(unit / parts) * rows_each, int64_t(p.b.rows));
-  const int row_end = min(row_begin + rows_each, p.b.rows);
-  const int off = sub * D + eA, ab = eB - eA;              // the lane's first group in a step, and the second behind it
-  const int pool_step = (kAtOnce * D) << d.lp;             // from a step's rows of a page to the next's
-  int first = 0, last = 0, pos0 = 0;   // rows [first, last) are of one entry; row r's position is pos0 + r
-  int slot = -1, page = -1;
-  for (int row = row_begin; row < row_end; ++row) {
-    const T* q = static_cast<const T*>(p.q) + row * p.q_stride + off;
-    F a[kAppendDepth], b[kAppendDepth];
-    auto load_q = [&](int st) {
-#pragma unroll
-      for (int y = 0; y < kAppendDepth; ++y)
-        if (st + y < min(sq, s1) && (st + y) * kAtOnce + sub < d.Hq) {
-          a[y] = *reinterpret_cast<const F*>(q + (st + y) * kStep);
-          b[y] = *reinterpret_cast<const F*>(q + (st + y) * kStep + ab);
-        }
-    };
-    load_q(s0);   // under way while the row's place is found
-    const bool fresh = row < first || row >= last;
-    if (fresh) {
-      const int i = entry_of(p.b.starts, p.b.n, row);
-      const int from = p.b.starts[i], to = p.b.starts[i + 1];
-      first = row;
-      last = row + 1;
-      slot = -1;
-      if (row >= from && row < to) {
-        const PagedSeq s = paged_seq(d, p.b, c.lens, w.status, i);
-        if (row < s.r0 + s.m) last = s.r0 + s.m;   // starts that are out of order: this row alone
-        slot = s.slot;
-        pos0 = s.len - s.m - s.r0;
-      }
-    }
-    const int pos = slot < 0 ? -1 : pos0 + row;
-    if (pos < 0) {   // a row of no entry, or of one that is shorter than its rows
-      if (fresh && row >= p.b.starts[0] && row < p.b.starts[p.b.n] && lane == 0) atomicOr(w.status, kStatusPageUse);
-      continue;
-    }
-    if (fresh || (pos & (d.P - 1)) == 0) {
-      page = paged_entry(d, c.table, w.status, slot, pos);
-    }
-    uint64_t tc[2] = {}, ts[2] = {};   // cos and sin of the lane's four angles, in pairs
-    if (ROT != kRotNone) {
-#pragma unroll
-      for (int k = lane; k < D / 2; k += 32)
-        if (k < half) cs[warp][k] = cos_sin_turns(uint32_t(uint64_t(pos) * p.freq[k] >> 32));
-      __syncwarp();
-      if (turned) {
-        const float4 x = *reinterpret_cast<const float4*>(&cs[warp][4 * el]);
-        const float4 y = *reinterpret_cast<const float4*>(&cs[warp][4 * el + 2]);
-        tc[0] = f32x2(x.x, x.z);
-        tc[1] = f32x2(y.x, y.z);
-        ts[0] = f32x2(x.y, x.w);
-        ts[1] = f32x2(y.y, y.w);
-      }
-      __syncwarp();   // before the next row's
-    }
-    auto work = [&](F& fa, F& fb, bool norm, const uint64_t (&wt)[4]) {   // by the whole warp
-      uint64_t f[2], g[2];
-      fa.unpack(f);
-      fb.unpack(g);
-      if (norm) {
-        const uint64_t sq2 = ffma_x2(g[1], g[1], ffma_x2(g[0], g[0], ffma_x2(f[1], f[1], fmul_x2(f[0], f[0]))));
-        float ss = __uint_as_float(uint32_t(sq2)) + __uint_as_float(uint32_t(sq2 >> 32));
-#pragma unroll
-        for (int o = kLph / 2; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const float rs = rsqrtf(fmaf(ss, 1.f / D, d.eps));
-        const uint64_t r2 = f32x2(rs, rs);
-        f[0] = fmul_x2(fmul_x2(f[0], r2), wt[0]);
-        f[1] = fmul_x2(fmul_x2(f[1], r2), wt[1]);
-        g[0] = fmul_x2(fmul_x2(g[0], r2), wt[2]);
-        g[1] = fmul_x2(fmul_x2(g[1], r2), wt[3]);
-      }
-      if (halves) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint64_t u = f[e], v = g[e], ns = ts[e] ^ 0x8000000080000000ull;
-          f[e] = ffma_x2(v, ns, fmul_x2(u, tc[e]));
-          g[e] = ffma_x2(u, ts[e], fmul_x2(v, tc[e]));
-        }
-      } else if (ROT == kRotPairs && turned) {
-        // the pairs of angles 0, 1 are f's, those of 2, 3 g's: (x c - y s, y c + x s)
-        auto turn = [](uint64_t v, float cn, float sn) {
-          const float x = __uint_as_float(uint32_t(v)), y = __uint_as_float(uint32_t(v >> 32));
-          return f32x2(x * cn - y * sn, y * cn + x * sn);
-        };
-        auto lo = [](uint64_t v) { return __uint_as_float(uint32_t(v)); };
-        auto hi = [](uint64_t v) { return __uint_as_float(uint32_t(v >> 32)); };
-        f[0] = turn(f[0], lo(tc[0]), lo(ts[0]));
-        f[1] = turn(f[1], hi(tc[0]), hi(ts[0]));
-        g[0] = turn(g[0], lo(tc[1]), lo(ts[1]));
-        g[1] = turn(g[1], hi(tc[1]), hi(ts[1]));
-      }
-      fa.pack(f);
-      fb.pack(g);
-    };
-    T* q_out = static_cast<T*>(p.q_out) + int64_t(row) * d.Hq * D + off;
-    for (int sb = s0; sb < min(sq, s1); sb += kAppendDepth) {
-      if (sb != s0) load_q(sb);
-#pragma unroll
-      for (int y = 0; y < kAppendDepth; ++y) {
-        const int st = sb + y;
-        if (st >= min(sq, s1)) break;
-        if (ROT != kRotNone || p.q_norm) work(a[y], b[y], p.q_norm != nullptr, wq);
-        if (st * kAtOnce + sub < d.Hq) {
-          *reinterpret_cast<F*>(q_out + st * kStep) = a[y];
-          *reinterpret_cast<F*>(q_out + st * kStep + ab) = b[y];
-        }
-      }
-    }
-    if (s1 <= sq || page < 0) continue;
-    const int64_t pool = ((int64_t(p.layer) * d.n_pages + page) * d.H * d.P + (pos & (d.P - 1))) * D +
-                         (int64_t(sub * D) << d.lp) + eA;
-    const T* k = static_cast<const T*>(p.k) + row * p.k_stride + off;
-    const T* v = static_cast<const T*>(p.v) + row * p.v_stride + off;
-    T* k_out = static_cast<T*>(c.k) + pool;
-    T* v_out = static_cast<T*>(c.v) + pool;
-    constexpr int kPairs = kAppendDepth / 2;   // steps of keys and of values at a time
-    for (int sb = max(s0, sq) - sq; sb < s1 - sq; sb += kPairs) {
-#pragma unroll
-      for (int y = 0; y < kPairs; ++y)
-        if (sb + y < s1 - sq && (sb + y) * kAtOnce + sub < d.H) {
-          a[y] = *reinterpret_cast<const F*>(k + (sb + y) * kStep);
-          b[y] = *reinterpret_cast<const F*>(k + (sb + y) * kStep + ab);
-          a[kPairs + y] = *reinterpret_cast<const F*>(v + (sb + y) * kStep);
-          b[kPairs + y] = *reinterpret_cast<const F*>(v + (sb + y) * kStep + ab);
-        }
-#pragma unroll
-      for (int y = 0; y < kPairs; ++y) {
-        const int st = sb + y;
-        if (st >= s1 - sq) break;
-        if (ROT != kRotNone || p.k_norm) work(a[y], b[y], p.k_norm != nullptr, wk);
-        if (st * kAtOnce + sub < d.H) {
-          const int64_t at = int64_t(st) * pool_step;
-          *reinterpret_cast<F*>(k_out + at) = a[y];
-          *reinterpret_cast<F*>(k_out + at + ab) = b[y];
-          *reinterpret_cast<F*>(v_out + at) = a[kPairs + y];
-          *reinterpret_cast<F*>(v_out + at + ab) = b[kPairs + y];
-        }
-      }
-    }
-  }
-}
-
-template <class T, int D>
-auto append_kernel(const PagedDims& d) {
-  return d.rot == 0 ? paged_append_kernel<T, D, kRotNone>
-                    : d.rot_pairs ? paged_append_kernel<T, D, kRotPairs> : paged_append_kernel<T, D, kRotHalves>;
-}
-
 int grid_of(int64_t items, int num_sms, int per_sm) {
   const int64_t most = int64_t(num_sms) * per_sm;
   return int(items < 1 ? 1 : (items < most ? items : most));
@@ -667,21 +412,4 @@ cudaError_t launch_paged_copy(const PagedDims& d, const PagedCache& c, const Pag
   const int64_t items = int64_t((p.S - 1) / d.P + 1) * p.n * p.n_layers;
   return launch_kernel(false, paged_copy_kernel, grid_of(items, num_sms, 8), kCopyThreads, 0, st, d, c, p, w);
 }
-cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const PagedAppend& p,
-                                const PagedWork& w, int num_sms, cudaStream_t st) {
-  // few rows: a row's heads over several warps, all of their loads in flight; many: a warp takes a row, or
-  // some in a row, which share the search for their entry
-  constexpr int kWarps = kAppendThreads / 32;
-  const int at_once = 256 / d.d, steps = (d.Hq + at_once - 1) / at_once + (d.H + at_once - 1) / at_once;
-  const int64_t fill = int64_t(num_sms) * 24;   // warps that are resident
-  const int most = (steps + kAppendDepth - 1) / kAppendDepth;
-  const int parts = p.b.rows >= fill ? 1 : int(fill / p.b.rows < most ? fill / p.b.rows : most);
-  const int rows_each = int((p.b.rows * int64_t(parts) + fill - 1) / fill);
-  const int64_t units = (int64_t(p.b.rows) + rows_each - 1) / rows_each * parts;
-  const int grid = int((units + kWarps - 1) / kWarps);
-  auto kern = d.dtype == 0 ? (d.d == 64 ? append_kernel<uint16_t, 64>(d) : append_kernel<uint16_t, 128>(d))
-                           : (d.d == 64 ? append_kernel<float, 64>(d) : append_kernel<float, 128>(d));
-  return launch_kernel(false, kern, grid, kAppendThreads, 0, st, d, c, p, w, rows_each, parts);
-}
-
 }  // namespace mot

@@ -10,6 +10,11 @@
 namespace mot {
 namespace {
 
+// Whether a change was refused, and none behind it is made.
+__device__ __forceinline__ bool refused(const int32_t* status) {
+  return (*reinterpret_cast<const volatile int32_t*>(status) & kStatusPages) != 0;
+}
+
 // Sum of v over the CTA's threads before this one; `total` over all of them. `sh`: 33 words.
 template <class T>
 __device__ __forceinline__ T block_scan(T v, T* sh, T& total) {

@@ -1,5 +1,5 @@
-// Internal declarations of the paged cache (paged.cu: its pages and the append; paged_simt.cu, paged_decode.cu, paged_fmha.cu:
-// attention over it), shared with the C-ABI layer.
+// Internal declarations of the paged cache (paged.cu: its pages; paged_append.cu: the append; paged_simt.cu,
+// paged_decode.cu, paged_fmha.cu: attention over it), shared with the C-ABI layer.
 #pragma once
 
 #include "mot_internal.h"
@@ -79,8 +79,16 @@ struct PagedAppend {
   const uint64_t* freq;             // [rot / 2]: turns per position in units of 2^-64
   void* q_out;                      // [rows][Hq][d]
 };
-cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const PagedAppend& p,
-                                const PagedWork& w, int num_sms, cudaStream_t st);
+// Rotation by several positions: pair i of a row turns by at[axis[i]][row] times freq[i] 2^-64 turns. at null: by
+// the row's place in its sequence.
+constexpr int kPagedMaxAxes = 4;
+struct PagedAxes {
+  uint64_t freq[64];
+  uint8_t axis[64];
+  const int32_t* at;   // [axes][rows]
+};
+cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const PagedAppend& p, const PagedWork& w,
+                                const PagedAxes& ax, int num_sms, cudaStream_t st);
 
 // Attention of a batch's rows over one layer's pages. `part` holds the partial results of split
 // items, two per CTA; `count` one arrival counter per CTA, zero between calls.

@@ -139,6 +139,9 @@ _SIGS = {
     "mot_paged_load": [_H, _CACHE, _I, _I, _P, _I, _I, _I, _P, _P, _P],
     "mot_paged_append": [_H, _I, _CACHE, _BATCH, _P, ctypes.c_int64, _P, ctypes.c_int64, _P,
                          ctypes.c_int64, _P, _P, _P, _P],
+    "mot_paged_set_axes": [_H, _I, _P, _P],
+    "mot_paged_append_at": [_H, _I, _CACHE, _BATCH, _P, _P, ctypes.c_int64, _P, ctypes.c_int64, _P,
+                         ctypes.c_int64, _P, _P, _P, _P],
     "mot_paged_attention": [_H, _I, _CACHE, _BATCH, _P, _P, _P],
 }
 for _name, _args in _SIGS.items():
@@ -199,6 +202,7 @@ class Handle:
     """Owns one ``mot_handle``; destroyed with ``mot_destroy`` or on GC."""
 
     paged = None    # the config of a paged handle
+    axes = 0        # positions of a row, once its axes are set
     device = None   # its device, where torch had one when it was made
 
     def __init__(self, ptr: int, n_layers_tgt: int):
@@ -495,14 +499,11 @@ def _row_stride(x, what: str, least=None, where: str = "") -> int:
     raise ValueError(f"{what}: [rows][heads][head_dim] with contiguous rows is wanted")
 
 
-def mot_paged_append(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, k, v, q_out,
-                     q_norm=None, k_norm=None, stream=None) -> None:
-    """Tensors q, k, v [rows][heads][head_dim], whose rows may lie apart (columns of a fused
-    projection); q_out [rows][q_heads][head_dim] contiguous."""
-    where = "mot_paged_append"
+def _append(h: Handle, layer, cache, batch, q, k, v, q_out, q_norm, k_norm, stream, where, positions=()) -> None:
     c, dev = _fits(h, cache, where), h.device
     if c is None:
         strides = [_row_stride(x, what) for x, what in ((q, "q"), (k, "k"), (v, "v"))]
+        positions = [_addr(x) for x in positions]
     else:
         rows, kinds, hq, d = _batch_fits(h, batch, where), _FLOATS[c.dtype], c.q_heads, c.head_dim
         kv = (rows, c.kv_heads, d)
@@ -511,9 +512,38 @@ def mot_paged_append(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_p
             _typed(x, kinds, where, what, dev)
         q_out = _whole(q_out, kinds, rows * hq * d, where, "q_out", dev)
         q_norm, k_norm = _whole(q_norm, kinds, d, where, "q_norm", dev), _whole(k_norm, kinds, d, where, "k_norm", dev)
-    _check(_lib.mot_paged_append(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), _addr(q), strides[0],
-                                 _addr(k), strides[1], _addr(v), strides[2], _addr(q_norm), _addr(k_norm),
-                                 _addr(q_out), _stream(stream)), where)
+        for x in positions:
+            if hasattr(x, "shape") and x.shape[-1] != rows:
+                raise _bad(where, f"positions is {tuple(x.shape)}, {(h.axes, rows)} is wanted")
+        positions = [_whole(x, _INT32, h.axes * rows, where, "positions", dev) for x in positions]
+    _check(getattr(_lib, where)(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), *positions, _addr(q),
+                                strides[0], _addr(k), strides[1], _addr(v), strides[2], _addr(q_norm), _addr(k_norm),
+                                _addr(q_out), _stream(stream)), where)
+
+
+def mot_paged_append(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, k, v, q_out,
+                     q_norm=None, k_norm=None, stream=None) -> None:
+    """Tensors q, k, v [rows][heads][head_dim], whose rows may lie apart (columns of a fused
+    projection); q_out [rows][q_heads][head_dim] contiguous."""
+    _append(h, layer, cache, batch, q, k, v, q_out, q_norm, k_norm, stream, "mot_paged_append")
+
+
+def mot_paged_set_axes(h: Handle, axes: int, axis, rates=None) -> None:
+    """Pair i of a head turns by the position of axis ``axis[i]``, times ``rates[i]`` radians (None: the
+    config's base). Host sequences of rot_dim / 2 numbers."""
+    where = "mot_paged_set_axes"
+    pairs = len(axis) if h.paged is None else h.paged.rot_dim // 2
+    if len(axis) != pairs or (rates is not None and len(rates) != pairs):
+        raise _bad(where, f"{pairs} pairs are rotated")
+    _check(_lib.mot_paged_set_axes(h.ptr, int(axes), (ctypes.c_int32 * pairs)(*axis),
+                                   None if rates is None else (ctypes.c_double * pairs)(*rates)), where)
+    h.axes = int(axes)
+
+
+def mot_paged_append_at(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, positions, q, k, v, q_out,
+                        q_norm=None, k_norm=None, stream=None) -> None:
+    """mot_paged_append with an int32 tensor ``positions`` [axes][rows] that the rotation goes by."""
+    _append(h, layer, cache, batch, q, k, v, q_out, q_norm, k_norm, stream, "mot_paged_append_at", (positions,))
 
 
 def mot_paged_attention(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, out,
