@@ -512,6 +512,8 @@ typedef struct {
   int32_t* table;
   int32_t* lens;
   int32_t* refs;
+  float* k_scale;          /* 8-bit pages (mot_create_paged8), else not looked at */
+  float* v_scale;
 } mot_paged_cache;
 
 typedef struct {
@@ -523,6 +525,26 @@ typedef struct {
 } mot_paged_batch;
 
 mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out);
+
+/*
+ * A paged cache that is held in 8 bits, half the bytes that a decoding step reads:
+ *   pools  k, v   [n_layers][n_pages][kv_heads][P][head_dim], 8-bit floats (1 sign, 4
+ *                 exponent and 3 mantissa bits, largest 448, no infinities)
+ *   scales k_scale, v_scale  float [n_layers][n_pages][kv_heads], a power of two for
+ *                 each page and head, of the page's keys and of its values
+ * A value is its 8 bits times the scale. The calls write 2^e, the least e in -60 .. 60
+ * that brings the page's largest value to 448 or below, and round once, to the nearest
+ * (off by 2^-4 of the value at most; below 2^-6 of the scale the steps stay 2^-9 of it). Where rows join others in a page (mot_paged_append, a page that
+ * mot_paged_store fills in part) its scale never falls; where it rises, the rows that
+ * were there are rounded again. A page without rows before those has no scale to
+ * keep: the memory of the scales needs no initial value. A value that is not finite,
+ * or above 448 2^60, is held as NaN and has no part in a scale.
+ *
+ * A handle of mot_create_paged8 takes every call of a paged one, with queries, new
+ * keys and values, outputs and contiguous caches in bf16 (cfg.dtype; fp32:
+ * MOT_ERR_UNSUPPORTED); forks and compactions take the scales with their pages.
+ */
+mot_status mot_create_paged8(const mot_paged_config* cfg, mot_handle* out);
 
 /*
  * What the last mot_get_device_status of a paged handle found, both or either
@@ -571,7 +593,7 @@ mot_status mot_paged_compact(mot_handle h, const mot_paged_cache* cache, int32_t
  * layers first_layer .. first_layer + n_layers - 1: batch entry i < n <= batch
  * is slot seqs[i], positions 0 .. lens - 1 (at most max_seq). store writes
  * the pages (of sequences that hold them alone), load the contiguous cache;
- * other positions keep their contents.
+ * other positions keep their contents (in 8 bits: but for a scale that rises).
  */
 mot_status mot_paged_store(mot_handle h, const mot_paged_cache* cache, int32_t first_layer,
                            int32_t n_layers, const int32_t* seqs, int32_t n, int32_t batch,

@@ -1851,7 +1851,7 @@ static uint64_t turn_of(long double radians) {
   return part >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(part);
 }
 
-mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
+static mot_status create_paged(const mot_paged_config* cfg, bool b8, mot_handle* out) {
   if (!out) return MOT_ERR_INVALID_ARG;
   *out = nullptr;
   if (!cfg) return MOT_ERR_INVALID_ARG;
@@ -1865,7 +1865,8 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
     return MOT_ERR_INVALID_ARG;
   if ((c.head_dim != 64 && c.head_dim != 128) || c.page < 16 || c.page > 128 || (c.page & (c.page - 1)) ||
       c.q_heads / c.kv_heads > kPagedMaxGroup || c.max_seqs > kPagedMaxSeqs || c.rot_dim % 16 ||
-      c.n_layers > 65535 || c.q_heads > 65535 || int64_t(c.n_pages) * c.kv_heads * c.page > (1 << 30))
+      c.n_layers > 65535 || c.q_heads > 65535 || int64_t(c.n_pages) * c.kv_heads * c.page > (1 << 30) ||
+      (b8 && c.dtype != MOT_BF16))
     return MOT_ERR_UNSUPPORTED;
   mot_ctx* h = new (std::nothrow) mot_ctx();
   if (!h) return MOT_ERR_OOM;
@@ -1873,7 +1874,7 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
   h->prot_base = c.rot_base;
   PagedDims& d = h->pd;
   d = PagedDims{c.n_layers, c.q_heads, c.kv_heads, c.head_dim, c.page, 0, c.n_pages, c.max_seqs, c.max_pages,
-                c.rot_dim, c.rot_pairs, c.norm_eps, c.dtype == MOT_BF16 ? 0 : 1};
+                c.rot_dim, c.rot_pairs, c.norm_eps, c.dtype == MOT_BF16 ? 0 : 1, b8};
   while ((1 << d.lp) < d.P) ++d.lp;
   int cc_major = 0, cc_minor = 0;
   if (cudaGetDevice(&h->device) != cudaSuccess ||
@@ -1918,23 +1919,28 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) {
   return MOT_OK;
 }
 
+mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out) { return create_paged(cfg, false, out); }
+mot_status mot_create_paged8(const mot_paged_config* cfg, mot_handle* out) { return create_paged(cfg, true, out); }
+
 namespace {
 
-size_t paged_es(const PagedDims& d) { return d.dtype ? 4 : 2; }
-size_t paged_layer_bytes(const PagedDims& d) { return size_t(d.n_pages) * d.H * d.P * d.d * paged_es(d); }
+size_t paged_es(const PagedDims& d) { return d.dtype ? 4 : 2; }   // of what the calls take and give
+size_t paged_layer_bytes(const PagedDims& d) { return size_t(d.n_pages) * d.H * d.P * d.d * paged_elem(d); }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 struct PagedSpan {
   const void* p;
   size_t n;
 };
-void paged_spans(const PagedDims& d, const PagedCache& c, PagedSpan (&s)[5]) {
-  const size_t pool = paged_layer_bytes(d) * d.L;
+void paged_spans(const PagedDims& d, const PagedCache& c, PagedSpan (&s)[7]) {
+  const size_t pool = paged_layer_bytes(d) * d.L, scales = d.b8 ? size_t(d.L) * d.n_pages * d.H * 4 : 0;
   s[0] = {c.k, pool};
   s[1] = {c.v, pool};
   s[2] = {c.table, size_t(d.max_seqs) * d.max_pages * 4};
   s[3] = {c.lens, size_t(d.max_seqs) * 4};
   s[4] = {c.refs, size_t(d.n_pages) * 4};
+  s[5] = {c.ks, scales};
+  s[6] = {c.vs, scales};
 }
 
 mot_status paged_args(mot_handle h, const mot_paged_cache* c, PagedCache& pc) {
@@ -1942,22 +1948,29 @@ mot_status paged_args(mot_handle h, const mot_paged_cache* c, PagedCache& pc) {
   if (!c->k || !c->v || !c->table || !c->lens || !c->refs || !aligned16(c->k) || !aligned16(c->v) ||
       !aligned4(c->table) || !aligned4(c->lens) || !aligned4(c->refs))
     return MOT_ERR_INVALID_ARG;
-  pc = PagedCache{c->k, c->v, c->table, c->lens, c->refs};
-  PagedSpan s[5];
+  pc = PagedCache{c->k, c->v, c->table, c->lens, c->refs, nullptr, nullptr};
+  if (h->pd.b8) {   // else the scales are not looked at
+    if (!c->k_scale || !c->v_scale || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return MOT_ERR_INVALID_ARG;
+    pc.ks = c->k_scale;
+    pc.vs = c->v_scale;
+  }
+  PagedSpan s[7];
   paged_spans(h->pd, pc, s);
-  for (int i = 0; i < 5; ++i)
+  for (int i = 0; i < 7; ++i)
     for (int j = 0; j < i; ++j)
       if (overlap(s[i].p, s[i].n, s[j].p, s[j].n)) return MOT_ERR_INVALID_ARG;
   return MOT_OK;
 }
 
-// Whether [p, p + n) meets the pools, or any of the cache's arrays.
+// Whether [p, p + n) meets the pools (with their scales), or any of the cache's arrays.
 bool meets_pools(const mot_ctx* h, const PagedCache& c, const void* p, size_t n) {
-  const size_t bytes = paged_layer_bytes(h->pd) * h->pd.L;
-  return overlap(p, n, c.k, bytes) || overlap(p, n, c.v, bytes);
+  PagedSpan s[7];
+  paged_spans(h->pd, c, s);
+  return overlap(p, n, s[0].p, s[0].n) || overlap(p, n, s[1].p, s[1].n) || overlap(p, n, s[5].p, s[5].n) ||
+         overlap(p, n, s[6].p, s[6].n);
 }
 bool meets_cache(const mot_ctx* h, const PagedCache& c, const void* p, size_t n) {
-  PagedSpan s[5];
+  PagedSpan s[7];
   paged_spans(h->pd, c, s);
   for (const PagedSpan& x : s)
     if (overlap(p, n, x.p, x.n)) return true;
@@ -2006,7 +2019,7 @@ mot_status paged_copy(mot_handle h, const mot_paged_cache* cache, const PagedCop
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   if (p.n == 0) return MOT_OK;
   MOT_CUDA_TRY(timed(h, p.store ? "paged_store" : "paged_load", st,
-                     [&] { return launch_paged_copy(d, c, p, h->pw, h->num_sms, st); }));
+                     [&] { return (d.b8 ? launch_paged8_copy : launch_paged_copy)(d, c, p, h->pw, h->num_sms, st); }));
   return MOT_OK;
 }
 
@@ -2107,6 +2120,7 @@ mot_status paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cach
   mot_status r = paged_args(h, cache, c);
   if (r != MOT_OK || (r = paged_batch_args(h, c, batch, p.b)) != MOT_OK) return r;
   const PagedDims& d = h->pd;
+  if (d.b8) return MOT_ERR_UNSUPPORTED;
   if (layer < 0 || layer >= d.L) return MOT_ERR_INVALID_ARG;
   if (!q || !k || !v || !q_out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
       !aligned16(q_norm) || !aligned16(k_norm))
@@ -2193,6 +2207,7 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   mot_status r = paged_args(h, cache, c);
   if (r != MOT_OK || (r = paged_batch_args(h, c, batch, a.b)) != MOT_OK) return r;
   const PagedDims& d = h->pd;
+  if (d.b8) return MOT_ERR_UNSUPPORTED;
   if (layer < 0 || layer >= d.L || !q || !out || !aligned16(q) || !aligned16(out)) return MOT_ERR_INVALID_ARG;
   const size_t qb = size_t(a.b.rows) * d.Hq * d.d * paged_es(d);
   if (overlap(out, qb, q, qb) || meets_cache(h, c, out, qb) || meets_batch(a.b, out, qb)) return MOT_ERR_INVALID_ARG;

@@ -202,8 +202,6 @@ __device__ __forceinline__ void copy_vecs(uint4* __restrict__ dst, const uint4* 
   for (; v < n_vec; v += kCopyThreads) dst[v] = src[v];
 }
 
-__device__ __forceinline__ int elem_bytes(const PagedDims& d) { return d.dtype ? 4 : 2; }
-
 // Block (x, i): fork i's table row (its x-th share) and its copied page, the filled rows of the
 // heads and layers x, x + gridDim.x, .. 16 branches of two prefixes, 44 MB of copies, 19 us with the plan
 // and the free before it (latency of three launches and of pieces of 16 KB).
@@ -230,12 +228,16 @@ __global__ void __launch_bounds__(kCopyThreads)
   }
   if (blockIdx.x == 0 && tid == 0) c.lens[b] = len;
   if (!part || mv.x < 0) return;
-  const int es = elem_bytes(d), run = d.P * d.d * es / 16, n_vec = part * d.d * es / 16;
+  const int es = paged_elem(d), run = d.P * d.d * es / 16, n_vec = part * d.d * es / 16;
   for (int x = blockIdx.x; x < 2 * d.L * d.H; x += gridDim.x) {
     uint4* pool = static_cast<uint4*>(x & 1 ? c.v : c.k);
     const int lh = x >> 1, l = lh / d.H, hk = lh - l * d.H;
     const int64_t row = (int64_t(l) * d.n_pages) * d.H + hk;
     copy_vecs(pool + (row + int64_t(mv.y) * d.H) * run, pool + (row + int64_t(mv.x) * d.H) * run, n_vec);
+    if (d.b8 && tid == 0) {
+      float* scale = x & 1 ? c.vs : c.ks;
+      scale[row + int64_t(mv.y) * d.H] = scale[row + int64_t(mv.x) * d.H];
+    }
   }
 }
 
@@ -293,7 +295,7 @@ __global__ void __launch_bounds__(kCopyThreads)
   pdl_enter();   // behind the plan
   const int n = w.count[0], used = w.count[1];
   if (n == 0) return;
-  const int vecs = d.H * d.P * (d.d * elem_bytes(d) / 16);   // of a page in one layer; its bytes may pass 2^31
+  const int vecs = d.H * d.P * (d.d * paged_elem(d) / 16);   // of a page in one layer; its bytes may pass 2^31
   constexpr int kPiece = 4 * kCopyThreads;
   const int pieces = (vecs + kPiece - 1) / kPiece;
   const int64_t items = int64_t(n) * d.L * 2 * pieces;
@@ -305,6 +307,11 @@ __global__ void __launch_bounds__(kCopyThreads)
     const int2 mv = w.moves[int(z - int64_t(l) * n)];
     uint4* pool = static_cast<uint4*>(y & 1 ? c.v : c.k) + int64_t(l) * d.n_pages * vecs + piece * kPiece;
     copy_vecs(pool + int64_t(mv.y) * vecs, pool + int64_t(mv.x) * vecs, min(kPiece, vecs - piece * kPiece));
+    if (d.b8 && piece == 0) {
+      float* scale = (y & 1 ? c.vs : c.ks) + int64_t(l) * d.n_pages * d.H;
+      for (int hk = threadIdx.x; hk < d.H; hk += kCopyThreads)
+        scale[int64_t(mv.y) * d.H + hk] = scale[int64_t(mv.x) * d.H + hk];
+    }
   }
   const int lane = threadIdx.x & 31, warps = kCopyThreads / 32;
   for (int s = blockIdx.x * warps + (threadIdx.x >> 5); s < d.max_seqs; s += gridDim.x * warps) {
@@ -328,7 +335,7 @@ __global__ void __launch_bounds__(kCopyThreads)
   if (p.store && refused(w.status)) return;
   const int per_seq = ((p.S - 1) >> d.lp) + 1;
   const int64_t items = int64_t(per_seq) * p.n * p.n_layers;
-  const int es = elem_bytes(d);
+  const int es = paged_elem(d);
   const int dv = d.d * es / 16;                       // vectors of a row: a power of two
   const int ldv = 31 - __clz(dv), lrun = ldv + d.lp;  // of a head's rows in a page
   for (int64_t x = blockIdx.x; x < items; x += gridDim.x) {

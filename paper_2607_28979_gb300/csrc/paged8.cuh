@@ -1,0 +1,62 @@
+// Values of 8-bit pages: x8 s with x8 of 1 sign, 4 exponent and 3 mantissa bits (largest 448, smallest step 2^-9,
+// no infinities) and a scale s = 2^e for each page, key/value head and K or V. A float wants no finer scale than a
+// power of two: its relative steps are the same wherever its range lies, and with such a scale a value is put in
+// units of it, and taken out again, exactly. e is the least in -60 .. 60 that brings the page's largest value to
+// 448 or below, so that 2^-17 of it still has all bits. Values that are not finite, or above 448 2^60, are NaN in 8
+// bits and have no part in the scale.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+namespace mot {
+namespace {
+
+constexpr float kLargest8 = 448.f * 1152921504606846976.f;   // 448 2^60
+constexpr uint32_t kNaN8 = 0x7Fu;
+
+__device__ __forceinline__ bool held8(float x) { return fabsf(x) <= kLargest8; }   // false for NaN
+
+// The scale for a largest value `top`, finite and not negative: 448 is 1.75 2^8.
+__device__ __forceinline__ float scale8(float top) {
+  const uint32_t u = __float_as_uint(top);
+  const int e = int(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u);
+  return __uint_as_float(uint32_t(min(max(e, -60), 60) + 127) << 23);
+}
+
+// Four values in units of the scale to 8 bits, to the nearest, ties to the even one; the first in the lowest byte.
+__device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  return uint32_t(lo) | uint32_t(hi) << 16;
+}
+// The same of values in their own units, inv = 1 / scale: what 8 bits do not hold becomes NaN.
+__device__ __forceinline__ float unit8(float x, float inv) { return held8(x) ? x * inv : __uint_as_float(0x7FC00000u); }
+
+// Two 8-bit values (of the lower or the upper half of a word) as fp16, exactly; NaN stays NaN.
+__device__ __forceinline__ uint32_t half2_of8(uint32_t pair) {
+  uint32_t y;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(static_cast<uint16_t>(pair)));
+  return y;
+}
+
+__device__ __forceinline__ float2 float2_of8(uint32_t pair) {
+  const uint32_t h = half2_of8(pair);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// n values (a multiple of 4) in units of a scale that grows, by n_threads threads: `ratio` is the old one over the
+// new one, and what it pushes below the smallest steps is rounded again.
+__device__ __forceinline__ void rescale8(uint8_t* x, int n, float ratio, int t, int n_threads) {
+  uint32_t* p = reinterpret_cast<uint32_t*>(x);
+  for (int k = t; k < n / 4; k += n_threads) {
+    const uint32_t u = p[k];
+    const float2 a = float2_of8(u), b = float2_of8(u >> 16);
+    p[k] = pack8(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio);
+  }
+}
+
+}  // namespace
+}  // namespace mot

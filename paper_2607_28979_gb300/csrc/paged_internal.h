@@ -1,5 +1,6 @@
-// Internal declarations of the paged cache (paged.cu: its pages; paged_append.cu: the append; paged_simt.cu,
-// paged_decode.cu, paged_fmha.cu: attention over it), shared with the C-ABI layer.
+// Internal declarations of the paged cache (paged.cu: its pages; paged8.cu: those in 8 bits
+// and contiguous caches; paged_append.cu: the append; paged_simt.cu, paged_decode.cu, paged_fmha.cu: attention over
+// it), shared with the C-ABI layer.
 #pragma once
 
 #include "mot_internal.h"
@@ -17,7 +18,10 @@ struct PagedDims {
   int32_t rot, rot_pairs;
   float eps;
   int32_t dtype;                // 0 = bf16, 1 = fp32
+  int32_t b8;                   // pages in 8 bits
 };
+// Bytes of an element of the pools.
+__host__ __device__ inline int paged_elem(const PagedDims& d) { return d.b8 ? 1 : (d.dtype ? 4 : 2); }
 
 struct PagedCache {
   void* k;
@@ -25,6 +29,8 @@ struct PagedCache {
   int32_t* table;
   int32_t* lens;
   int32_t* refs;
+  float* ks;   // 8-bit pages: scales [n_layers][n_pages][H]
+  float* vs;
 };
 
 struct PagedBatch {
@@ -69,6 +75,10 @@ struct PagedCopy {
 };
 cudaError_t launch_paged_copy(const PagedDims& d, const PagedCache& c, const PagedCopy& p,
                               const PagedWork& w, int num_sms, cudaStream_t st);
+
+// The same between bf16 and 8-bit pages.
+cudaError_t launch_paged8_copy(const PagedDims& d, const PagedCache& c, const PagedCopy& p,
+                               const PagedWork& w, int num_sms, cudaStream_t st);
 
 struct PagedAppend {
   PagedBatch b;

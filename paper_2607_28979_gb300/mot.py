@@ -78,7 +78,8 @@ class mot_paged_config(ctypes.Structure):
 
 class mot_paged_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
-                ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+                ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 class mot_paged_batch(ctypes.Structure):
@@ -130,6 +131,7 @@ _SIGS = {
     "mot_replay_attention": [_H, ctypes.c_int32, _P, _P, _P, _P, _P, ctypes.c_int32, _P, _P],
     "mot_replay_select": [_H, _P, _P, ctypes.c_int32, _P, _P],
     "mot_create_paged": [ctypes.POINTER(mot_paged_config), ctypes.POINTER(ctypes.c_void_p)],
+    "mot_create_paged8": [ctypes.POINTER(mot_paged_config), ctypes.POINTER(ctypes.c_void_p)],
     "mot_paged_cause": [_H, ctypes.POINTER(ctypes.c_int32)],
     "mot_paged_reserve": [_H, _CACHE, _BATCH, _P],
     "mot_paged_fork": [_H, _CACHE, _P, _P, _I, _P],
@@ -202,6 +204,7 @@ class Handle:
     """Owns one ``mot_handle``; destroyed with ``mot_destroy`` or on GC."""
 
     paged = None    # the config of a paged handle
+    bits8 = False   # its pages are in 8 bits
     axes = 0        # positions of a row, once its axes are set
     device = None   # its device, where torch had one when it was made
 
@@ -317,7 +320,8 @@ def make_paged_config(n_layers, q_heads, kv_heads, head_dim, page, n_pages, max_
 # and the types themselves as they come.
 _FLOATS = {MOT_BF16: {"torch.bfloat16", "torch.int16", "torch.uint16"},   # the values, or their bits
            MOT_FP32: {"torch.float32"}}
-_INT32 = {"torch.int32"}
+_EIGHT = {"torch.float8_e4m3fn", "torch.uint8", "torch.int8"}
+_INT32, _FLOAT32 = {"torch.int32"}, {"torch.float32"}
 
 
 def _bad(where: str, what: str) -> MotError:
@@ -348,12 +352,14 @@ def _whole(x, kinds, least: int, where: str, what: str, dev) -> Optional[int]:
     return x.data_ptr()
 
 
-def paged_cache(k, v, table, lens, refs) -> mot_paged_cache:
+def paged_cache(k, v, table, lens, refs, k_scale=None, v_scale=None) -> mot_paged_cache:
     """The arrays of a paged cache (contiguous device tensors): pools k, v
     [n_layers][n_pages][kv_heads][page][head_dim], int32 table [max_seqs][max_pages], lens
-    [max_seqs] and refs [n_pages]. The struct keeps the tensors; the calls check them."""
-    c = mot_paged_cache(*[_addr(x) for x in (k, v, table, lens, refs)])
-    c._keep = (k, v, table, lens, refs)
+    [max_seqs] and refs [n_pages]; of one in 8 bits (pools of float8_e4m3fn) also the float32 scales
+    [n_layers][n_pages][kv_heads]. The struct keeps the tensors; the calls check them."""
+    keep = (k, v, table, lens, refs, k_scale, v_scale)
+    c = mot_paged_cache(*[_addr(x) for x in keep])
+    c._keep = keep
     return c
 
 
@@ -366,9 +372,16 @@ def paged_batch(seqs, starts, n: int, rows: int, max_chunk: Optional[int] = None
     return b
 
 
-def mot_create_paged(cfg: mot_paged_config) -> Handle:
+def mot_create_paged8(cfg: mot_paged_config) -> Handle:
+    """mot_create_paged with pages in 8 bits; ``cfg.dtype`` is that of the calls, bf16."""
+    h = mot_create_paged(cfg, "mot_create_paged8")
+    h.bits8 = True
+    return h
+
+
+def mot_create_paged(cfg: mot_paged_config, _call: str = "mot_create_paged") -> Handle:
     out = ctypes.c_void_p()
-    _check(_lib.mot_create_paged(ctypes.byref(cfg), ctypes.byref(out)), "mot_create_paged")
+    _check(getattr(_lib, _call)(ctypes.byref(cfg), ctypes.byref(out)), _call)
     h = Handle(out.value, 0)
     h.paged = mot_paged_config.from_buffer_copy(cfg)
     torch = sys.modules.get("torch")
@@ -388,10 +401,13 @@ def _fits(h: Handle, cache: mot_paged_cache, where: str) -> Optional[mot_paged_c
         c = cfg
         form = (c.n_pages, c.kv_heads, c.page, c.head_dim)
         for x, what in zip(keep, "kv"):
-            _whole(x, _FLOATS[c.dtype], 0, where, what, h.device)
+            _whole(x, _EIGHT if h.bits8 else _FLOATS[c.dtype], 0, where, what, h.device)
             if hasattr(x, "shape") and (tuple(x.shape[1:]) != form or x.shape[0] < c.n_layers):
                 raise _bad(where, f"{what} is {tuple(x.shape)}, the handle's pools are {(c.n_layers,) + form}")
-        table, lens, refs = keep[2:]
+        table, lens, refs = keep[2:5]
+        if h.bits8:
+            for x, what in zip(keep[5:], ("k_scale", "v_scale")):
+                _whole(x, _FLOAT32, c.n_layers * c.n_pages * c.kv_heads, where, what, h.device)
         _whole(table, _INT32, c.max_seqs * c.max_pages, where, "table", h.device)
         if hasattr(table, "shape") and table.shape[-1] != c.max_pages and table.dim() > 1:
             raise _bad(where, f"table is {tuple(table.shape)}, the handle's {(c.max_seqs, c.max_pages)}")
