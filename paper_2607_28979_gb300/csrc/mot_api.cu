@@ -2120,7 +2120,6 @@ mot_status paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cach
   mot_status r = paged_args(h, cache, c);
   if (r != MOT_OK || (r = paged_batch_args(h, c, batch, p.b)) != MOT_OK) return r;
   const PagedDims& d = h->pd;
-  if (d.b8) return MOT_ERR_UNSUPPORTED;
   if (layer < 0 || layer >= d.L) return MOT_ERR_INVALID_ARG;
   if (!q || !k || !v || !q_out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
       !aligned16(q_norm) || !aligned16(k_norm))
@@ -2155,6 +2154,7 @@ mot_status paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cach
   p.k_norm = k_norm;
   p.freq = h->pfreq;
   p.q_out = q_out;
+  p.one_row = batch->max_chunk <= 1;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   MOT_CUDA_TRY(timed(h, "paged_append", st,
                      [&] { return launch_paged_append(d, c, p, h->pw, ax, h->num_sms, st); }));

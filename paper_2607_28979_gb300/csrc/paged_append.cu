@@ -1,5 +1,8 @@
 // The append of new queries, keys and values to a paged cache on sm_103a.
 #include "paged_common.cuh"
+#include "paged8.cuh"
+
+#include <algorithm>
 
 namespace mot {
 namespace {
@@ -277,6 +280,242 @@ auto append_kernel(const PagedDims& d, const PagedAxes& ax) {
   return ax.at ? append_kernel<T, D, true>(d) : append_kernel<T, D, false>(d);
 }
 
+// ---------------------------------------------------------------- 8-bit pages
+//
+// Queries as above, by the first blocks of the grid. The others take units (entry, page, head of keys or of
+// values): the new rows of one page, whose scale wants the largest of them before the first is written. A block
+// takes 8 or 16 of the rows at a time, d / 8 lanes to a row and the lane's pairs turned by angles of its own (a row
+// of one head has each angle once); twice, for the scale and to write, where they are more than that (the second
+// time from the cache). Units are dealt out by a scan of the entries in every block, or, with one row to an entry,
+// by the row.
+template <int D, int ROT, bool AXES>
+struct Rows8 {
+  static constexpr int kLph = D / 8, kAtOnce = kAppendThreads / kLph;   // lanes of a row, rows at a time
+  int el, eA, eB;
+  bool turned;
+  uint64_t turn[4];        // the lane's pairs
+  const int32_t* at[4];    // AXES: the positions of their axes
+  uint64_t wk[4];
+
+  __device__ __forceinline__ Rows8(const PagedDims& d, const PagedAppend& p, const PagedAxes& ax) {
+    using F = Four<uint16_t>;
+    el = threadIdx.x % kLph;
+    turned = ROT != kRotNone && 8 * el < d.rot;
+    const bool halves = ROT == kRotHalves && turned;
+    eA = halves ? 4 * el : 8 * el;
+    eB = halves ? (d.rot >> 1) + 4 * el : 8 * el + 4;
+    if (turned)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        turn[k] = AXES ? ax.freq[4 * el + k] : p.freq[4 * el + k];
+        if (AXES) at[k] = ax.at + int64_t(ax.axis[4 * el + k]) * p.b.rows;
+      }
+    if (p.k_norm) {
+      const uint16_t* src = static_cast<const uint16_t*>(p.k_norm);
+      uint64_t a[2], b[2];
+      reinterpret_cast<const F*>(src + eA)->unpack(a);
+      reinterpret_cast<const F*>(src + eB)->unpack(b);
+      wk[0] = a[0];
+      wk[1] = a[1];
+      wk[2] = b[0];
+      wk[3] = b[1];
+    }
+  }
+
+  // A row's eight values of this lane (two groups of four) in fp32; `key`: normed and rotated. By whole warps.
+  __device__ __forceinline__ void values(const PagedDims& d, const PagedAppend& p, const Four<uint16_t> (&raw)[2], bool key,
+                                         int row, int pos, float (&x)[8]) const {
+    uint64_t f[2], g[2];
+    raw[0].unpack(f);
+    raw[1].unpack(g);
+    if (key && p.k_norm) {
+      const uint64_t sq2 = ffma_x2(g[1], g[1], ffma_x2(g[0], g[0], ffma_x2(f[1], f[1], fmul_x2(f[0], f[0]))));
+      float ss = Four<uint16_t>::lo_f(sq2) + Four<uint16_t>::hi_f(sq2);
+#pragma unroll
+      for (int o = kLph / 2; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      const float rs = rsqrtf(fmaf(ss, 1.f / D, d.eps));
+      const uint64_t r2 = f32x2(rs, rs);
+      f[0] = fmul_x2(fmul_x2(f[0], r2), wk[0]);
+      f[1] = fmul_x2(fmul_x2(f[1], r2), wk[1]);
+      g[0] = fmul_x2(fmul_x2(g[0], r2), wk[2]);
+      g[1] = fmul_x2(fmul_x2(g[1], r2), wk[3]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      x[2 * k] = Four<uint16_t>::lo_f(f[k]);
+      x[2 * k + 1] = Four<uint16_t>::hi_f(f[k]);
+      x[4 + 2 * k] = Four<uint16_t>::lo_f(g[k]);
+      x[4 + 2 * k + 1] = Four<uint16_t>::hi_f(g[k]);
+    }
+    if (key && turned) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t by = AXES ? int64_t(at[k][row]) : int64_t(pos);
+        const float2 cs = cos_sin_turns(uint32_t(uint64_t(by) * turn[k] >> 32));
+        float& a = ROT == kRotHalves ? x[k] : x[2 * k];
+        float& b = ROT == kRotHalves ? x[4 + k] : x[2 * k + 1];
+        const float u = a, v = b;
+        a = fmaf(-v, cs.y, u * cs.x);
+        b = fmaf(u, cs.y, v * cs.x);
+      }
+    }
+  }
+
+  // The `rows` new rows from `row` on, at position pos (of one page) and on, of unit g. By the whole block.
+  __device__ __forceinline__ void page(const PagedDims& d, const PagedCache& c, const PagedAppend& p, int32_t* status,
+                                       float* top, int slot, int row, int pos, int rows, int g) const {
+    using F = Four<uint16_t>;
+    const int page = paged_entry(d, c.table, status, slot, pos);
+    if (page < 0) return;
+    const bool key = g < d.H;
+    const int hk = key ? g : g - d.H, old = pos & (d.P - 1), sub = threadIdx.x / kLph;
+    const int64_t at_head = (int64_t(p.layer) * d.n_pages + page) * d.H + hk;
+    float* place = (key ? c.ks : c.vs) + at_head;
+    uint8_t* dst = static_cast<uint8_t*>(key ? c.k : c.v) + (at_head << d.lp) * D;
+    const uint16_t* src = static_cast<const uint16_t*>(key ? p.k : p.v) + hk * D;
+    const int64_t stride = key ? p.k_stride : p.v_stride;
+    const float was = old ? *place : 0.f;
+    constexpr int kAhead = 4;   // rows of a lane with their loads in flight
+    float x[8], big = 0.f;
+    auto each = [&](auto&& use) {
+      for (int r0 = sub; r0 < rows + sub; r0 += kAhead * kAtOnce) {   // as often for every lane
+        F raw[kAhead][2];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const int r = r0 + e * kAtOnce;
+          raw[e][0].u = raw[e][1].u = make_uint2(0u, 0u);
+          if (r < rows) {
+            const uint16_t* s = src + (row + r) * stride;
+            raw[e][0] = *reinterpret_cast<const F*>(s + eA);
+            raw[e][1] = *reinterpret_cast<const F*>(s + eB);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const int r = r0 + e * kAtOnce;
+          if (r - sub >= rows) break;
+          values(d, p, raw[e], key, row + min(r, rows - 1), pos + r, x);
+          use(r);
+        }
+      }
+    };
+    each([&](int r) {
+      if (r < rows)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (held8(x[k])) big = fmaxf(big, fabsf(x[k]));
+    });
+#pragma unroll
+    for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+    if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = big;
+    __syncthreads();   // and the old scale is read
+#pragma unroll
+    for (int k = 0; k < kAppendThreads / 32; ++k) big = fmaxf(big, top[k]);
+    float scale = scale8(big);
+    if (old) {
+      scale = fmaxf(scale, was);
+      if (scale != was) rescale8(dst, old * D, was / scale, threadIdx.x, kAppendThreads);
+    }
+    if (threadIdx.x == 0) *place = scale;
+    const float inv = 1.f / scale;
+    auto write = [&](int r) {
+      if (r >= rows) return;
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = unit8(x[k], inv);
+      uint8_t* to = dst + (old + r) * D;
+      *reinterpret_cast<uint32_t*>(to + eA) = pack8(y[0], y[1], y[2], y[3]);
+      *reinterpret_cast<uint32_t*>(to + eB) = pack8(y[4], y[5], y[6], y[7]);
+    };
+    if (rows <= kAtOnce) write(sub);   // x is still there
+    else each(write);
+    __syncthreads();   // top is read
+  }
+};
+
+// The pages that an entry's new rows touch: first position and count.
+struct Touched8 {
+  int first, pages;
+};
+__device__ __forceinline__ Touched8 touched8(const PagedDims& d, const PagedSeq& s) {
+  const int first = max(s.len - s.m, 0);
+  return {first, s.slot < 0 || s.m == 0 || s.len == 0 ? 0 : ((s.len - 1) >> d.lp) - (first >> d.lp) + 1};
+}
+
+template <int D, int ROT, bool AXES>
+__global__ void __launch_bounds__(kAppendThreads, 6)
+    paged_append8_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w,
+                         const __grid_constant__ PagedAxes ax, int q_blocks, int rows_each, int parts, int by_row) {
+  __shared__ float top[kAppendThreads / 32];
+  __shared__ int64_t sh[33];
+  __shared__ int64_t s_at;
+  __shared__ int s_i;
+  if (refused(w.status)) return;
+  const int tid = threadIdx.x;
+  if (int(blockIdx.x) < q_blocks) {
+    PagedDims dq = d;
+    dq.H = 0;   // queries alone
+    append_rows<uint16_t, D, ROT, AXES>(dq, c, p, w, ax, blockIdx.x * (kAppendThreads / 32) + (tid >> 5), rows_each, parts);
+    return;
+  }
+  const Rows8<D, ROT, AXES> lanes(d, p, ax);
+  const int64_t block = int(blockIdx.x) - q_blocks, blocks = int(gridDim.x) - q_blocks;
+  const int G = 2 * d.H, n = p.b.n;
+  if (by_row) {   // a unit for each row that is the first of its entry or of a page
+    for (int64_t u = block; u < int64_t(p.b.rows) * G; u += blocks) {
+      const int row = int(u / G), g = int(u - int64_t(row) * G);
+      const PagedSeq s = paged_seq(d, p.b, c.lens, w.status, entry_of(p.b.starts, n, row));
+      const int from = s.len - s.m, pos = from + row - s.r0;
+      if (s.slot < 0 || row < s.r0 || row >= s.r0 + s.m || pos < 0) continue;   // the queries' blocks report it
+      if (row != s.r0 + max(0, -from) && (pos & (d.P - 1))) continue;
+      lanes.page(d, c, p, w.status, top, s.slot, row, pos, min(d.P - (pos & (d.P - 1)), s.len - pos), g);
+    }
+    return;
+  }
+  int64_t W = 0, mine = 0, at = 0;
+  auto scan = [&](int i0) {   // this thread's entry of the next block of them: its units, and those before it
+    mine = 0;
+    if (i0 + tid < n) mine = int64_t(touched8(d, paged_seq(d, p.b, c.lens, w.status, i0 + tid)).pages) * G;
+    int64_t t;
+    at = W + block_scan(mine, sh, t);
+    W += t;
+  };
+  for (int i0 = 0; i0 < n; i0 += kAppendThreads) scan(i0);
+  const int64_t all = W, u0 = all * block / blocks, u1 = all * (block + 1) / blocks;
+  if (u0 >= u1) return;
+  if (n > kAppendThreads) W = 0;
+  for (int i0 = 0; i0 < n; i0 += kAppendThreads) {
+    if (n > kAppendThreads) scan(i0);
+    if (u0 >= at && u0 < at + mine) {
+      s_i = i0 + tid;
+      s_at = u0 - at;
+    }
+    if (W > u0) break;
+  }
+  __syncthreads();
+  int i = s_i;
+  int64_t in = s_at;   // units of entry i before this one
+  PagedSeq s = paged_seq(d, p.b, c.lens, w.status, i);
+  Touched8 t = touched8(d, s);
+  for (int64_t u = u0; u < u1; ++u, ++in) {
+    while (in >= int64_t(t.pages) * G) {   // units are left, so an entry with pages follows
+      if (++i >= n) return;
+      in = 0;
+      s = paged_seq(d, p.b, c.lens, w.status, i);
+      t = touched8(d, s);
+    }
+    const int j = int(in / G), g = int(in - int64_t(j) * G);
+    const int pos = j ? ((t.first >> d.lp) + j) << d.lp : t.first;
+    lanes.page(d, c, p, w.status, top, s.slot, s.r0 + pos - (s.len - s.m), pos, min(d.P - (pos & (d.P - 1)), s.len - pos), g);
+  }
+}
+
+template <int D, bool AXES>
+auto append8_kernel(const PagedDims& d) {
+  return d.rot == 0 ? paged_append8_kernel<D, kRotNone, false>
+                    : d.rot_pairs ? paged_append8_kernel<D, kRotPairs, AXES> : paged_append8_kernel<D, kRotHalves, AXES>;
+}
+
 }  // namespace
 
 cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const PagedAppend& p, const PagedWork& w,
@@ -284,17 +523,26 @@ cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const P
   // few rows: a row's heads over several warps, all of their loads in flight; many: a warp takes a row, or
   // some in a row, which share the search for their entry
   constexpr int kWarps = kAppendThreads / 32;
-  const int at_once = 256 / d.d, steps = (d.Hq + at_once - 1) / at_once + (d.H + at_once - 1) / at_once;
+  const int at_once = 256 / d.d, kv = d.b8 ? 0 : d.H;
+  const int steps = (d.Hq + at_once - 1) / at_once + (kv + at_once - 1) / at_once;
   const int64_t fill = int64_t(num_sms) * 24;   // warps that are resident
   const int most = (steps + kAppendDepth - 1) / kAppendDepth;
   const int parts = p.b.rows >= fill ? 1 : int(fill / p.b.rows < most ? fill / p.b.rows : most);
   const int rows_each = int((p.b.rows * int64_t(parts) + fill - 1) / fill);
   const int64_t units = (int64_t(p.b.rows) + rows_each - 1) / rows_each * parts;
   const int grid = int((units + kWarps - 1) / kWarps);
+  if (d.b8) {
+    // pages that the rows touch: an entry of m rows at most (m - 2) / P + 2
+    const int64_t pages = std::min(int64_t(p.b.rows), int64_t(p.b.rows) / d.P + 2 * int64_t(p.b.n));
+    const int64_t blocks = std::min((p.one_row ? int64_t(p.b.rows) : pages) * 2 * d.H, int64_t(num_sms) * 16);
+    auto kern = d.d == 64 ? (ax.at ? append8_kernel<64, true>(d) : append8_kernel<64, false>(d))
+                          : (ax.at ? append8_kernel<128, true>(d) : append8_kernel<128, false>(d));
+    return launch_kernel(false, kern, int(grid + blocks), kAppendThreads, 0, st, d, c, p, w, ax, grid, rows_each, parts,
+                         int(p.one_row));
+  }
   auto kern = d.dtype == 0 ? (d.d == 64 ? append_kernel<uint16_t, 64>(d, ax) : append_kernel<uint16_t, 128>(d, ax))
                            : (d.d == 64 ? append_kernel<float, 64>(d, ax) : append_kernel<float, 128>(d, ax));
   return launch_kernel(false, kern, grid, kAppendThreads, 0, st, d, c, p, w, ax, rows_each, parts);
 }
-
 
 }  // namespace mot

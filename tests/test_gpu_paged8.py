@@ -206,3 +206,193 @@ def test_refusals():
     refused(lambda: M.mot_paged_free(plain.h, c.c, i32([0]), 1))
     M.mot_paged_store(c.h, c.c, i32([0]), 1, *flat)
     assert c.status() == M.MOT_OK
+
+
+# ---------------------------------------------------------------- append
+
+def _turned(x, angle, pairs):
+    y, rot = x.clone(), 2 * angle.shape[1]
+    if not rot:
+        return y
+    c, s = angle.cos()[:, None], angle.sin()[:, None]
+    a, b = (x[..., 0:rot:2], x[..., 1:rot:2]) if pairs else (x[..., :rot // 2], x[..., rot // 2:rot])
+    u, v = a * c - b * s, b * c + a * s
+    if pairs:
+        y[..., 0:rot:2], y[..., 1:rot:2] = u, v
+    else:
+        y[..., :rot // 2], y[..., rot // 2:rot] = u, v
+    return y
+
+
+def _check_pages(c, before, layer, seqs, new, keys, slop, values):
+    """The pools and scales after an append, from those before it ([k, v, k scales, v scales] in 64 bits) and the
+    rows' keys and values in 64 bits: values, old rows and what was not touched exactly, new keys within their
+    rounding and `slop` (largest of a row's, [rows][heads])."""
+    at = 0
+    now = [x.double() for x in (c.k, c.v, c.ks, c.vs)]
+    touched = torch.ones((c.L, c.n_pages), dtype=torch.bool, device="cuda")
+    for s, m in zip(seqs, new):
+        a = c.n[s] - m
+        while a < c.n[s]:
+            b = min(c.n[s], (a // c.P + 1) * c.P)
+            p, o, r = c.t[s][a // c.P], a % c.P, slice(at, at + b - a)
+            touched[layer, p] = False
+            for hk in range(c.H):
+                was, old = before[3][layer, p, hk], before[1][layer, p, hk, :o]
+                sc, kept, fresh = P8.joined(old, was, values[r, hk])
+                assert float(now[3][layer, p, hk]) == float(sc), (s, a, hk)
+                assert P8.same(now[1][layer, p, hk, :o], kept) and P8.same(now[1][layer, p, hk, o:o + b - a], fresh)
+                was, old, x = before[2][layer, p, hk], before[0][layer, p, hk, :o], keys[r, hk]
+                top, off = P8.largest(x, (0, 1)), slop[r, hk].max()
+                sc = now[2][layer, p, hk]
+                lo, hi = (P8.scale_of((top + e * off).clamp_min(0)) for e in (-1, 1))
+                if o:
+                    lo, hi = torch.maximum(lo, was), torch.maximum(hi, was)
+                assert float(sc) in (float(lo), float(hi)), (s, a, hk)
+                if o:
+                    assert P8.same(now[0][layer, p, hk, :o], P8.eighths(old * (was / sc)))
+                got = now[0][layer, p, hk, o:o + b - a] * sc
+                # half a step: 2^-4 of the value, 2^-10 of the scale at the least
+                P.assert_close(got, x, 2.0 ** -4 * x.abs() + 2.0 ** -10 * sc + 2 * slop[r, hk][:, None], f"k {s} {a} {hk}")
+                for x_, y_ in ((now[0], before[0]), (now[1], before[1])):   # the page's rows behind
+                    assert P8.same(x_[layer, p, hk, o + b - a:], y_[layer, p, hk, o + b - a:])
+            at += b - a
+            a = b
+    for x, y in zip(now, before):
+        assert P8.same(x[touched], y[touched])
+
+
+APPEND = [
+    # q heads, kv heads, d, page, rot, pairs, norm, axes
+    (12, 2, 128, 16, 128, False, False, False),
+    (5, 5, 64, 32, 64, True, True, False),
+    (14, 2, 64, 64, 32, False, True, True),
+    (16, 1, 128, 128, 0, False, True, False),
+    (3, 3, 128, 16, 48, True, False, True),
+    (12, 12, 64, 16, 0, False, False, False),
+    (28, 4, 128, 64, 128, False, True, True),
+]
+
+
+@pytest.mark.parametrize("new", [[5, 2, 0, 1], [1, 1, 1, 1], [150, 2, 37, 1], [16, 1, 0, 64]])
+@pytest.mark.parametrize("hq,h,d,page,rot,pairs,norm,axes", APPEND)
+def test_append_matches_the_formula(hq, h, d, page, rot, pairs, norm, axes, new):
+    base, eps = 1e6, 1e-5
+    c = P8.Cache(layers=2, q_heads=hq, kv_heads=h, d=d, page=page, n_pages=60, max_pages=20, rot_dim=rot, rot_pairs=pairs,
+                 rot_base=base, norm_eps=eps)
+    seqs = [3, 0, 5, 2]
+    c.reserve(seqs, [m + x for m, x in zip(new, (page + 3, 0, 19, 5))])
+    rows = sum(new)
+    x = c.normal(rows + 3, hq + 2 * h, d) * 3
+    x[:, :, d // 2] *= 6
+    w = [(1 + 0.2 * c.normal(d)).bfloat16() for _ in range(2)] if norm else [None, None]
+    starts = [1 + sum(new[:i]) for i in range(5)]
+    b = M.paged_batch(i32(seqs), i32(starts), 4, rows + 3, max(new))
+    out = torch.full((rows + 3, hq, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    before = [t.double() for t in (c.k, c.v, c.ks, c.vs)]
+    args = x[:, :hq], x[:, hq:hq + h], x[:, hq + h:], out, *w
+    rate = base ** (-2 * torch.arange(rot // 2, dtype=torch.float64, device="cuda") / max(rot, 1))
+    if axes:
+        at = torch.randint(-5000, 5000, (3, rows + 3), generator=c.gen, device="cuda", dtype=torch.int32)
+        M.mot_paged_set_axes(c.h, 3, [i % 3 for i in range(rot // 2)])
+        M.mot_paged_append_at(c.h, 1, c.c, b, at, *args)
+        angle = at[torch.arange(rot // 2, device="cuda") % 3].T[1:1 + rows].double() * rate
+    else:
+        M.mot_paged_append(c.h, 1, c.c, b, *args)
+        pos = torch.cat([torch.arange(c.n[s] - m, c.n[s]) for s, m in zip(seqs, new)]).cuda()
+        angle = pos.double()[:, None] * rate
+    assert c.status() == M.MOT_OK
+    y = x[1:1 + rows].double()
+
+    def expect(z, weight):
+        if weight is not None:
+            z = z * (z.square().mean(2, keepdim=True) + eps).rsqrt() * weight.double()
+        # fp32 on the way, as in 16 bits; without norm and rotation the values are the inputs
+        return _turned(z, angle, pairs), (2.0 ** -20 if norm or rot else 0.0) * z.abs().amax(2, keepdim=True)
+
+    want, slop = expect(y[:, :hq], w[0])
+    half = P.HALF["bf16"] if norm or rot else 0.0
+    P.assert_close(out[1:1 + rows], want, half * want.abs() + slop, "q")
+    assert bool((out[0] == 9).all()) and bool((out[1 + rows:] == 9).all())
+    keys, slop = expect(y[:, hq:hq + h], w[1])
+    _check_pages(c, before, 1, seqs, new, keys, slop[..., 0], y[:, hq + h:])
+
+
+def test_rows_that_come_one_by_one_and_grow():
+    """Single tokens into two pages, each of a larger range than the one before, then smaller ones: a scale only
+    rises, old rows are rounded again and again; zeros first, and values that 8 bits do not hold among them."""
+    c = P8.Cache(q_heads=2, kv_heads=2, d=64, page=16, n_pages=6, rot_dim=0)
+    c.ks.fill_(math.nan)
+    c.vs.fill_(math.nan)
+    for step in range(40):
+        c.reserve([1, 4], [1, 1])
+        x = c.normal(2, 6, 64) * (0.0 if step == 0 else 2.0 ** (step % 16 if step < 24 else 16 - step % 16))
+        if step == 3:
+            x[0, 2, 5], x[1, 4, 6], x[1, 5, :] = math.inf, math.nan, -math.inf
+        out = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device="cuda")
+        before = [t.double() for t in (c.k, c.v, c.ks, c.vs)]
+        M.mot_paged_append(c.h, 0, c.c, c.batch([1, 4], [1, 1]), x[:, :2], x[:, 2:4], x[:, 4:], out)
+        assert c.status() == M.MOT_OK
+        y = x.double()
+        if step != 3:
+            _check_pages(c, before, 0, [1, 4], [1, 1], y[:, 2:4], torch.zeros((2, 2), dtype=torch.float64, device="cuda"), y[:, 4:])
+        else:
+            assert bool(c.k[0, c.t[1][0], 0, 3, 5].double().isnan()) and int(c.k.double().isnan().sum()) == 1
+            assert bool(c.v[0, c.t[4][0], 1, 3].double().isnan().all()) and int(c.v.double().isnan().sum()) == 65
+            assert bool(torch.isfinite(c.ks[0, [c.t[1][0], c.t[4][0]]]).all())
+
+
+def test_many_entries_and_a_hint_that_is_wrong():
+    """More entries than a block has threads, some without rows, pages that several entries' rows reach; the same
+    with a max_chunk of one, which bounds nothing that is right."""
+    n = 700
+    got = []
+    for hint in (14, 1):
+        c = P8.Cache(q_heads=2, kv_heads=1, d=64, page=16, n_pages=2 * n, max_seqs=n, max_pages=3, rot_dim=64, seed=1)
+        new = [(i * 7) % 15 for i in range(n)]
+        c.reserve(list(range(n)), [m + i % 9 for i, m in enumerate(new)])
+        rows = sum(new)
+        x = c.normal(rows, 4, 64)
+        starts = [sum(new[:i]) for i in range(n + 1)]
+        out = torch.zeros((rows, 2, 64), dtype=torch.bfloat16, device="cuda")
+        before = [t.double() for t in (c.k, c.v, c.ks, c.vs)]
+        M.mot_paged_append(c.h, 0, c.c, M.paged_batch(i32(list(range(n))), i32(starts), n, rows, hint), x[:, :2], x[:, 2:3],
+                           x[:, 3:], out)
+        assert c.status() == M.MOT_OK
+        got.append(c.bytes() + [out])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    y = x.double()
+    pos = torch.cat([torch.arange(c.n[s] - m, c.n[s]) for s, m in enumerate(new)]).cuda()
+    angle = pos.double()[:, None] * 1e4 ** (-2 * torch.arange(32, dtype=torch.float64, device="cuda") / 64)
+    keys = _turned(y[:, 2:3], angle, False)
+    _check_pages(c, before, 0, list(range(n)), new, keys, 2.0 ** -20 * keys.abs().amax(2), y[:, 3:])
+
+
+def test_append_and_store_do_nothing_behind_a_refused_change():
+    c = P8.Cache(n_pages=4, max_pages=4)
+    c.reserve([0], [20])
+    before = c.bytes()
+    c.reserve([1], [64], ok=False)
+    x, out = c.normal(3, 8, 64), torch.zeros((3, 4, 64), dtype=torch.bfloat16, device="cuda")
+    M.mot_paged_store(c.h, c.c, i32([0]), 1, *[c.normal(1, 1, 2, 32, 64) for _ in range(2)])
+    M.mot_paged_append(c.h, 0, c.c, c.batch([0], [3]), x[:, :4], x[:, 4:6], x[:, 6:], out)
+    assert c.status() == M.MOT_ERR_PAGES
+    assert all(torch.equal(a, b) for a, b in zip(before, c.bytes())) and not bool(out.any())
+
+
+def test_appends_of_entries_out_of_range_write_nothing():
+    """A slot outside the table, a table entry outside the pool, rows before position 0, a negative length."""
+    c = P8.Cache(n_pages=8, max_pages=4, rot_dim=64)
+    c.reserve([0, 1, 2, 3], [20, 20, 3, 5])
+    c.table[1, 1] = 4711
+    c.lens[3] = -5
+    before = [t.double() for t in (c.k, c.v, c.ks, c.vs)]
+    for new in ([2, 2, 5, 2, 2], [1, 1, 1, 1, 1], [19, 19, 4, 3, 1]):
+        x = c.normal(sum(new), 8, 64)
+        out = torch.zeros((sum(new), 4, 64), dtype=torch.bfloat16, device="cuda")
+        M.mot_paged_append(c.h, 0, c.c, c.batch([99, 1, 2, 3, 0], new), x[:, :4], x[:, 4:6], x[:, 6:], out)
+        assert c.status() == M.MOT_ERR_PAGES
+        mine = set(c.t[0] + c.t[1][:1] + c.t[2])
+        others = torch.tensor([p for p in range(8) if p not in mine], device="cuda")
+        for a, b in zip((c.k, c.v, c.ks, c.vs), before):
+            assert P8.same(a.double()[:, others], b[:, others])
