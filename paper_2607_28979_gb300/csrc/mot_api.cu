@@ -2207,7 +2207,6 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   mot_status r = paged_args(h, cache, c);
   if (r != MOT_OK || (r = paged_batch_args(h, c, batch, a.b)) != MOT_OK) return r;
   const PagedDims& d = h->pd;
-  if (d.b8) return MOT_ERR_UNSUPPORTED;
   if (layer < 0 || layer >= d.L || !q || !out || !aligned16(q) || !aligned16(out)) return MOT_ERR_INVALID_ARG;
   const size_t qb = size_t(a.b.rows) * d.Hq * d.d * paged_es(d);
   if (overlap(out, qb, q, qb) || meets_cache(h, c, out, qb) || meets_batch(a.b, out, qb)) return MOT_ERR_INVALID_ARG;
@@ -2219,6 +2218,10 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.out = out;
   a.k = static_cast<const char*>(c.k) + at;
   a.v = static_cast<const char*>(c.v) + at;
+  if (d.b8) {
+    a.ks = c.ks + size_t(layer) * d.n_pages * d.H;
+    a.vs = c.vs + size_t(layer) * d.n_pages * d.H;
+  }
   a.table = c.table;
   a.lens = c.lens;
   a.part = h->ppart;
@@ -2228,6 +2231,10 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.wait_limit = h->wait_limit;
   a.stall_test = h->stall_test;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (d.b8) {
+    MOT_CUDA_TRY(timed(h, "paged8_decode", st, [&] { return launch_paged8_decode(a, h->num_sms, st); }));
+    return MOT_OK;
+  }
   if (paged_fmha_takes(d, batch->max_chunk)) {
     CUtensorMap tmK{}, tmV{};
     const uint64_t dims[2] = {uint64_t(d.d), uint64_t(d.n_pages) * d.H * d.P};

@@ -80,3 +80,30 @@ def same(a, b):
 
 
 assert math.isclose(TOP, 448.0 * 2.0 ** 60)
+
+
+def check_attention(c, seqs, new, q, out, layer=0, label=""):
+    """out against the formula in 64 bits, for the slots' last `new` positions."""
+    at = 0
+    for s, m in zip(seqs, new):
+        K, V = c.rows(s, layer)
+        n = K.shape[1]
+        ref, absv, slop = P.attention(q[at:at + m], K, V)
+        # beside what 16-bit pages are off by: the exponent of a page's value scale, 60 at most, is added to a score
+        # (61 roundings' worth of 2^-24, in the numerator and the sum); a weight is rounded to fp16, whose steps
+        # are 2^-10 above a power of two (11 bits): by 2^-11 of it, or by 2^-25 of the row's largest weight times its
+        # value scale, half the smallest step
+        tol = 2.0 ** -8 * ref.abs() + slop + (2.0 ** -17 + 2.0 ** -11) * absv + 1e-30
+        if m and n:
+            of = torch.tensor([c.t[s][j // c.P] for j in range(n)], device=q.device)
+            sv = c.vs[layer][of].double().T.repeat_interleave(c.Hq // c.H, 0)   # [Hq][n]
+            v8 = (V.abs().nan_to_num(0.0) / c.vs[layer][of].double().T[..., None]).repeat_interleave(c.Hq // c.H, 0).cumsum(1)
+            for r in range(m):
+                p = n - m + r
+                if p < 0:
+                    continue
+                w = torch.softmax(torch.einsum("hd,hnd->hn", q[at + r].double(), K[:, :p + 1].repeat_interleave(c.Hq // c.H, 0))
+                                  / math.sqrt(c.d), 1)
+                tol[r] += 2.0 ** -25 * (w * sv[:, :p + 1]).amax(1)[:, None] * v8[:, p]
+        P.assert_close(out[at:at + m], ref, tol, f"{label} slot {s}")
+        at += m

@@ -396,3 +396,271 @@ def test_appends_of_entries_out_of_range_write_nothing():
         others = torch.tensor([p for p in range(8) if p not in mine], device="cuda")
         for a, b in zip((c.k, c.v, c.ks, c.vs), before):
             assert P8.same(a.double()[:, others], b[:, others])
+
+
+# ---------------------------------------------------------------- attention
+
+def _attend(c, seqs, new, layer=0, hint=None, q=None):
+    q = c.normal(sum(new), c.Hq, c.d) if q is None else q
+    out = torch.full((sum(new) + 1, c.Hq, c.d), 9.0, dtype=torch.bfloat16, device="cuda")
+    starts = [sum(new[:i]) for i in range(len(new) + 1)]
+    M.mot_paged_attention(c.h, layer, c.c, M.paged_batch(i32(seqs), i32(starts), len(seqs), sum(new),
+                                                         max(new, default=0) if hint is None else hint), q, out)
+    assert bool((out[-1] == 9).all())
+    return q, out[:-1]
+
+
+SHAPES = [
+    # q heads, kv heads, d, page
+    (12, 2, 128, 16), (7, 7, 64, 32), (14, 2, 64, 64), (16, 1, 128, 128), (28, 4, 128, 64), (3, 1, 64, 16),
+]
+
+
+@pytest.mark.parametrize("hq,h,d,page", SHAPES)
+@pytest.mark.parametrize("lens,new", [
+    ([1, 2, 15, 16, 17, 31], [1, 1, 1, 1, 1, 1]),                    # single tokens on the shortest sequences
+    ([127, 128, 129, 300, 511], [1, 1, 1, 1, 1]),                    # around the tiles' ends
+    ([1000, 3, 64, 500, 33], [2, 3, 1, 0, 4]),                       # a few tokens, an entry without any
+    ([40, 200, 1, 129, 300], [40, 17, 1, 129, 33]),                  # chunks: whole sequences and pieces
+    ([700], [300]), ([513], [257]),
+])
+def test_attention_matches_the_formula(hq, h, d, page, lens, new):
+    c = P8.Cache(layers=2, q_heads=hq, kv_heads=h, d=d, page=page, n_pages=130, max_seqs=8, max_pages=64, seed=len(lens))
+    seqs = [3, 0, 5, 2, 7, 1][:len(lens)]
+    c.reserve(seqs, lens)
+    q, out = _attend(c, seqs, new, layer=1)
+    assert c.status() == M.MOT_OK
+    P8.check_attention(c, seqs, new, q, out, layer=1)
+
+
+@pytest.mark.parametrize("hint", [1, 5000])
+def test_a_hint_of_the_chunks_that_is_wrong(hint):
+    """max_chunk bounds the work, never the result: the same rows under hints that pick other kernels."""
+    c = P8.Cache(q_heads=6, kv_heads=2, d=128, page=32, n_pages=60, max_pages=32)
+    c.reserve([0, 1, 2], [300, 64, 700])
+    q, out = _attend(c, [0, 1, 2], [200, 1, 30], hint=hint)
+    assert c.status() == M.MOT_OK
+    P8.check_attention(c, [0, 1, 2], [200, 1, 30], q, out)
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_scales_of_very_different_pages(new):
+    """Value scales from 2^-60 to 2^60 from page to page, in front and behind; key scales of several steps."""
+    for order in (1, -1):
+        c = P8.Cache(q_heads=4, kv_heads=2, d=64, page=16, n_pages=40, max_pages=32)
+        c.reserve([0], [400])
+        e = torch.linspace(-60 * order, 60 * order, 25).round().cuda()
+        c.vs[0, c.t[0]] = torch.exp2(e)[:, None].expand(-1, 2)
+        c.ks[0, c.t[0]] = torch.exp2(-10 + torch.arange(25, device="cuda").float() % 5)[:, None]
+        q, out = _attend(c, [0], [new])
+        assert c.status() == M.MOT_OK
+        P8.check_attention(c, [0], [new], q, out, label=f"order {order}")
+        # pages of small values whose keys have all the weight: what is left of the large ones decides
+        c.vs[0, c.t[0]] = torch.exp2(torch.tensor([-60.0, 60.0, 0.0, -30.0] * 7, device="cuda")[:25])[:, None]
+        q, out = _attend(c, [0], [new])
+        P8.check_attention(c, [0], [new], q, out, label=f"mixed {order}")
+
+
+@pytest.mark.parametrize("new", [1, 3, 90])
+def test_what_is_not_seen_is_not_met(new):
+    """NaN in every position behind the sequence, in pages that nobody holds, in their scales, and in the new
+    positions that a row does not see."""
+    c = P8.Cache(q_heads=8, kv_heads=2, d=128, page=64, n_pages=12, max_pages=8)
+    c.reserve([0, 1], [203, 150])
+    nan = torch.tensor(127, dtype=torch.uint8, device="cuda")
+    held = {p for s in (0, 1) for p in c.t[s]}
+    for x in (c.k.view(torch.uint8), c.v.view(torch.uint8)):
+        for s in (0, 1):
+            x[0, c.t[s][-1], :, c.n[s] % 64:] = nan
+        for p in range(12):
+            if p not in held:
+                x[0, p] = nan
+    for p in range(12):
+        if p not in held:
+            c.ks[0, p], c.vs[0, p] = math.nan, math.inf
+    q, clean = _attend(c, [0, 1], [new, new])
+    P8.check_attention(c, [0, 1], [new, new], q, clean)
+    # the last new position of slot 0 holds NaN in one dimension of one head's value: that row's heads alone meet it
+    p, o = c.t[0][202 // 64], 202 % 64
+    c.v.view(torch.uint8)[0, p, 1, o, 77] = 255
+    _, out = _attend(c, [0, 1], [new, new], q=q)
+    want = clean.clone()
+    want[new - 1, 4:, 77] = math.nan
+    assert P8.same(out, want)
+    # the same of a key: the rows that see it are NaN in that head
+    c.k.view(torch.uint8)[0, p, 0, o, 5] = 127
+    _, out = _attend(c, [0, 1], [new, new], q=q)
+    want[new - 1, :4] = math.nan
+    assert P8.same(out, want)
+    assert c.status() == M.MOT_OK
+
+
+@pytest.mark.parametrize("new", [2, 200])
+def test_a_value_that_is_nan_in_the_middle_of_what_rows_see(new):
+    """A NaN value that the first rows of a chunk do not see and the later ones do."""
+    c = P8.Cache(q_heads=4, kv_heads=1, d=64, page=16, n_pages=40, max_pages=32)
+    c.reserve([0], [333])
+    q, clean = _attend(c, [0], [new])
+    at = 333 - new + new // 2
+    c.v.view(torch.uint8)[0, c.t[0][at // 16], 0, at % 16, [0, 31, 63]] = 127
+    _, out = _attend(c, [0], [new], q=q)
+    want = clean.clone()
+    want[new // 2:, :, [0, 31, 63]] = math.nan
+    assert P8.same(out, want)
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_queries_of_every_size_and_ones_that_are_not_finite(new):
+    """Rows of zeros, of the smallest and of large values; an infinity or a NaN makes its own row NaN."""
+    c = P8.Cache(q_heads=8, kv_heads=1, d=64, page=16, n_pages=20)
+    c.reserve([0], [200])
+    q = c.normal(new, 8, 64)
+    q[:, 0] = 0.0
+    q[:, 1] *= 2.0 ** -130
+    q[:, 2] *= 2.0 ** -20
+    q[:, 3] *= 2.0 ** 6
+    q[:, 4, 1:] *= 2.0 ** -40
+    q[:, 5, 9], q[:, 6, 63] = math.inf, math.nan
+    _, out = _attend(c, [0], [new], q=q)
+    assert bool(out[:, 5:7].isnan().all())
+    q[:, 5:7], out[:, 5:7] = q[:, :1], out[:, :1]
+    P8.check_attention(c, [0], [new], q, out)
+
+
+def test_rows_before_the_first_position_are_zeros():
+    c = P8.Cache(q_heads=4, kv_heads=2, d=64, page=16, n_pages=20)
+    for n, new in ((3, 5), (0, 2), (50, 90)):
+        c.reserve([1], [n])
+        q, out = _attend(c, [1], [new])
+        assert not bool(out[:new - n].any())
+        P8.check_attention(c, [1], [new], q, out)
+        c.free([1])
+
+
+def test_entries_out_of_range_are_reported():
+    c = P8.Cache(q_heads=4, kv_heads=2, d=64, page=16, n_pages=20)
+    c.reserve([0, 1], [100, 90])
+    c.table[1, 2] = 20
+    for new in (1, 50):
+        q, out = _attend(c, [0, 1], [new, new])
+        assert c.status() == M.MOT_ERR_PAGES
+        P8.check_attention(c, [0], [new], q, out)
+        q, out = _attend(c, [0, 44], [new, new])
+        assert c.status() == M.MOT_ERR_PAGES
+        P8.check_attention(c, [0], [new], q, out)
+
+
+def test_many_sequences_of_different_lengths():
+    rng = np.random.default_rng(5)
+    n = 150
+    c = P8.Cache(q_heads=8, kv_heads=2, d=64, page=32, n_pages=4000, max_seqs=n, max_pages=40)
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(1200), n))]
+    c.reserve(list(range(n)), lens)
+    for new in ([1] * n, [min(x, int(rng.integers(0, 9))) for x in lens], [min(x, 1 + 30 * (i % 40 == 0)) for i, x in enumerate(lens)]):
+        q, out = _attend(c, list(range(n)), new)
+        assert c.status() == M.MOT_OK
+        P8.check_attention(c, list(range(n)), new, q, out)
+
+
+def test_offsets_beyond_32_bits():
+    """Pages whose bytes lie behind 2^32 of a pool, in a later layer."""
+    c = P8.Cache(layers=1, q_heads=2, kv_heads=1, d=128, page=128, n_pages=4, max_pages=4)
+    pages = 1 << 18   # 4 GB a layer
+    pool = [torch.zeros((2, pages, 1, 128, 128), dtype=torch.uint8, device="cuda").view(P8.F8) for _ in range(2)]
+    scales = [torch.ones((2, pages, 1), device="cuda") for _ in range(2)]
+    table, lens = i32([[pages - 1, 7, pages - 2]]), i32([300])
+    refs = torch.zeros(pages, dtype=torch.int32, device="cuda")
+    h = M.mot_create_paged8(M.make_paged_config(2, 2, 1, 128, 128, pages, 1, 3))
+    cache = M.paged_cache(*pool, table, lens, refs, *scales)
+    c.reserve([0], [300])
+    for mine, there in zip((c.k, c.v, c.ks, c.vs), (*pool, *scales)):
+        for a, b in zip(c.t[0], (pages - 1, 7, pages - 2)):
+            there[1, b].copy_(mine[0, a])
+    for new in (1, 100):
+        q, out = _attend(c, [0], [new])
+        far = torch.zeros((new, 2, 128), dtype=torch.bfloat16, device="cuda")
+        M.mot_paged_attention(h, 1, cache, M.paged_batch(i32([0]), i32([0, new]), 1, new), q, far)
+        assert M.mot_get_device_status(h) == M.MOT_OK
+        assert torch.equal(out, far)
+    x = c.normal(40, 4, 128)
+    outs = [torch.zeros((40, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    M.mot_paged_append(c.h, 0, c.c, c.batch([0], [40]), x[:, :2], x[:, 2:3], x[:, 3:], outs[0])
+    M.mot_paged_append(h, 1, cache, M.paged_batch(i32([0]), i32([0, 40]), 1, 40), x[:, :2], x[:, 2:3], x[:, 3:], outs[1])
+    for mine, there in zip((c.k, c.v, c.ks, c.vs), (*pool, *scales)):
+        for a, b in zip(c.t[0], (pages - 1, 7, pages - 2)):
+            assert torch.equal(mine[0, a].view(torch.uint8), there[1, b].view(torch.uint8))
+    flat = [torch.zeros((1, 1, 1, 300, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    M.mot_paged_load(h, cache, i32([0]), 1, *flat, first_layer=1)
+    for f, x in zip(flat, c.rows(0)):
+        assert torch.equal(f[0, 0].double(), x)
+
+
+# ---------------------------------------------------------------- together
+
+def test_from_a_translated_context_to_branches_that_grow():
+    """A contiguous context stored, forked to branches, each with a prompt and then single tokens, captured and
+    replayed on another stream: every step's attention is that of the rows held, and branches do not meet."""
+    Hq, H, d, L = 8, 2, 64, 2
+    c = P8.Cache(layers=L, q_heads=Hq, kv_heads=H, d=d, page=16, n_pages=120, max_seqs=6, max_pages=16, rot_dim=64)
+    c.reserve([0], [75])
+    flat = [c.normal(L, 1, H, 75, d) for _ in range(2)]
+    M.mot_paged_store(c.h, c.c, i32([0]), 1, *flat)
+    c.fork([0, 0, 0], [1, 3, 5])
+    c.check("fork")
+    kids = [1, 3, 5]
+    for new in ([20, 1, 64], [1, 1, 1]):
+        c.reserve(kids, new)
+        rows = sum(new)
+        b = c.batch(kids, new)
+        for l in range(L):
+            x = c.normal(rows, Hq + 2 * H, d)
+            q = torch.zeros((rows, Hq, d), dtype=torch.bfloat16, device="cuda")
+            out = torch.zeros_like(q)
+            before = [t.double() for t in (c.k, c.v, c.ks, c.vs)]
+            M.mot_paged_append(c.h, l, c.c, b, x[:, :Hq], x[:, Hq:Hq + H], x[:, Hq + H:], q)
+            M.mot_paged_attention(c.h, l, c.c, b, q, out)
+            pos = torch.cat([torch.arange(c.n[s] - m, c.n[s]) for s, m in zip(kids, new)]).cuda()
+            angle = pos.double()[:, None] * 1e4 ** (-2 * torch.arange(32, dtype=torch.float64, device="cuda") / 64)
+            keys = _turned(x[:, Hq:Hq + H].double(), angle, False)
+            _check_pages(c, before, l, kids, new, keys, 2.0 ** -20 * keys.abs().amax(2), x[:, Hq + H:].double())
+            P8.check_attention(c, kids, new, q, out, layer=l)
+    # a decoding step as a graph
+    st = torch.cuda.Stream()
+    seqs, starts = i32(kids), i32([0, 1, 2, 3])
+    b = M.paged_batch(seqs, starts, 3, 3, 1)
+    x = c.normal(L, 3, Hq + 2 * H, d)
+    q, out = (torch.zeros((L, 3, Hq, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+
+    def step(stream):
+        M.mot_paged_reserve(c.h, c.c, b, stream=stream)
+        for l in range(L):
+            y = x[l]
+            M.mot_paged_append(c.h, l, c.c, b, y[:, :Hq], y[:, Hq:Hq + H], y[:, Hq + H:], q[l], stream=stream)
+            M.mot_paged_attention(c.h, l, c.c, b, q[l], out[l], stream=stream)
+
+    def follow():   # the same on the lists
+        for s in kids:
+            c.t[s] += c.take(c.pages(c.n[s] + 1) - c.pages(c.n[s]))
+            c.n[s] += 1
+
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        step(st)
+    follow()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        step(torch.cuda.current_stream())
+    for _ in range(20):
+        x.copy_(c.normal(L, 3, Hq + 2 * H, d))
+        g.replay()
+        follow()
+        torch.cuda.synchronize()
+        for l in range(L):
+            P8.check_attention(c, kids, [1, 1, 1], q[l], out[l], layer=l)
+    c.check("replays")
+    back = [torch.zeros((L, 1, H, 75, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    M.mot_paged_load(c.h, c.c, i32([0]), 1, *back)   # the context itself is as it was stored
+    for x, y in zip(back, flat):
+        assert torch.equal(x[:, 0].double(), _kept(y[:, 0].double(), 16))
+    assert c.status() == M.MOT_OK
