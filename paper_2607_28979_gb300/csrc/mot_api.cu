@@ -69,6 +69,17 @@ bool encode_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* d
   return r == CUDA_SUCCESS;
 }
 
+// The same of bytes: 64 or 128 of them in the first dimension of the box, swizzled as wide.
+bool encode_u8(CUtensorMap* map, const void* base, const uint64_t (&dims)[2], const uint32_t (&box)[2]) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t gd[2] = {dims[0], dims[1]}, gs[1] = {dims[0]};
+  const cuuint32_t bx[2] = {box[0], box[1]}, es[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            box[0] == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Ev {
   cudaEvent_t a, b;
   int kind;
@@ -2231,6 +2242,14 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.wait_limit = h->wait_limit;
   a.stall_test = h->stall_test;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (d.b8 && paged_fmha_takes(d, batch->max_chunk)) {
+    CUtensorMap tmK{}, tmV{};
+    const uint64_t dims[2] = {uint64_t(d.d), uint64_t(d.n_pages) * d.H * d.P};
+    const uint32_t box[2] = {uint32_t(d.d), uint32_t(d.P)};
+    if (!encode_u8(&tmK, a.k, dims, box) || !encode_u8(&tmV, a.v, dims, box)) return MOT_ERR_CUDA;
+    MOT_CUDA_TRY(timed(h, "paged8_fmha", st, [&] { return launch_paged8_fmha(a, tmK, tmV, h->num_sms, st); }));
+    return MOT_OK;
+  }
   if (d.b8) {
     MOT_CUDA_TRY(timed(h, "paged8_decode", st, [&] { return launch_paged8_decode(a, h->num_sms, st); }));
     return MOT_OK;

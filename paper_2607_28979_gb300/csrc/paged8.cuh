@@ -35,6 +35,9 @@ __device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d) {
 // The same of values in their own units, inv = 1 / scale: what 8 bits do not hold becomes NaN.
 __device__ __forceinline__ float unit8(float x, float inv) { return held8(x) ? x * inv : __uint_as_float(0x7FC00000u); }
 
+// Which of a word's four values are NaN, as bit 7 of each.
+__device__ __forceinline__ uint32_t nan8(uint32_t u) { return ((u & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+
 // Two 8-bit values (of the lower or the upper half of a word) as fp16, exactly; NaN stays NaN.
 __device__ __forceinline__ uint32_t half2_of8(uint32_t pair) {
   uint32_t y;

@@ -61,8 +61,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Bytes of four values that are NaN, as bit 7 of each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t u) { return ((u & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
 // CTAs per SM: as many as have their registers without spilling.
 template <int D, int NT>
@@ -297,7 +295,7 @@ __global__ void __launch_bounds__(kDecThreads, kResident<D, NT>) paged8_decode_k
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-          for (int w = 0; w < kV / 4; ++w) odd |= nan_bytes(vr[e >> 2][e & 3].w[w]) != 0;
+          for (int w = 0; w < kV / 4; ++w) odd |= nan8(vr[e >> 2][e & 3].w[w]) != 0;
         odd = __any_sync(0xffffffffu, odd);
       }
       if (odd) {   // taken out of the product, and added below where it is seen
@@ -306,7 +304,7 @@ __global__ void __launch_bounds__(kDecThreads, kResident<D, NT>) paged8_decode_k
 #pragma unroll
           for (int w = 0; w < kV / 4; ++w) {
             uint32_t& u = vr[e >> 2][e & 3].w[w];
-            u &= ~((nan_bytes(u) >> 7) * 255u);
+            u &= ~((nan8(u) >> 7) * 255u);
           }
       }
 #pragma unroll

@@ -134,5 +134,8 @@ cudaError_t launch_paged8_decode(const PagedAttnArgs& a, int num_sms, cudaStream
 bool paged_fmha_takes(const PagedDims& d, int max_chunk);
 cudaError_t launch_paged_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV,
                               int num_sms, cudaStream_t st);
+// The same over 8-bit pages: maps of bytes, box d x P.
+cudaError_t launch_paged8_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                               int num_sms, cudaStream_t st);
 
 }  // namespace mot
