@@ -2242,16 +2242,15 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.wait_limit = h->wait_limit;
   a.stall_test = h->stall_test;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (d.b8 && paged_fmha_takes(d, batch->max_chunk)) {
+  if (d.b8) {
+    const bool chunks = paged_fmha_takes(d, batch->max_chunk);
     CUtensorMap tmK{}, tmV{};
     const uint64_t dims[2] = {uint64_t(d.d), uint64_t(d.n_pages) * d.H * d.P};
     const uint32_t box[2] = {uint32_t(d.d), uint32_t(d.P)};
     if (!encode_u8(&tmK, a.k, dims, box) || !encode_u8(&tmV, a.v, dims, box)) return MOT_ERR_CUDA;
-    MOT_CUDA_TRY(timed(h, "paged8_fmha", st, [&] { return launch_paged8_fmha(a, tmK, tmV, h->num_sms, st); }));
-    return MOT_OK;
-  }
-  if (d.b8) {
-    MOT_CUDA_TRY(timed(h, "paged8_decode", st, [&] { return launch_paged8_decode(a, h->num_sms, st); }));
+    MOT_CUDA_TRY(timed(h, chunks ? "paged8_fmha" : "paged8_decode", st, [&] {
+      return (chunks ? launch_paged8_fmha : launch_paged8_decode)(a, tmK, tmV, h->num_sms, st);
+    }));
     return MOT_OK;
   }
   if (paged_fmha_takes(d, batch->max_chunk)) {

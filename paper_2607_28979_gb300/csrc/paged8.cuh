@@ -50,6 +50,34 @@ __device__ __forceinline__ float2 float2_of8(uint32_t pair) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+// A query's row in two 8-bit parts, q = (hi + lo) 2^-up: put by a power of two so that its largest value is at 2^7,
+// each part takes 4 of the 8 bits that a bf16 has. That is exact from 2^-9 of the row's largest on, and off by 2^-17
+// of that below (or by 2^-70: the power is 2^60 at most, so that a score's factor stays above 0 with any key scale).
+// Two products with 8-bit keys take as long as one of 16 bits, and no key is converted.
+struct Split8 {
+  float by;       // 2^up
+  float factor;   // 2^-up; NaN for a row that holds an infinity or NaN
+  // top: the largest magnitude of the row as the bits of a bf16
+  __device__ __forceinline__ explicit Split8(uint32_t top) {
+    const int up = min(7 + 127 - int(top >> 7), 60);
+    by = __uint_as_float(uint32_t(up + 127) << 23);
+    factor = top >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float(uint32_t(127 - up) << 23);
+  }
+  // Four bf16 in two words.
+  __device__ __forceinline__ void operator()(uint32_t w0, uint32_t w1, uint32_t& hi, uint32_t& lo) const {
+    const float a = __uint_as_float(w0 << 16) * by, b = __uint_as_float(w0 & 0xFFFF0000u) * by;
+    const float c = __uint_as_float(w1 << 16) * by, d = __uint_as_float(w1 & 0xFFFF0000u) * by;
+    hi = pack8(a, b, c, d);
+    const float2 x = float2_of8(hi), y = float2_of8(hi >> 16);
+    lo = pack8(a - x.x, b - x.y, c - y.x, d - y.y);
+  }
+};
+// The largest magnitude among eight bf16 and `top`, in each half: magnitudes of bf16 are ordered as integers.
+__device__ __forceinline__ uint32_t top_bf16x2(uint32_t top, const uint4& u) {
+  return __vmaxu2(top, __vmaxu2(__vmaxu2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu),
+                                __vmaxu2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu)));
+}
+
 // n values (a multiple of 4) in units of a scale that grows, by n_threads threads: `ratio` is the old one over the
 // new one, and what it pushes below the smallest steps is rounded again.
 __device__ __forceinline__ void rescale8(uint8_t* x, int n, float ratio, int t, int n_threads) {

@@ -3,11 +3,7 @@
 //   paged8_fmha_kernel  persistent, one CTA per SM over its run of key tiles (paged_common.cuh), an item being 256
 //                       rows of one key/value head as two streams of 128, over tiles of 128 keys, as in the kernel of
 //                       16-bit pages. What is different:
-//                         keys       go as they lie into an 8-bit product (kind::f8f6f4). A row of Q, put by a power
-//                                    of two so that its largest value is at 2^7, is split in two 8-bit parts, q = q1
-//                                    + q2: a bf16 has 8 bits and each part takes 4 of them, so this is exact from
-//                                    2^-9 of the row's largest on, and off by 2^-17 of that below (or by 2^-70:
-//                                    the power is 2^60 at most). Two 8-bit products take as long as one of 16 bits, and no key is converted;
+//                         keys       go as they lie into an 8-bit product (kind::f8f6f4), with Q in two parts (Split8);
 //                         values     are turned to fp16, which holds them exactly, by warps 2 and 3, between two
 //                                    rings of shared memory (16 values a thread and step: one 16-byte load, two
 //                                    stores, without bank conflicts); P in two 8-bit parts would leave them as they
@@ -24,8 +20,6 @@
 #include "paged_chunk.cuh"
 #include "paged8.cuh"
 
-#include <type_traits>
-
 namespace mot {
 namespace {
 
@@ -37,7 +31,7 @@ struct Pf8 {
   static constexpr int kTile = 128 * D;                // bytes of 128 rows in 8 bits
   static constexpr int kBlk = 128 * 128;               // 128 rows of 64 fp16
   static constexpr int kTile16 = D / 64 * kBlk;
-  static constexpr int kNK = 2, kNV = 2, kNH = 2;      // tiles in flight: keys, values, values in fp16
+  static constexpr int kNK = 2, kNV = 3, kNH = 2;      // tiles in flight: keys, values, values in fp16
   static constexpr int kThreads = 32 * 12;
   static constexpr int kBytes = (4 + kNK + kNV) * kTile + kNH * kTile16;
   static constexpr int kSmem = kBytes + 2048 + 1024;   // barriers, scales and notes; alignment
@@ -60,7 +54,7 @@ struct Scales8 {   // of a tile's groups of 16 keys
 // Barriers and what the roles leave for one another.
 struct Pf8Shared {
   uint64_t q_ready[2], s_full[2], p_half[2][2], pv_done[2];
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], h_full[2], h_empty[2], drain;
+  uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3], h_full[3], h_empty[3], drain;
   uint32_t tmem;
   int32_t abort;
   PagedJoinShared join;
@@ -117,6 +111,8 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
       mbar_init(&sh.p_half[i][0], 4);
       mbar_init(&sh.p_half[i][1], 4);
       mbar_init(&sh.pv_done[i], 1);
+    }
+    for (int i = 0; i < 3; ++i) {
       mbar_init(&sh.k_full[i], 1);
       mbar_init(&sh.k_empty[i], 1);
       mbar_init(&sh.v_full[i], 1);
@@ -290,7 +286,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
       __syncwarp();
     } else {
       // ------------------------------------------------ warps 2, 3: values to fp16, half of the rows each
-      constexpr int kPasses = D / 64;   // 4 pieces of 16 bytes at a time, of 8 rows
+      constexpr int kPasses = D / 64;   // steps of 8 rows, 4 pieces of 16 bytes each
       uint32_t t = 0;
       bool ok = true;
       for (int piece = 0; ok && c.u < c.u_end; ++piece) {
@@ -313,29 +309,41 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           const uint32_t from = smem_u32(sV + sv * F::kTile), to = smem_u32(sH + shf * F::kTile16);
           const int r_end = min(rows, 64 * (warp - 1));
           const bool part_seen = kt >= masked;
-#pragma unroll 2
-          for (int r = 64 * (warp - 2) + (lane >> 2); r < r_end; r += 8) {
+          // kAhead pieces with their loads in flight; two rows of a quarter warp take different halves of their 128
+          // bytes, so that no bank is met twice
+          constexpr int kAhead = 4, kRows = 8 * kAhead / kPasses;
+#pragma unroll 1
+          for (int r0 = 64 * (warp - 2); r0 < r_end; r0 += kRows) {
+            uint4 v[kAhead];
 #pragma unroll
-            for (int h = 0; h < kPasses; ++h) {
-              // two rows of a quarter warp take different halves of their 128 bytes: no bank is met twice
-              const int x = (lane & 3) | (kPasses == 2 ? ((r & 1) ^ h) << 2 : 0);
-              uint4 v = ld_shared_v4(from + F::at(r, x));
-              if (r >= n_keys) v = make_uint4(0u, 0u, 0u, 0u);
-              if (part_seen) {   // some rows do not see all of the tile: NaN goes out of the product, and is noted
-                const uint32_t n0 = nan8(v.x), n1 = nan8(v.y), n2 = nan8(v.z), n3 = nan8(v.w);
-                if (n0 | n1 | n2 | n3) {
-                  v.x &= ~((n0 >> 7) * 255u);
-                  v.y &= ~((n1 >> 7) * 255u);
-                  v.z &= ~((n2 >> 7) * 255u);
-                  v.w &= ~((n3 >> 7) * 255u);
-                  atomicOr(&notes[min(kt - masked, 3)][r >> 5], 1u << (r & 31));
-                }
+            for (int y = 0; y < kAhead; ++y) {
+              const int r = r0 + 8 * (y / kPasses) + (lane >> 2);
+              const int x = (lane & 3) | (kPasses == 2 ? ((r & 1) ^ (y & 1)) << 2 : 0);
+              v[y] = r < n_keys ? ld_shared_v4(from + F::at(r, x)) : make_uint4(0u, 0u, 0u, 0u);
+            }
+            if (part_seen) {   // some rows do not see all of the tile: NaN goes out of the product, and is noted
+#pragma unroll
+              for (int y = 0; y < kAhead; ++y) {
+                const int r = r0 + 8 * (y / kPasses) + (lane >> 2);
+                const uint32_t n0 = nan8(v[y].x), n1 = nan8(v[y].y), n2 = nan8(v[y].z), n3 = nan8(v[y].w);
+                if (!(n0 | n1 | n2 | n3)) continue;
+                v[y].x &= ~((n0 >> 7) * 255u);
+                v[y].y &= ~((n1 >> 7) * 255u);
+                v[y].z &= ~((n2 >> 7) * 255u);
+                v[y].w &= ~((n3 >> 7) * 255u);
+                atomicOr(&notes[min(kt - masked, 3)][r >> 5], 1u << (r & 31));
               }
+            }
+#pragma unroll
+            for (int y = 0; y < kAhead; ++y) {
+              const int r = r0 + 8 * (y / kPasses) + (lane >> 2);
+              const int x = (lane & 3) | (kPasses == 2 ? ((r & 1) ^ (y & 1)) << 2 : 0);
               const uint32_t dst = to + (x >> 2) * F::kBlk + r * 128;
               const int c0 = 2 * (x & 3), s7 = r & 7;
-              st_shared_v4(dst + ((c0 ^ s7) << 4), half2_of8(v.x), half2_of8(v.x >> 16), half2_of8(v.y), half2_of8(v.y >> 16));
-              st_shared_v4(dst + (((c0 + 1) ^ s7) << 4), half2_of8(v.z), half2_of8(v.z >> 16), half2_of8(v.w),
-                           half2_of8(v.w >> 16));
+              st_shared_v4(dst + ((c0 ^ s7) << 4), half2_of8(v[y].x), half2_of8(v[y].x >> 16), half2_of8(v[y].y),
+                           half2_of8(v[y].y >> 16));
+              st_shared_v4(dst + (((c0 + 1) ^ s7) << 4), half2_of8(v[y].z), half2_of8(v[y].z >> 16), half2_of8(v[y].w),
+                           half2_of8(v[y].w >> 16));
             }
           }
           fence_proxy_async_smem();
@@ -374,35 +382,17 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
         const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + out_row * D);
         uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < D / 8; ++e) {
-          const uint4 u = valid ? src[e] : make_uint4(0u, 0u, 0u, 0u);
-          top = __vmaxu2(top, __vmaxu2(__vmaxu2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu),
-                                       __vmaxu2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu)));
-        }
-        top = max(top & 0xFFFFu, top >> 16);   // magnitudes of bf16 are ordered as integers
-        const int up = min(7 + 127 - int(top >> 7), 60);   // rf times any key scale stays above 0: -inf times it is -inf
-        const float by = __uint_as_float(uint32_t(up + 127) << 23);
-        // a row that holds an infinity or NaN: its scores are NaN
-        rf = top >= 0x7F80u ? __uint_as_float(0x7FC00000u) : sl2 * __uint_as_float(uint32_t(127 - up) << 23);
+        for (int e = 0; e < D / 8; ++e) top = top_bf16x2(top, valid ? src[e] : make_uint4(0u, 0u, 0u, 0u));
+        const Split8 split(max(top & 0xFFFFu, top >> 16));
+        rf = sl2 * split.factor;
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) {
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const uint4 u = valid ? src[2 * e + k] : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              float q[4];
-#pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                q[2 * z] = __uint_as_float(w[2 * y + z] << 16) * by;
-                q[2 * z + 1] = __uint_as_float(w[2 * y + z] & 0xFFFF0000u) * by;
-              }
-              hi[2 * k + y] = pack8(q[0], q[1], q[2], q[3]);
-              const float2 h0 = float2_of8(hi[2 * k + y]), h1 = float2_of8(hi[2 * k + y] >> 16);
-              lo[2 * k + y] = pack8(q[0] - h0.x, q[1] - h0.y, q[2] - h1.x, q[3] - h1.y);
-            }
+            split(u.x, u.y, hi[2 * k], lo[2 * k]);
+            split(u.z, u.w, hi[2 * k + 1], lo[2 * k + 1]);
           }
           const uint32_t at = smem_u32(sQ + 2 * i * F::kTile) + F::at(r, e);
           st_shared_v4(at, hi[0], hi[1], hi[2], hi[3]);
@@ -418,6 +408,8 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             break;
           }
           tc_fence_after();
+          const Scales8& ring = sh.scales[(tile + kt - p.kt) % kScaleRing];
+          const Scales8 sc = ring;   // in registers
           uint32_t v[4][32];
 #pragma unroll
           for (int e = 0; e < 4; ++e) tmem_ld_32x32b_x32(tS + 32 * e, v[e]);
@@ -431,7 +423,6 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
               for (int k = 0; k < 32; ++k)
                 if (32 * e + k > see) v[e][k] = 0xFF800000u;   // -inf: its weight is 0 exactly
           }
-          const Scales8& sc = sh.scales[(tile + kt - p.kt) % kScaleRing];
           float mg[8];   // largest of 16 keys, with their scales
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -469,41 +460,51 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           }
           if (raise) m = mx;
           const float mu = m == -INFINITY ? 0.f : m;
-          auto weigh = [&](auto how) {
-            constexpr bool kWide = decltype(how)::value;
+          float wide_sum = 0.f;
+          if (ring.wide) {   // the sum by itself, from the scores again: small code beside the loop below
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+              uint32_t u[16];
+              tmem_ld_32x32b_x16(tS + 16 * e, u);
+              tmem_ld_wait(u);
+              const float f = rf * ring.k[e], b = ring.e[e] - mu;
+              float g = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t pk[16];
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const float f = rf * sc.k[2 * e + y], b = sc.e[2 * e + y] - mu;
-                const uint64_t s2 = f32x2(f, f), b2 = f32x2(b, b);
-                uint64_t sum[2] = {0, 0};
-#pragma unroll
-                for (int k = 8 * y; k < 8 * y + 8; ++k) {
-                  const uint64_t x = ffma_x2((static_cast<uint64_t>(v[e][2 * k + 1]) << 32) | v[e][2 * k], s2, b2);
-                  const float p0 = kWide ? exp2f(__uint_as_float(static_cast<uint32_t>(x))) : ex2_fast(__uint_as_float(static_cast<uint32_t>(x)));
-                  const float p1 = kWide ? exp2f(__uint_as_float(static_cast<uint32_t>(x >> 32)))
-                                         : ex2_fast(__uint_as_float(static_cast<uint32_t>(x >> 32)));
-                  const __half2 ph = __floats2half2_rn(p0, p1);
-                  pk[k] = *reinterpret_cast<const uint32_t*>(&ph);
-                  sum[k & 1] = fadd_x2(sum[k & 1], f32x2(p0, p1));
-                }
-                sum[0] = fadd_x2(sum[0], sum[1]);
-                l = fmaf(__uint_as_float(static_cast<uint32_t>(sum[0])) + __uint_as_float(static_cast<uint32_t>(sum[0] >> 32)),
-                         sc.inv[2 * e + y], l);
-              }
-              tmem_st_32x32b_x16(tS + 16 * e, pk);
-              if (e & 1) {
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.p_half[i][e >> 1]);
-              }
+              for (int k = 0; k < 16; ++k) g += 16 * e + k > see ? 0.f : exp2f(fmaf(__uint_as_float(u[k]), f, b));
+              wide_sum = fmaf(g, ring.inv[e], wide_sum);
             }
-          };
-          if (sc.wide) weigh(std::true_type{});
-          else weigh(std::false_type{});
+            wide_sum += l;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const float f = rf * sc.k[2 * e + y], b = sc.e[2 * e + y] - mu;
+              const uint64_t s2 = f32x2(f, f), b2 = f32x2(b, b);
+              uint64_t sum[2] = {0, 0};
+#pragma unroll
+              for (int k = 8 * y; k < 8 * y + 8; ++k) {
+                const uint64_t x = ffma_x2((static_cast<uint64_t>(v[e][2 * k + 1]) << 32) | v[e][2 * k], s2, b2);
+                const float p0 = ex2_fast(__uint_as_float(static_cast<uint32_t>(x)));
+                const float p1 = ex2_fast(__uint_as_float(static_cast<uint32_t>(x >> 32)));
+                const __half2 ph = __floats2half2_rn(p0, p1);
+                pk[k] = *reinterpret_cast<const uint32_t*>(&ph);
+                sum[k & 1] = fadd_x2(sum[k & 1], f32x2(p0, p1));
+              }
+              sum[0] = fadd_x2(sum[0], sum[1]);
+              l = fmaf(__uint_as_float(static_cast<uint32_t>(sum[0])) + __uint_as_float(static_cast<uint32_t>(sum[0] >> 32)),
+                       sc.inv[2 * e + y], l);
+            }
+            tmem_st_32x32b_x16(tS + 16 * e, pk);
+            if (e & 1) {
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.p_half[i][e >> 1]);
+            }
+          }
+          if (ring.wide) l = wide_sum;
         }
         ok = ok && wait(&sh.pv_done[i], (t - 1) & 1u);
       }
@@ -595,7 +596,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
   if (*abort_flag) {
     if (warp == 0 && lane == 0) {
       for (int kv = 0; kv < 2; ++kv)
-        for (int st = 0; st < 2; ++st)
+        for (int st = 0; st < 3; ++st)
           if (((kv ? v_issued : k_issued) >> st) & 1u) {
             const uint32_t ad = smem_u32(kv ? &sh.v_full[st] : &sh.k_full[st]);
             const long long t0 = clock64();

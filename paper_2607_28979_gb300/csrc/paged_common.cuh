@@ -209,10 +209,12 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& a, PagedShare& s
 }
 
 // The share of CTA blockIdx.x, with its first piece: a run of `least` units at least where there are as
-// many, or a piece of `least` to `most` units. Called by all threads, which see st (in shared memory, as
+// many, or a piece of `least` to `most` units (or of more, where `near` is set and that makes no CTA's work more than
+// an eighth longer than the runs). Called by all threads, which see st (in shared memory, as
 // sh) behind it. Up to 32 entries are one warp's, an entry per lane, without a barrier between.
 template <int BM, int TK>
-__device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, int most, int64_t* sh, PagedShare& st) {
+__device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, int most, int64_t* sh, PagedShare& st,
+                                            bool near = false) {
   using S = PagedSplit<BM, TK>;
   const int G = a.d.Hq / a.d.H, H = a.d.H, n = a.b.n;
   const bool by_warp = n <= 32;
@@ -257,7 +259,7 @@ __device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, i
     int f = 0;
     if (items < grid && W > 0) {
       const int64_t need = div_fast(W + grid - items - 1, grid - items);
-      if (need <= most) {
+      if (need <= most || (near && 8 * need * grid <= 9 * W)) {
         f = need < least ? least : int(need);
         if (f > 1) W = total(f);
         if (W > grid) {   // max_chunk was no bound: runs
@@ -391,8 +393,9 @@ __device__ __forceinline__ void paged_arrive_owed(const PagedAttnArgs& a, const 
 }
 
 // Joins a group's places in order, by all threads of the CTA: to the output, or into its first place.
-// Four columns a thread; kJoin places at a time with all their loads in flight, under a running maximum.
-template <class T, int BM, int D>
+// Four columns a thread; kJoin places at a time with all their loads in flight, under a running maximum. kBar: the
+// named barrier of n_threads that join where they are not all of the CTA.
+template <class T, int BM, int D, int kBar = 0>
 __device__ __forceinline__ void paged_join(const PagedAttnArgs& a, const PagedCursor& c, const PagedGroup& g, int tid,
                                            int n_threads) {
   constexpr int kJoin = 8;
@@ -434,7 +437,9 @@ __device__ __forceinline__ void paged_join(const PagedAttnArgs& a, const PagedCu
         paged_store4(static_cast<T*>(a.out) + paged_out_row(c, a.d.H, G, r0 + r) * D + col, o, l);
     } else {
       float* part = paged_place<BM, D>(a, g, 0);
-      __syncthreads();   // a row's maximum and sum have been read by the threads of all its columns
+      // a row's maximum and sum have been read by the threads of all its columns
+      if (kBar) asm volatile("bar.sync %0, %1;" ::"n"(kBar), "r"(n_threads) : "memory");
+      else __syncthreads();
       if (x0 + tid < items) {
         __stcg(reinterpret_cast<float4*>(part + r * D + col), make_float4(o[0], o[1], o[2], o[3]));
         if (col == 0) {

@@ -128,8 +128,9 @@ int paged_counters(int num_sms);
 cudaError_t launch_paged_simt(const PagedAttnArgs& a, int num_sms, cudaStream_t st);
 // bf16, few rows per key/value head (any number is right).
 cudaError_t launch_paged_decode(const PagedAttnArgs& a, int num_sms, cudaStream_t st);
-// The same over 8-bit pages.
-cudaError_t launch_paged8_decode(const PagedAttnArgs& a, int num_sms, cudaStream_t st);
+// The same over 8-bit pages: maps of bytes, box d x P.
+cudaError_t launch_paged8_decode(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV, int num_sms,
+                                 cudaStream_t st);
 // Chunks in bf16 on the tensor cores: maps over the layer's pools as rows [n_pages * H * P][d], box 64 x P.
 bool paged_fmha_takes(const PagedDims& d, int max_chunk);
 cudaError_t launch_paged_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, const CUtensorMap& tmV,

@@ -104,7 +104,7 @@ def check_attention(c, seqs, new, q, out, layer=0, label=""):
                     continue
                 w = torch.softmax(torch.einsum("hd,hnd->hn", q[at + r].double(), K[:, :p + 1].repeat_interleave(c.Hq // c.H, 0))
                                   / math.sqrt(c.d), 1)
-                # chunks: a query's element is off by 2^-17 of its row's largest, and every score by that
+                # a query's element is off by 2^-17 of its row's largest at most, and every score by that
                 qmax = q[at + r].double().abs().amax(1)
                 off = 2.0 ** -17 * qmax * K[:, :p + 1].abs().sum(2).amax(1).repeat_interleave(c.Hq // c.H) / math.sqrt(c.d)
                 tol[r] += 2 * off[:, None] * absv[r]

@@ -668,15 +668,15 @@ def test_from_a_translated_context_to_branches_that_grow():
 
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right():
     """The first block loads nothing: every wait of the kernel ends, and nothing is left behind for the next call."""
-    for d in (64, 128):
+    for d, new in ((64, 300), (128, 300), (64, 1), (128, 1), (128, 5)):
         c = P8.Cache(q_heads=4, kv_heads=2, d=d, page=16, n_pages=130, max_pages=128)
         c.reserve([0], [2000])
-        q, want = _attend(c, [0], [300])
+        q, want = _attend(c, [0], [new])
         M.mot_debug_set(c.h, True, 1_000_000)
-        _attend(c, [0], [300], q=q)
+        _attend(c, [0], [new], q=q)
         assert c.status() == M.MOT_ERR_TIMEOUT
         M.mot_debug_set(c.h, False)
         for _ in range(2):
-            _, out = _attend(c, [0], [300], q=q)
+            _, out = _attend(c, [0], [new], q=q)
             assert c.status() == M.MOT_OK
             assert torch.equal(out, want)
