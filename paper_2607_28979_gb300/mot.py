@@ -150,6 +150,7 @@ for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
     _f.argtypes = _args
     _f.restype = _S
+_calls = {_name: getattr(_lib, _name) for _name in _SIGS}
 _lib.mot_status_string.argtypes = [_S]
 _lib.mot_status_string.restype = ctypes.c_char_p
 
@@ -173,24 +174,30 @@ def _check(status: int, where: str) -> None:
 
 
 def _addr(x) -> Optional[int]:
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
+    at = getattr(x, "data_ptr", None)
+    if at is not None:
+        return at()
     if hasattr(x, "ctypes"):   # numpy array (host buffers)
         return x.ctypes.data
     raise TypeError(f"cannot take the address of {type(x)}")
 
 
+_raw_stream = _get_device = None   # torch's, once CUDA is initialised: 0.4 us together, the Stream object 2.8
+
+
 def _stream(s) -> Optional[int]:
+    global _raw_stream, _get_device
     if s is None:
+        if _raw_stream is not None:
+            return _raw_stream(_get_device())
         torch = sys.modules.get("torch")
         if torch is not None and torch.cuda.is_initialized():
-            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # 0.4 us; the Stream object 2.8
-            if raw is not None:
-                return raw(torch.cuda.current_device())
+            raw, dev = (getattr(torch._C, x, None) for x in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+            if raw is not None and dev is not None:
+                _raw_stream, _get_device = raw, dev
+                return raw(dev())
             return torch.cuda.current_stream().cuda_stream
         return None
     if isinstance(s, int):
@@ -504,10 +511,10 @@ def mot_paged_load(h: Handle, cache: mot_paged_cache, seqs, n: int, dst_k, dst_v
 
 def _row_stride(x, what: str, least=None, where: str = "") -> int:
     """The stride of rows [heads][head_dim]; ``least``: (rows, heads, head_dim) that x has to hold."""
-    shape, strides = x.shape, x.stride()
+    shape = x.shape
     if len(shape) == 3:
         n, heads, d = shape
-        row, head, last = strides
+        row, head, last = x.stride()
         if last == 1 and (head == d or heads == 1):
             if least is not None and (n < least[0] or heads != least[1] or d != least[2]):
                 raise _bad(where, f"{what} is {tuple(shape)}, the handle's is {least}")
@@ -518,23 +525,29 @@ def _row_stride(x, what: str, least=None, where: str = "") -> int:
 def _append(h: Handle, layer, cache, batch, q, k, v, q_out, q_norm, k_norm, stream, where, positions=()) -> None:
     c, dev = _fits(h, cache, where), h.device
     if c is None:
-        strides = [_row_stride(x, what) for x, what in ((q, "q"), (k, "k"), (v, "v"))]
+        sq, sk, sv = (_row_stride(x, what) for x, what in ((q, "q"), (k, "k"), (v, "v")))
         positions = [_addr(x) for x in positions]
+        q_out, q_norm, k_norm = _addr(q_out), _addr(q_norm), _addr(k_norm)
     else:
         rows, kinds, hq, d = _batch_fits(h, batch, where), _FLOATS[c.dtype], c.q_heads, c.head_dim
         kv = (rows, c.kv_heads, d)
-        strides = _row_stride(q, "q", (rows, hq, d), where), _row_stride(k, "k", kv, where), _row_stride(v, "v", kv, where)
+        sq, sk, sv = _row_stride(q, "q", (rows, hq, d), where), _row_stride(k, "k", kv, where), _row_stride(v, "v", kv, where)
         for x, what in ((q, "q"), (k, "k"), (v, "v")):
             _typed(x, kinds, where, what, dev)
         q_out = _whole(q_out, kinds, rows * hq * d, where, "q_out", dev)
-        q_norm, k_norm = _whole(q_norm, kinds, d, where, "q_norm", dev), _whole(k_norm, kinds, d, where, "k_norm", dev)
-        for x in positions:
+        if q_norm is not None:
+            q_norm = _whole(q_norm, kinds, d, where, "q_norm", dev)
+        if k_norm is not None:
+            k_norm = _whole(k_norm, kinds, d, where, "k_norm", dev)
+        if positions:
+            x, = positions
             if hasattr(x, "shape") and x.shape[-1] != rows:
                 raise _bad(where, f"positions is {tuple(x.shape)}, {(h.axes, rows)} is wanted")
-        positions = [_whole(x, _INT32, h.axes * rows, where, "positions", dev) for x in positions]
-    _check(getattr(_lib, where)(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), *positions, _addr(q),
-                                strides[0], _addr(k), strides[1], _addr(v), strides[2], _addr(q_norm), _addr(k_norm),
-                                _addr(q_out), _stream(stream)), where)
+            positions = (_whole(x, _INT32, h.axes * rows, where, "positions", dev),)
+    status = _calls[where](h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), *positions, q.data_ptr(), sq, k.data_ptr(),
+                           sk, v.data_ptr(), sv, q_norm, k_norm, q_out, _stream(stream))
+    if status:
+        _check(status, where)
 
 
 def mot_paged_append(h: Handle, layer: int, cache: mot_paged_cache, batch: mot_paged_batch, q, k, v, q_out,
@@ -572,8 +585,9 @@ def mot_paged_attention(h: Handle, layer: int, cache: mot_paged_cache, batch: mo
     else:
         least, kinds = _batch_fits(h, batch, where) * c.q_heads * c.head_dim, _FLOATS[c.dtype]
         q, out = _whole(q, kinds, least, where, "q", dev), _whole(out, kinds, least, where, "out", dev)
-    _check(_lib.mot_paged_attention(h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), q, out,
-                                    _stream(stream)), where)
+    status = _calls[where](h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), q, out, _stream(stream))
+    if status:
+        _check(status, where)
 
 
 def mot_create(cfg: mot_config) -> Handle:
