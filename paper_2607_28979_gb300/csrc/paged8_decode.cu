@@ -27,7 +27,11 @@ constexpr int kWarps = 4;
 constexpr int kDecThreads = 2 * 32 * kWarps;   // warp 4 loads, 5 to 7 only make a group whose registers can be given away
 constexpr int kRowThreads = 32 * kWarps;   // those that compute
 constexpr int kDecTK = 32 * kWarps;
-constexpr int kLeast = 1, kMost = 4;   // units of a share
+// Units of a share, and what an item costs a CTA beside its units (its queries, the results' end: some microseconds). A
+// CTA whose run is many short items would finish last: one token of 28 heads on 4 for 64 sequences of 100 to 16,384
+// positions takes 48.3 us with three units for each, 65.8 with none, 49.0 with six; 64 of 4,096 take 55.5 for 55.0.
+// Pieces where they make no CTA's work much longer: contexts of 131,072 and 70,001 positions 46.2 us, 53.9 in runs.
+constexpr int kLeast = 1, kMost = 4, kPad = 3;
 
 // Key of a block of 16 that is row g of its first 8: of the swizzled rows of 128 bytes a quarter of a warp takes
 // those that differ in the upper half of the 16-byte pieces, of the rows of 64 bytes both halves of 128.
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
   }
-  paged_begin<BM, TK>(a, kLeast, kMost, scan, shares[0], true);
+  paged_begin<BM, TK, kPad>(a, kLeast, kMost, scan, shares[0], true);
   if (!shares[0].work) return;
   uint32_t tile = 0;   // of this CTA so far
   bool ok = true;
@@ -130,7 +134,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
     PagedCursor c = shares[0].c;
     ok = a.stall_test == 0 || blockIdx.x != 0;   // test hook: CTA 0 loads nothing
     while (ok && c.u < c.u_end) {
-      const PagedPiece p = paged_piece<BM, TK>(c, G);
+      const PagedPiece p = paged_piece<BM, TK, kPad>(c, G);
       const int kt_end = p.kt + p.n;
       // lanes 0 .. 7: a tile's blocks; their table entries are read two tiles ahead, their scales one
       auto mine = [&](int kt) { return lane < 8 && kt < kt_end && kt * TK + 16 * lane < c.s.len; };
@@ -162,7 +166,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
         next = next2;
         sc = sc2;
       }
-      paged_next<BM, TK>(a, c, p);
+      paged_next<BM, TK, kPad>(a, c, p);
     }
     }
   } else {
@@ -173,7 +177,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
   const uint32_t ring_at = smem_u32(ring) + 32 * warp * D;
   if (tid == 0) {   // seen by the others behind the first piece's barriers
     shares[1] = shares[0];
-    paged_step<BM, TK>(a, shares[1]);
+    paged_step<BM, TK, kPad>(a, shares[1]);
   }
   for (; shares[piece % 3].work; ++piece) {
     const PagedCursor& c = shares[piece % 3].c;
@@ -417,7 +421,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
     if (tid == 0) {   // by the barrier at this piece's end
       PagedShare& s = shares[(piece + 2) % 3];
       s = shares[(piece + 1) % 3];
-      if (s.work) paged_step<BM, TK>(a, s);
+      if (s.work) paged_step<BM, TK, kPad>(a, s);
     }
     // the four warps' results: to the output, or to the piece's place
     float* part = p.whole ? nullptr : paged_part<BM, D>(a, blockIdx.x, p.kt == 0);
@@ -475,7 +479,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
       }
     }
     if (tid == 0) {   // the arrivals that are still owed, so that the counters are zero for the next call
-      for (PagedShare& s = shares[piece % 3]; s.work; paged_step<BM, TK>(a, s))
+      for (PagedShare& s = shares[piece % 3]; s.work; paged_step<BM, TK, kPad>(a, s))
         if (!s.p.whole) paged_arrive_owed(a, s.p);
       atomicOr(a.status, kStatusTimeout);
     }

@@ -452,14 +452,16 @@ __global__ void __launch_bounds__(kAppendThreads, 6)
   __shared__ int s_i;
   if (refused(w.status)) return;
   const int tid = threadIdx.x;
-  if (int(blockIdx.x) < q_blocks) {
+  // blocks of the queries evenly among those of the pages: one kind streams while the other waits on its few loads
+  const int64_t q0 = int64_t(blockIdx.x) * q_blocks / gridDim.x, q1 = (int64_t(blockIdx.x) + 1) * q_blocks / gridDim.x;
+  if (q0 != q1) {
     PagedDims dq = d;
     dq.H = 0;   // queries alone
-    append_rows<uint16_t, D, ROT, AXES>(dq, c, p, w, ax, blockIdx.x * (kAppendThreads / 32) + (tid >> 5), rows_each, parts);
+    append_rows<uint16_t, D, ROT, AXES>(dq, c, p, w, ax, int(q0) * (kAppendThreads / 32) + (tid >> 5), rows_each, parts);
     return;
   }
   const Rows8<D, ROT, AXES> lanes(d, p, ax);
-  const int64_t block = int(blockIdx.x) - q_blocks, blocks = int(gridDim.x) - q_blocks;
+  const int64_t block = int(blockIdx.x) - q0, blocks = int(gridDim.x) - q_blocks;
   const int G = 2 * d.H, n = p.b.n;
   if (by_row) {   // a unit for each row that is the first of its entry or of a page
     for (int64_t u = block; u < int64_t(p.b.rows) * G; u += blocks) {
@@ -525,7 +527,7 @@ cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const P
   constexpr int kWarps = kAppendThreads / 32;
   const int at_once = 256 / d.d, kv = d.b8 ? 0 : d.H;
   const int steps = (d.Hq + at_once - 1) / at_once + (kv + at_once - 1) / at_once;
-  const int64_t fill = int64_t(num_sms) * 24;   // warps that are resident
+  const int64_t fill = int64_t(num_sms) * 24 * (d.b8 ? 2 : 1);   // warps that are resident; in shares that mix with the pages'
   const int most = (steps + kAppendDepth - 1) / kAppendDepth;
   const int parts = p.b.rows >= fill ? 1 : int(fill / p.b.rows < most ? fill / p.b.rows : most);
   const int rows_each = int((p.b.rows * int64_t(parts) + fill - 1) / fill);

@@ -82,7 +82,8 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedDims& d, const PagedBat
 //           than CTAs. No CTA then has parts of two items, which cost it some microseconds (a piece's
 //           start and end do not overlap with another's): taken while coarse is small, where that
 //           outweighs the CTAs that have less than their share.
-// The partial results of an item in several pieces are joined by the CTA that finishes last, in order.
+// The partial results of an item in several pieces are joined by the CTA that finishes last, in order. Where an item
+// costs a CTA time of its own beside its units, runs count it as PAD units more, in front of the others.
 
 // sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0, by the steps of Euclid's algorithm.
 __device__ __noinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
@@ -102,7 +103,7 @@ __device__ __noinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64
   return s;
 }
 
-template <int BM, int TK>
+template <int BM, int TK, int PAD = 0>
 struct PagedSplit {
   // Row tiles of an entry.
   static __device__ __forceinline__ int row_tiles(int m, int G) { return (m * G + BM - 1) / BM; }
@@ -112,8 +113,11 @@ struct PagedSplit {
     const int p = s.len - s.m + x / G;
     return p < 0 ? 1 : p / (TK * f) + 1;
   }
-  // Those of the row tiles [0, rt) of one head.
-  static __device__ __forceinline__ int64_t before(const PagedSeq& s, int G, int rt, int f = 1) {
+  // Those of the row tiles [0, rt) of one head, with the items' own (f = 0: runs; else pieces of f units).
+  static __device__ __forceinline__ int64_t before(const PagedSeq& s, int G, int rt, int f) {
+    return f ? plain(s, G, rt, f) : plain(s, G, rt, 1) + int64_t(rt) * PAD;
+  }
+  static __device__ __forceinline__ int64_t plain(const PagedSeq& s, int G, int rt, int f) {
     if (rt == 0) return 0;
     if (rt <= 4 || s.len < s.m) {   // few terms, or rows before position 0 (a malformed batch)
       int64_t u = 0;
@@ -126,7 +130,7 @@ struct PagedSplit {
     if (rt == R) u += units(s, G, R - 1, f);
     return u;
   }
-  static __device__ __forceinline__ int64_t head_units(const PagedSeq& s, int G, int f = 1) {
+  static __device__ __forceinline__ int64_t head_units(const PagedSeq& s, int G, int f) {
     return before(s, G, row_tiles(s.m, G), f);
   }
 };
@@ -138,7 +142,7 @@ struct PagedCursor {
   int64_t W;             // runs: all units
   int32_t C;             // runs: CTAs that have work
   int32_t coarse;        // units of a piece; 0: runs
-  int32_t i, hk, rt, kt; // the next unit
+  int32_t i, hk, rt, kt; // the next unit; runs: kt counts the item's own too
   // runs: the CTA that unit x belongs to
   __device__ __forceinline__ int owner(int64_t x) const;
 };
@@ -153,6 +157,7 @@ __device__ __forceinline__ int PagedCursor::owner(int64_t x) const { return int(
 // One piece of a share: units [kt, kt + n) of the item's `units`.
 struct PagedPiece {
   int32_t kt, n, units;
+  int32_t run;      // runs: the units that it takes of the run
   bool whole;
   int32_t c0, c1;   // the item's CTAs, in order
 };
@@ -162,12 +167,12 @@ struct PagedShare {
   PagedPiece p;
   int32_t work;   // whether this CTA has a share, or is not through it
 };
-template <int BM, int TK>
+template <int BM, int TK, int PAD = 0>
 __device__ __forceinline__ PagedPiece paged_piece(const PagedCursor& c, int G) {
   PagedPiece p;
   p.units = PagedSplit<BM, TK>::units(c.s, G, c.rt);
-  p.kt = c.kt;
   if (c.coarse) {
+    p.kt = c.kt;
     p.n = min(c.coarse, p.units - p.kt);
     p.whole = p.n == p.units;
     p.c0 = int(blockIdx.x) - p.kt / c.coarse;
@@ -175,23 +180,28 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedCursor& c, int G) {
     return p;
   }
   const int64_t left = c.u_end - c.u;
-  p.n = left < p.units - c.kt ? int(left) : p.units - c.kt;
+  p.run = left < p.units + PAD - c.kt ? int(left) : p.units + PAD - c.kt;
+  p.kt = max(c.kt - PAD, 0);
+  p.n = c.kt + p.run - PAD - p.kt;   // above 0: a run that ends in an item's own units has none of it
   p.whole = p.kt == 0 && p.n == p.units;
   p.c0 = p.c1 = int(blockIdx.x);
   if (!p.whole) {
-    p.c0 = c.owner(c.u - c.kt);
-    p.c1 = c.owner(c.u - c.kt + p.units - 1);
+    p.c0 = c.owner(c.u - c.kt + PAD);
+    p.c1 = c.owner(c.u - c.kt + PAD + p.units - 1);
   }
   return p;
 }
 // Behind a piece; loads the next entry where the run goes on to it.
-template <int BM, int TK>
+template <int BM, int TK, int PAD = 0>
 __device__ __forceinline__ void paged_next(const PagedAttnArgs& a, PagedCursor& c, const PagedPiece& p) {
   using S = PagedSplit<BM, TK>;
   const int G = a.d.Hq / a.d.H;
-  c.u = c.coarse ? c.u_end : c.u + p.n;
+  c.u = c.coarse ? c.u_end : c.u + p.run;
   c.kt = 0;
-  if (c.u >= c.u_end) return;
+  if (c.u >= c.u_end - PAD) {   // nothing is left, or only an item's own units
+    c.u = c.u_end;
+    return;
+  }
   if (++c.rt < S::row_tiles(c.s.m, G)) return;
   c.rt = 0;
   if (++c.hk < a.d.H) return;
@@ -201,21 +211,21 @@ __device__ __forceinline__ void paged_next(const PagedAttnArgs& a, PagedCursor& 
   } while (c.s.m == 0 && c.i + 1 < a.b.n);
 }
 // The same on a share, in one thread.
-template <int BM, int TK>
+template <int BM, int TK, int PAD = 0>
 __device__ __forceinline__ void paged_step(const PagedAttnArgs& a, PagedShare& st) {
-  paged_next<BM, TK>(a, st.c, st.p);
+  paged_next<BM, TK, PAD>(a, st.c, st.p);
   st.work = st.c.u < st.c.u_end;
-  if (st.work) st.p = paged_piece<BM, TK>(st.c, a.d.Hq / a.d.H);
+  if (st.work) st.p = paged_piece<BM, TK, PAD>(st.c, a.d.Hq / a.d.H);
 }
 
 // The share of CTA blockIdx.x, with its first piece: a run of `least` units at least where there are as
 // many, or a piece of `least` to `most` units (or of more, where `near` is set and that makes no CTA's work more than
 // an eighth longer than the runs). Called by all threads, which see st (in shared memory, as
 // sh) behind it. Up to 32 entries are one warp's, an entry per lane, without a barrier between.
-template <int BM, int TK>
+template <int BM, int TK, int PAD = 0>
 __device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, int most, int64_t* sh, PagedShare& st,
                                             bool near = false) {
-  using S = PagedSplit<BM, TK>;
+  using S = PagedSplit<BM, TK, PAD>;
   const int G = a.d.Hq / a.d.H, H = a.d.H, n = a.b.n;
   const bool by_warp = n <= 32;
   const int T = by_warp ? 32 : int(blockDim.x), me = threadIdx.x;
@@ -234,7 +244,7 @@ __device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, i
       t = __shfl_sync(0xffffffffu, x, n - 1);
       return x - v;
     };
-    // all entries' units, in pieces of f; `at`, `mine`: of this thread's entry among the last T entries
+    // all entries' units (f = 0), or pieces of f; `at`, `mine`: of this thread's entry among the last T entries
     int64_t mine = 0, at = 0;
     PagedSeq ms{-1, 0, 0, 0};
     if (n <= T && me < n) ms = paged_seq(a.d, a.b, a.lens, a.status, me);
@@ -264,21 +274,21 @@ __device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, i
         if (f > 1) W = total(f);
         if (W > grid) {   // max_chunk was no bound: runs
           f = 0;
-          W = total(1);
+          if (!PAD) W = total(1);
         }
       }
     }
-    const int64_t runs = div_fast(W + least - 1, least);
+    if (PAD && !f) W = total(0);
+    const int64_t runs = div_fast(W + least + PAD - 1, least + PAD);
     const int C = f || runs < grid ? int(f ? W : runs) : int(grid);
     if (int(blockIdx.x) < C) {
       const int64_t u = f ? int64_t(blockIdx.x) : div_fast(W * int(blockIdx.x), C);
-      const int ff = f ? f : 1;
       int64_t carry = 0;
       for (int i0 = 0; i0 < n; i0 += T) {
         if (n > T) {
           ms.m = 0;
           if (i0 + me < n) ms = paged_seq(a.d, a.b, a.lens, a.status, i0 + me);
-          mine = ms.m ? H * S::head_units(ms, G, ff) : 0;
+          mine = ms.m ? H * S::head_units(ms, G, f) : 0;
           int64_t t;
           at = carry + scan(mine, t);
           carry += t;
@@ -299,14 +309,18 @@ __device__ __forceinline__ void paged_begin(const PagedAttnArgs& a, int least, i
           int lo = 0, hi = S::row_tiles(o.s.m, G) - 1;   // the last rt with before(rt) <= r
           while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (S::before(o.s, G, mid, ff) <= r) lo = mid;
+            if (S::before(o.s, G, mid, f) <= r) lo = mid;
             else hi = mid - 1;
           }
           o.rt = lo;
-          o.kt = int(r - S::before(o.s, G, lo, ff)) * ff;
-          st.c = o;
-          st.p = paged_piece<BM, TK>(o, G);
-          st.work = 1;
+          o.kt = int(r - S::before(o.s, G, lo, f)) * (f ? f : 1);
+          if (!f && o.u_end - o.u <= PAD - o.kt) {   // nothing but an item's own units: its first CTA is the next
+            st.work = 0;
+          } else {
+            st.c = o;
+            st.p = paged_piece<BM, TK, PAD>(o, G);
+            st.work = 1;
+          }
         }
         if (n > T && carry > u) break;
       }
