@@ -286,8 +286,8 @@ auto append_kernel(const PagedDims& d, const PagedAxes& ax) {
 // values): the new rows of one page, whose scale wants the largest of them before the first is written. A block
 // takes 8 or 16 of the rows at a time, d / 8 lanes to a row and the lane's pairs turned by angles of its own (a row
 // of one head has each angle once); twice, for the scale and to write, where they are more than that (the second
-// time from the cache). Units are dealt out by a scan of the entries in every block, or, with one row to an entry,
-// by the row.
+// time from the cache). Units are dealt out by a scan of the entries in every block, or, with one row to an entry
+// (or few, and many entries), by the row.
 template <int D, int ROT, bool AXES>
 struct Rows8 {
   static constexpr int kLph = D / 8, kAtOnce = kAppendThreads / kLph;   // lanes of a row, rows at a time
@@ -536,11 +536,11 @@ cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const P
   if (d.b8) {
     // pages that the rows touch: an entry of m rows at most (m - 2) / P + 2
     const int64_t pages = std::min(int64_t(p.b.rows), int64_t(p.b.rows) / d.P + 2 * int64_t(p.b.n));
-    const int64_t blocks = std::min((p.one_row ? int64_t(p.b.rows) : pages) * 2 * d.H, int64_t(num_sms) * 16);
+    const int64_t blocks = std::min((p.by_row ? int64_t(p.b.rows) : pages) * 2 * d.H, int64_t(num_sms) * 16);
     auto kern = d.d == 64 ? (ax.at ? append8_kernel<64, true>(d) : append8_kernel<64, false>(d))
                           : (ax.at ? append8_kernel<128, true>(d) : append8_kernel<128, false>(d));
     return launch_kernel(false, kern, int(grid + blocks), kAppendThreads, 0, st, d, c, p, w, ax, grid, rows_each, parts,
-                         int(p.one_row));
+                         int(p.by_row));
   }
   auto kern = d.dtype == 0 ? (d.d == 64 ? append_kernel<uint16_t, 64>(d, ax) : append_kernel<uint16_t, 128>(d, ax))
                            : (d.d == 64 ? append_kernel<float, 64>(d, ax) : append_kernel<float, 128>(d, ax));
