@@ -23,7 +23,11 @@
 namespace mot {
 namespace {
 
-constexpr int kLeast = 1, kMost = 16;   // units of a share, as with 16-bit pages
+// Units of a share, as with 16-bit pages, and what an item costs beside its units: its queries and its end, about as
+// much as eight tiles, which a CTA with a run of short items has many times. 28 heads on 4, prompts of 2,111, 700 and 3,000
+// tokens from nothing: 174 us with eight, 176 with six, 178 with ten, 295 with none; a mixture with long contexts (500
+// of 9,000, 2,111 of 2,500, 1,999 of 4,097, 48 of 700) 229, 249, 238 and 363.
+constexpr int kLeast = 1, kMost = 16, kPad = 8;
 
 template <int D>
 struct Pf8 {
@@ -130,7 +134,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
     tmem_alloc(&sh.tmem, 512);
     tmem_relinquish();
   }
-  paged_begin<F::kBM, F::kTK>(a, kLeast, kMost, scan, share);
+  paged_begin<F::kBM, F::kTK, kPad>(a, kLeast, kMost, scan, share);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -156,7 +160,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
       uint32_t t = 0;   // tiles so far
       bool ok = a.stall_test == 0 || blockIdx.x != 0;   // test hook: CTA 0 loads nothing
       while (ok && c.u < c.u_end) {
-        const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+        const PagedPiece p = paged_piece<F::kBM, F::kTK, kPad>(c, G);
         const int kt_end = p.kt + p.n;
         // lanes 0 .. 7: the keys 16 lane .. of a tile; its table entry is read two tiles ahead, its scales one
         auto mine = [&](int kt) { return lane < 8 && kt < kt_end && kt * F::kTK + 16 * lane < c.s.len; };
@@ -214,7 +218,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           next = next2;
           sc = sc2;
         }
-        paged_next<F::kBM, F::kTK>(a, c, p);
+        paged_next<F::kBM, F::kTK, kPad>(a, c, p);
       }
     } else if (warp == 1) {
       // ------------------------------------------------ MMA issuer: one thread
@@ -256,7 +260,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           return true;
         };
         while (ok && c.u < c.u_end) {
-          const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+          const PagedPiece p = paged_piece<F::kBM, F::kTK, kPad>(c, G);
           const int n_str = c.s.m * G - c.rt * F::kBM > 128 ? 2 : 1;
           for (int i = 0; ok && i < n_str; ++i) {
             ok = wait1(&sh.q_ready[i], n_q[i]++ & 1u);
@@ -280,7 +284,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
               }
             }
           }
-          paged_next<F::kBM, F::kTK>(a, c, p);
+          paged_next<F::kBM, F::kTK, kPad>(a, c, p);
         }
       }
       __syncwarp();
@@ -290,7 +294,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
       uint32_t t = 0;
       bool ok = true;
       for (int piece = 0; ok && c.u < c.u_end; ++piece) {
-        const PagedPiece p = paged_piece<F::kBM, F::kTK>(c, G);
+        const PagedPiece p = paged_piece<F::kBM, F::kTK, kPad>(c, G);
         const int masked = first_masked(c.s, G, c.rt * F::kBM);
         uint32_t (*notes)[4] = sh.notes[piece & 3];
         // the notes of four pieces ago are read: this piece's values were loaded behind products that
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             mbar_arrive(&sh.h_full[shf]);
           }
         }
-        paged_next<F::kBM, F::kTK>(a, c, p);
+        paged_next<F::kBM, F::kTK, kPad>(a, c, p);
       }
     }
   } else {
@@ -585,7 +589,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
         }
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");   // everyone has read the share
-      if (tid == 128) paged_step<F::kBM, F::kTK>(a, share);
+      if (tid == 128) paged_step<F::kBM, F::kTK, kPad>(a, share);
       asm volatile("bar.sync 1, 256;" ::: "memory");
       if (!share.work) break;
     }
@@ -613,7 +617,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
       }
     }
     if (tid == 128) {   // the arrivals that are still owed, so that the counters are zero for the next call
-      for (; share.work; paged_step<F::kBM, F::kTK>(a, share))   // from the piece that was not finished
+      for (; share.work; paged_step<F::kBM, F::kTK, kPad>(a, share))   // from the piece that was not finished
         if (!share.p.whole) paged_arrive_owed(a, share.p);
       atomicOr(a.status, kStatusTimeout);
     }
