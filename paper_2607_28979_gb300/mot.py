@@ -429,8 +429,9 @@ def _batch_fits(h: Handle, batch: mot_paged_batch, where: str) -> int:
     keep, n = getattr(batch, "_keep", None), batch.n
     if keep is not None and getattr(batch, "_fitted", None) != n:
         if 0 < n <= h.paged.max_seqs:   # else nothing is read, or the library refuses it
-            _whole(keep[0], _INT32, n, where, "seqs", h.device)
-            _whole(keep[1], _INT32, n + 1, where, "starts", h.device)
+            dev = h.device
+            _whole(keep[0], _INT32, n, where, "seqs", dev)
+            _whole(keep[1], _INT32, n + 1, where, "starts", dev)
             batch._fitted = n
     return batch.rows
 
@@ -522,18 +523,32 @@ def _row_stride(x, what: str, least=None, where: str = "") -> int:
     raise ValueError(f"{what}: [rows][heads][head_dim] with contiguous rows is wanted")
 
 
+def _rows_at(x, what: str, least, kinds, where: str, dev):
+    """Address and stride of rows x that have to hold ``least`` and to be of one of the types; what is refused is
+    found out by the checks one by one."""
+    shape = x.shape
+    if len(shape) == 3 and shape[0] >= least[0] and shape[1] == least[1] and shape[2] == least[2] and x.dtype in kinds \
+            and x.is_cuda and (dev is None or x.get_device() == dev):
+        row, head, last = x.stride()
+        if last == 1 and (head == least[2] or least[1] == 1):
+            return x.data_ptr(), row if shape[0] > 1 else least[1] * least[2]
+    stride = _row_stride(x, what, least, where)
+    _typed(x, kinds, where, what, dev)
+    return x.data_ptr(), stride
+
+
 def _append(h: Handle, layer, cache, batch, q, k, v, q_out, q_norm, k_norm, stream, where, positions=()) -> None:
     c, dev = _fits(h, cache, where), h.device
     if c is None:
-        sq, sk, sv = (_row_stride(x, what) for x, what in ((q, "q"), (k, "k"), (v, "v")))
+        (q, sq), (k, sk), (v, sv) = ((x.data_ptr(), _row_stride(x, what)) for x, what in ((q, "q"), (k, "k"), (v, "v")))
         positions = [_addr(x) for x in positions]
         q_out, q_norm, k_norm = _addr(q_out), _addr(q_norm), _addr(k_norm)
     else:
         rows, kinds, hq, d = _batch_fits(h, batch, where), _FLOATS[c.dtype], c.q_heads, c.head_dim
         kv = (rows, c.kv_heads, d)
-        sq, sk, sv = _row_stride(q, "q", (rows, hq, d), where), _row_stride(k, "k", kv, where), _row_stride(v, "v", kv, where)
-        for x, what in ((q, "q"), (k, "k"), (v, "v")):
-            _typed(x, kinds, where, what, dev)
+        q, sq = _rows_at(q, "q", (rows, hq, d), kinds, where, dev)
+        k, sk = _rows_at(k, "k", kv, kinds, where, dev)
+        v, sv = _rows_at(v, "v", kv, kinds, where, dev)
         q_out = _whole(q_out, kinds, rows * hq * d, where, "q_out", dev)
         if q_norm is not None:
             q_norm = _whole(q_norm, kinds, d, where, "q_norm", dev)
@@ -544,8 +559,8 @@ def _append(h: Handle, layer, cache, batch, q, k, v, q_out, q_norm, k_norm, stre
             if hasattr(x, "shape") and x.shape[-1] != rows:
                 raise _bad(where, f"positions is {tuple(x.shape)}, {(h.axes, rows)} is wanted")
             positions = (_whole(x, _INT32, h.axes * rows, where, "positions", dev),)
-    status = _calls[where](h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), *positions, q.data_ptr(), sq, k.data_ptr(),
-                           sk, v.data_ptr(), sv, q_norm, k_norm, q_out, _stream(stream))
+    status = _calls[where](h.ptr, int(layer), ctypes.byref(cache), ctypes.byref(batch), *positions, q, sq, k, sk, v, sv, q_norm,
+                           k_norm, q_out, _stream(stream))
     if status:
         _check(status, where)
 
