@@ -534,11 +534,13 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out);
  *                 each page and head, of the page's keys and of its values
  * A value is its 8 bits times the scale. The calls write 2^e, the least e in -60 .. 60
  * that brings the page's largest value to 448 or below, and round once, to the nearest
- * (off by 2^-4 of the value at most; below 2^-6 of the scale the steps stay 2^-9 of it). Where rows join others in a page (mot_paged_append, a page that
- * mot_paged_store fills in part) its scale never falls; where it rises, the rows that
- * were there are rounded again. A page without rows before those has no scale to
- * keep: the memory of the scales needs no initial value. A value that is not finite,
- * or above 448 2^60, is held as NaN and has no part in a scale.
+ * (off by 2^-4 of the value at most; below 2^-6 of the scale the steps stay 2^-9 of it).
+ * Where rows join others in a page (mot_paged_append, a page that mot_paged_store
+ * fills in part) its scale never falls; where it rises, the rows that were there are
+ * rounded again. A page without rows before those has no scale to
+ * keep: the memory of the scales needs no initial value. Scales that the caller
+ * writes are powers of two from 2^-60 to 2^60. A value that is not finite, or above
+ * 448 2^60, is held as NaN and has no part in a scale.
  *
  * A handle of mot_create_paged8 takes every call of a paged one, with queries, new
  * keys and values, outputs and contiguous caches in bf16 (cfg.dtype; fp32:
@@ -591,9 +593,9 @@ mot_status mot_paged_compact(mot_handle h, const mot_paged_cache* cache, int32_t
  * Between a contiguous cache [n_layers][batch][kv_heads][max_seq][head_dim] (the
  * target cache of mot_translate, or a source cache for it) and the pages of
  * layers first_layer .. first_layer + n_layers - 1: batch entry i < n <= batch
- * is slot seqs[i], positions 0 .. lens - 1 (at most max_seq). store writes
- * the pages (of sequences that hold them alone), load the contiguous cache;
- * other positions keep their contents (in 8 bits: but for a scale that rises).
+ * is slot seqs[i], positions 0 .. lens - 1 (at most max_seq). store writes the
+ * pages (of sequences that hold them alone, each given once), load the contiguous
+ * cache; other positions keep their contents (in 8 bits: but for a scale that rises).
  */
 mot_status mot_paged_store(mot_handle h, const mot_paged_cache* cache, int32_t first_layer,
                            int32_t n_layers, const int32_t* seqs, int32_t n, int32_t batch,
@@ -666,8 +668,9 @@ mot_status mot_paged_append_at(mot_handle h, int32_t layer, const mot_paged_cach
  * Over 8-bit pages keys and values enter exactly, a query's elements too (those
  * below 2^-9 of its row's largest are off by 2^-17 of that), and a weight, times the
  * scale of its page's values and beside the row's largest such product, rounded to fp16
- * (2^-11 of it, 2^-25 of the largest at the least). A NaN that is seen gives NaN, in a value for its
- * dimension alone; so does a query that holds one or an infinity, for its whole row.
+ * (2^-11 of it, 2^-25 of the largest at the least). A NaN that is seen gives NaN, in a
+ * value for its dimension alone; so does a query that holds one or an infinity, for its
+ * whole row.
  */
 mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cache* cache,
                                const mot_paged_batch* batch, const void* q, void* out,

@@ -13,8 +13,8 @@ namespace {
 // but the norm's sum), 8 in a row otherwise. A lane's angles and norm weights are the same for every
 // head; fp32 in packed pairs. Angles: F_i = base^(-2 i / rot) / (2 pi) turns per position as a 64-bit
 // fraction, so the upper half of pos * F_i mod 2^64 is the angle in 2^-32 turns (1.5e-9), for any
-// position below 2^30. 10,254 rows of 36 heads of 128, normed and rotated, 39.4 us (4.8 TB/s; bound by
-// loads that stand still while a warp works), in fp32 73.5 (5.1 TB/s); one row 4.4.
+// position below 2^30. 10,254 rows of 36 heads of 128, normed and rotated, 37.4 us (5.1 TB/s; bound by
+// loads that stand still while a warp works), in fp32 73.6 (5.1 TB/s); one row 3.8. With three positions of a row 40.0.
 constexpr int kAppendThreads = 128;
 constexpr int kAppendDepth = 4;   // steps with their loads in flight
 
@@ -218,13 +218,18 @@ __device__ __forceinline__ void append_rows(const PagedDims& d, const PagedCache
     for (int sb = s0; sb < min(sq, s1); sb += kAppendDepth) {
       if (sb != s0) load_q(sb);
 #pragma unroll
-      for (int y = 0; y < kAppendDepth; ++y) {
-        const int st = sb + y;
-        if (st >= min(sq, s1)) break;
-        if (ROT != kRotNone || p.q_norm) work(a[y], b[y], p.q_norm != nullptr, wq);
-        if (st * kAtOnce + sub < d.Hq) {
-          *reinterpret_cast<F*>(q_out + st * kStep) = a[y];
-          *reinterpret_cast<F*>(q_out + st * kStep + ab) = b[y];
+      for (int y0 = 0; y0 < kAppendDepth; y0 += 2) {
+        if (sb + y0 >= min(sq, s1)) break;   // two steps in one run of instructions: 37.4 us, 39.0 one by one
+#pragma unroll
+        for (int y = y0; y < y0 + 2; ++y)
+          if (ROT != kRotNone || p.q_norm) work(a[y], b[y], p.q_norm != nullptr, wq);
+#pragma unroll
+        for (int y = y0; y < y0 + 2; ++y) {
+          const int st = sb + y;
+          if (st < min(sq, s1) && st * kAtOnce + sub < d.Hq) {
+            *reinterpret_cast<F*>(q_out + st * kStep) = a[y];
+            *reinterpret_cast<F*>(q_out + st * kStep + ab) = b[y];
+          }
         }
       }
     }
@@ -282,12 +287,17 @@ auto append_kernel(const PagedDims& d, const PagedAxes& ax) {
 
 // ---------------------------------------------------------------- 8-bit pages
 //
-// Queries as above, by the first blocks of the grid. The others take units (entry, page, head of keys or of
-// values): the new rows of one page, whose scale wants the largest of them before the first is written. A block
-// takes 8 or 16 of the rows at a time, d / 8 lanes to a row and the lane's pairs turned by angles of its own (a row
-// of one head has each angle once); twice, for the scale and to write, where they are more than that (the second
-// time from the cache). Units are dealt out by a scan of the entries in every block, or, with one row to an entry
-// (or few, and many entries), by the row.
+// Queries as above, by some blocks of the grid. The others take units (entry, page, head of keys or of values):
+// the new rows of one page, whose scale wants the largest of them before the first is written. A block takes 8 or
+// 16 of the rows at a time, d / 8 lanes to a row and the lane's pairs turned by angles of its own (a row of one head
+// has each angle once). What comes out waits for the scale in fp32: in registers where that is all, else in shared
+// memory, a lane's own (kHeld rows; those behind them, of pages of 128 rows of 128, are worked out a second time).
+// Units are dealt out by a scan of the entries in every block, or, with one row to an entry (or few, and many
+// entries), by the row. Bound by instructions, and loads that stand still beside them: 10,254 rows of 28 heads on 4
+// of 128, normed and turned, pages of 64, 46.6 us (3.8 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
+// of 64, pages of 128, 33.5 (52.2); five blocks per SM (47.9 and 36.6 before the order below; six 49.3 and 39.4, four
+// 54.3 and 38.9). One row for each of 64 sequences 3.8.
+constexpr int kHeld = 8;   // rows of a lane that wait in shared memory for their scale
 template <int D, int ROT, bool AXES>
 struct Rows8 {
   static constexpr int kLph = D / 8, kAtOnce = kAppendThreads / kLph;   // lanes of a row, rows at a time
@@ -363,7 +373,8 @@ struct Rows8 {
 
   // The `rows` new rows from `row` on, at position pos (of one page) and on, of unit g. By the whole block.
   __device__ __forceinline__ void page(const PagedDims& d, const PagedCache& c, const PagedAppend& p, int32_t* status,
-                                       float* top, int slot, int row, int pos, int rows, int g) const {
+                                       float* top, float4 (*held)[kAppendThreads], int slot, int row, int pos, int rows,
+                                       int g) const {
     using F = Four<uint16_t>;
     const int page = paged_entry(d, c.table, status, slot, pos);
     if (page < 0) return;
@@ -377,8 +388,8 @@ struct Rows8 {
     const float was = old ? *place : 0.f;
     constexpr int kAhead = 4;   // rows of a lane with their loads in flight
     float x[8], big = 0.f;
-    auto each = [&](auto&& use) {
-      for (int r0 = sub; r0 < rows + sub; r0 += kAhead * kAtOnce) {   // as often for every lane
+    auto each = [&](int from, auto&& use) {
+      for (int r0 = from + sub; r0 < rows + sub; r0 += kAhead * kAtOnce) {   // as often for every lane
         F raw[kAhead][2];
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
@@ -399,11 +410,16 @@ struct Rows8 {
         }
       }
     };
-    each([&](int r) {
-      if (r < rows)
+    each(0, [&](int r) {
+      if (r >= rows) return;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (held8(x[k])) big = fmaxf(big, fabsf(x[k]));
+      for (int k = 0; k < 8; ++k)
+        if (held8(x[k])) big = fmaxf(big, fabsf(x[k]));
+      if (r < kHeld * kAtOnce && rows > kAtOnce) {   // for this lane, behind the scale
+        const int e = r / kAtOnce;
+        held[2 * e][threadIdx.x] = make_float4(x[0], x[1], x[2], x[3]);
+        held[2 * e + 1][threadIdx.x] = make_float4(x[4], x[5], x[6], x[7]);
+      }
     });
 #pragma unroll
     for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
@@ -427,8 +443,18 @@ struct Rows8 {
       *reinterpret_cast<uint32_t*>(to + eA) = pack8(y[0], y[1], y[2], y[3]);
       *reinterpret_cast<uint32_t*>(to + eB) = pack8(y[4], y[5], y[6], y[7]);
     };
-    if (rows <= kAtOnce) write(sub);   // x is still there
-    else each(write);
+    if (rows <= kAtOnce) {   // x is still there
+      write(sub);
+    } else {
+#pragma unroll 4
+      for (int e = 0; e < kHeld && e * kAtOnce < rows; ++e) {
+        const float4 u = held[2 * e][threadIdx.x], v = held[2 * e + 1][threadIdx.x];
+        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+        x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+        write(e * kAtOnce + sub);
+      }
+      if (rows > kHeld * kAtOnce) each(kHeld * kAtOnce, write);
+    }
     __syncthreads();   // top is read
   }
 };
@@ -443,25 +469,27 @@ __device__ __forceinline__ Touched8 touched8(const PagedDims& d, const PagedSeq&
 }
 
 template <int D, int ROT, bool AXES>
-__global__ void __launch_bounds__(kAppendThreads, 6)
+__global__ void __launch_bounds__(kAppendThreads, 5)
     paged_append8_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w,
                          const __grid_constant__ PagedAxes ax, int q_blocks, int rows_each, int parts, int by_row) {
   __shared__ float top[kAppendThreads / 32];
+  __shared__ float4 held[2 * kHeld][kAppendThreads];
   __shared__ int64_t sh[33];
   __shared__ int64_t s_at;
   __shared__ int s_i;
   if (refused(w.status)) return;
   const int tid = threadIdx.x;
-  // blocks of the queries evenly among those of the pages: one kind streams while the other waits on its few loads
-  const int64_t q0 = int64_t(blockIdx.x) * q_blocks / gridDim.x, q1 = (int64_t(blockIdx.x) + 1) * q_blocks / gridDim.x;
-  if (q0 != q1) {
+  // blocks of the pages first, whose shares are the longest; those of the queries behind fill the gaps (the example above:
+  // 46.6 and 33.5 us; the other way round 47.1 and 36.1)
+  const int block = blockIdx.x, blocks = int(gridDim.x) - q_blocks;
+  if (block >= blocks) {
     PagedDims dq = d;
     dq.H = 0;   // queries alone
-    append_rows<uint16_t, D, ROT, AXES>(dq, c, p, w, ax, int(q0) * (kAppendThreads / 32) + (tid >> 5), rows_each, parts);
+    append_rows<uint16_t, D, ROT, AXES>(dq, c, p, w, ax, (block - blocks) * (kAppendThreads / 32) + (tid >> 5), rows_each,
+                                        parts);
     return;
   }
   const Rows8<D, ROT, AXES> lanes(d, p, ax);
-  const int64_t block = int(blockIdx.x) - q0, blocks = int(gridDim.x) - q_blocks;
   const int G = 2 * d.H, n = p.b.n;
   if (by_row) {   // a unit for each row that is the first of its entry or of a page
     for (int64_t u = block; u < int64_t(p.b.rows) * G; u += blocks) {
@@ -470,7 +498,7 @@ __global__ void __launch_bounds__(kAppendThreads, 6)
       const int from = s.len - s.m, pos = from + row - s.r0;
       if (s.slot < 0 || row < s.r0 || row >= s.r0 + s.m || pos < 0) continue;   // the queries' blocks report it
       if (row != s.r0 + max(0, -from) && (pos & (d.P - 1))) continue;
-      lanes.page(d, c, p, w.status, top, s.slot, row, pos, min(d.P - (pos & (d.P - 1)), s.len - pos), g);
+      lanes.page(d, c, p, w.status, top, held, s.slot, row, pos, min(d.P - (pos & (d.P - 1)), s.len - pos), g);
     }
     return;
   }
@@ -508,7 +536,8 @@ __global__ void __launch_bounds__(kAppendThreads, 6)
     }
     const int j = int(in / G), g = int(in - int64_t(j) * G);
     const int pos = j ? ((t.first >> d.lp) + j) << d.lp : t.first;
-    lanes.page(d, c, p, w.status, top, s.slot, s.r0 + pos - (s.len - s.m), pos, min(d.P - (pos & (d.P - 1)), s.len - pos), g);
+    const int rows = min(d.P - (pos & (d.P - 1)), s.len - pos);
+    lanes.page(d, c, p, w.status, top, held, s.slot, s.r0 + pos - (s.len - s.m), pos, rows, g);
   }
 }
 
@@ -527,7 +556,8 @@ cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const P
   constexpr int kWarps = kAppendThreads / 32;
   const int at_once = 256 / d.d, kv = d.b8 ? 0 : d.H;
   const int steps = (d.Hq + at_once - 1) / at_once + (kv + at_once - 1) / at_once;
-  const int64_t fill = int64_t(num_sms) * 24 * (d.b8 ? 2 : 1);   // warps that are resident; in shares that mix with the pages'
+  // warps that are resident; in 8 bits smaller shares, behind those of the pages
+  const int64_t fill = int64_t(num_sms) * 24 * (d.b8 ? 2 : 1);
   const int most = (steps + kAppendDepth - 1) / kAppendDepth;
   const int parts = p.b.rows >= fill ? 1 : int(fill / p.b.rows < most ? fill / p.b.rows : most);
   const int rows_each = int((p.b.rows * int64_t(parts) + fill - 1) / fill);
