@@ -668,6 +668,41 @@ def test_from_a_translated_context_to_branches_that_grow():
     assert c.status() == M.MOT_OK
 
 
+def test_two_handles_on_two_streams_serve_one_cache():
+    """Sequences of one cache under a handle of their own each, at the same time: both give what they give alone."""
+    shape = dict(q_heads=6, kv_heads=2, d=128, page=32, n_pages=200, max_seqs=8, max_pages=64)
+    c = P8.Cache(**shape)
+    other = M.mot_create_paged8(M.make_paged_config(1, *shape.values()))
+    c.reserve(list(range(6)), [900, 33, 700, 1500, 64, 5])
+    parts = []
+    for h, seqs, new in ((c.h, [0, 1, 2], [200, 1, 30]), (other, [3, 4, 5], [100, 2, 5]), (c.h, [2, 0], [1, 1]), (other, [5, 3], [1, 1])):
+        rows = sum(new)
+        x = c.normal(rows, 10, 128)
+        q, out = (torch.zeros((rows, 6, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        parts.append((h, c.batch(seqs, new), x, q, out, torch.cuda.Stream()))
+
+    def step(part, stream):
+        h, b, x, q, out, _ = part
+        M.mot_paged_append(h, 0, c.c, b, x[:, :6], x[:, 6:8], x[:, 8:], q, stream=stream)
+        M.mot_paged_attention(h, 0, c.c, b, q, out, stream=stream)
+
+    for a, b in (parts[:2], parts[2:]):   # chunks, then single tokens
+        for part in (a, b):
+            step(part, None)
+        torch.cuda.synchronize()
+        want = [part[4].clone() for part in (a, b)], c.bytes()
+        for _ in range(20):
+            for part in (a, b):
+                part[4].zero_()
+            torch.cuda.synchronize()
+            for part in (a, b):
+                step(part, part[5])
+            torch.cuda.synchronize()
+            for x, y in zip([part[4] for part in (a, b)] + c.bytes(), want[0] + want[1]):
+                assert torch.equal(x, y)
+    assert c.status() == M.MOT_OK and M.mot_get_device_status(other) == M.MOT_OK
+
+
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right():
     """The first block loads nothing: every wait of the kernel ends, and nothing is left behind for the next call."""
     for d, new in ((64, 300), (128, 300), (64, 1), (128, 1), (128, 5)):
