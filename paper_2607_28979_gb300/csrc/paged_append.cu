@@ -13,10 +13,17 @@ namespace {
 // but the norm's sum), 8 in a row otherwise. A lane's angles and norm weights are the same for every
 // head; fp32 in packed pairs. Angles: F_i = base^(-2 i / rot) / (2 pi) turns per position as a 64-bit
 // fraction, so the upper half of pos * F_i mod 2^64 is the angle in 2^-32 turns (1.5e-9), for any
-// position below 2^30. 10,254 rows of 36 heads of 128, normed and rotated, 37.4 us (5.1 TB/s; bound by
-// loads that stand still while a warp works), in fp32 73.6 (5.1 TB/s); one row 3.8. With three positions of a row 40.0.
+// position below 2^30. 10,254 rows of 36 heads of 128, normed and rotated, 37.3 us (5.1 TB/s; bound by
+// loads that stand still while a warp works), in fp32 69.8 (5.4 TB/s); one row 3.7. With three positions of a row 40.0.
 constexpr int kAppendThreads = 128;
-constexpr int kAppendDepth = 4;   // steps with their loads in flight
+// Steps with their loads in flight, and blocks per SM: in 16 bits 4 and 6 (10,254 rows with three positions: 39.7 us; 4
+// and 5 44.0, 6 and 6 42.6, 8 and 5 41.3, 2 and 8 47.1), in fp32 4 and 5 (2,200 rows of 36 heads of 64: 11.8 us; 6 blocks
+// 12.7, with spills), where queries go alone beside 8-bit pages 6 and 5 (44.9 us of the example there; 4 46.4, 8 44.3,
+// but 34.5 for 33.3 with few heads).
+constexpr int kDepth = 4, kDepth8 = 6;
+template <class T>
+constexpr int kAppendBlocks = sizeof(T) == 4 ? 5 : 6;
+constexpr int kAppendBlocks8 = 5;
 
 template <class T>
 struct Four;   // four elements, as two pairs of fp32
@@ -76,11 +83,13 @@ __device__ __forceinline__ float2 cos_sin_turns(uint32_t t) {
   return make_float2((quarter + 1u) & 2u ? -c : c, quarter & 2u ? -s : s);
 }
 
-// Rows `unit` of the call. AXES: a pair turns by the caller's position of its axis, ax.at[axis][row], else by the
+// Rows `unit` of the call; none where a change before it was refused (stop: its load is under way beside the first
+// others). AXES: a pair turns by the caller's position of its axis, ax.at[axis][row], else by the
 // row's place in its sequence.
-template <class T, int D, int ROT, bool AXES>
+template <class T, int D, int ROT, bool AXES, int kAppendDepth>
 __device__ __forceinline__ void append_rows(const PagedDims& d, const PagedCache& c, const PagedAppend& p,
-                                            const PagedWork& w, const PagedAxes& ax, int unit, int rows_each, int parts) {
+                                            const PagedWork& w, const PagedAxes& ax, bool stop, int unit, int rows_each,
+                                            int parts) {
   using F = Four<T>;
   constexpr int kLph = D / 8, kAtOnce = 32 / kLph, kStep = kAtOnce * D;   // lanes per head; heads and elements of a step
   __shared__ __align__(16) float2 cs[kAppendThreads / 32][D / 2];        // cos, sin of a row's angles
@@ -134,6 +143,7 @@ __device__ __forceinline__ void append_rows(const PagedDims& d, const PagedCache
         }
     };
     load_q(s0);   // under way while the row's place is found
+    if (stop) return;
     const bool fresh = row < first || row >= last;
     if (fresh) {
       const int i = entry_of(p.b.starts, p.b.n, row);
@@ -268,11 +278,11 @@ __device__ __forceinline__ void append_rows(const PagedDims& d, const PagedCache
 }
 
 template <class T, int D, int ROT, bool AXES>
-__global__ void __launch_bounds__(kAppendThreads, 6)
+__global__ void __launch_bounds__(kAppendThreads, kAppendBlocks<T>)
     paged_append_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w,
                         const __grid_constant__ PagedAxes ax, int rows_each, int parts) {
-  if (refused(w.status)) return;
-  append_rows<T, D, ROT, AXES>(d, c, p, w, ax, blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5), rows_each, parts);
+  append_rows<T, D, ROT, AXES, kDepth>(d, c, p, w, ax, refused(w.status),
+                                       blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5), rows_each, parts);
 }
 
 template <class T, int D, bool AXES>
@@ -294,9 +304,9 @@ auto append_kernel(const PagedDims& d, const PagedAxes& ax) {
 // memory, a lane's own (kHeld rows; those behind them, of pages of 128 rows of 128, are worked out a second time).
 // Units are dealt out by a scan of the entries in every block, or, with one row to an entry (or few, and many
 // entries), by the row. Bound by instructions, and loads that stand still beside them: 10,254 rows of 28 heads on 4
-// of 128, normed and turned, pages of 64, 46.6 us (3.8 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
-// of 64, pages of 128, 33.5 (52.2); five blocks per SM (47.9 and 36.6 before the order below; six 49.3 and 39.4, four
-// 54.3 and 38.9). One row for each of 64 sequences 3.8.
+// of 128, normed and turned, pages of 64, 44.3 us (4.0 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
+// of 64, pages of 128, 32.5 (52.2). Five blocks per SM 47.9 and 36.6 before the order below, six 49.3 and 39.4, four
+// 54.3 and 38.9. One row for each of eight sequences 3.7.
 constexpr int kHeld = 8;   // rows of a lane that wait in shared memory for their scale
 template <int D, int ROT, bool AXES>
 struct Rows8 {
@@ -376,31 +386,35 @@ struct Rows8 {
                                        float* top, float4 (*held)[kAppendThreads], int slot, int row, int pos, int rows,
                                        int g) const {
     using F = Four<uint16_t>;
-    const int page = paged_entry(d, c.table, status, slot, pos);
-    if (page < 0) return;
     const bool key = g < d.H;
     const int hk = key ? g : g - d.H, old = pos & (d.P - 1), sub = threadIdx.x / kLph;
+    const uint16_t* src = static_cast<const uint16_t*>(key ? p.k : p.v) + hk * D;
+    const int64_t stride = key ? p.k_stride : p.v_stride;
+    constexpr int kAhead = 4;   // rows of a lane with their loads in flight
+    F raw[kAhead][2];
+    auto load = [&](int r0) {
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        const int r = r0 + e * kAtOnce;
+        raw[e][0].u = raw[e][1].u = make_uint2(0u, 0u);
+        if (r < rows) {
+          const uint16_t* s = src + (row + r) * stride;
+          raw[e][0] = *reinterpret_cast<const F*>(s + eA);
+          raw[e][1] = *reinterpret_cast<const F*>(s + eB);
+        }
+      }
+    };
+    load(sub);   // under way while the page is found
+    const int page = paged_entry(d, c.table, status, slot, pos);
+    if (page < 0) return;
     const int64_t at_head = (int64_t(p.layer) * d.n_pages + page) * d.H + hk;
     float* place = (key ? c.ks : c.vs) + at_head;
     uint8_t* dst = static_cast<uint8_t*>(key ? c.k : c.v) + (at_head << d.lp) * D;
-    const uint16_t* src = static_cast<const uint16_t*>(key ? p.k : p.v) + hk * D;
-    const int64_t stride = key ? p.k_stride : p.v_stride;
     const float was = old ? *place : 0.f;
-    constexpr int kAhead = 4;   // rows of a lane with their loads in flight
     float x[8], big = 0.f;
     auto each = [&](int from, auto&& use) {
       for (int r0 = from + sub; r0 < rows + sub; r0 += kAhead * kAtOnce) {   // as often for every lane
-        F raw[kAhead][2];
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) {
-          const int r = r0 + e * kAtOnce;
-          raw[e][0].u = raw[e][1].u = make_uint2(0u, 0u);
-          if (r < rows) {
-            const uint16_t* s = src + (row + r) * stride;
-            raw[e][0] = *reinterpret_cast<const F*>(s + eA);
-            raw[e][1] = *reinterpret_cast<const F*>(s + eB);
-          }
-        }
+        if (r0 != sub) load(r0);
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
           const int r = r0 + e * kAtOnce;
@@ -469,7 +483,7 @@ __device__ __forceinline__ Touched8 touched8(const PagedDims& d, const PagedSeq&
 }
 
 template <int D, int ROT, bool AXES>
-__global__ void __launch_bounds__(kAppendThreads, 5)
+__global__ void __launch_bounds__(kAppendThreads, kAppendBlocks8)
     paged_append8_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w,
                          const __grid_constant__ PagedAxes ax, int q_blocks, int rows_each, int parts, int by_row) {
   __shared__ float top[kAppendThreads / 32];
@@ -477,19 +491,20 @@ __global__ void __launch_bounds__(kAppendThreads, 5)
   __shared__ int64_t sh[33];
   __shared__ int64_t s_at;
   __shared__ int s_i;
-  if (refused(w.status)) return;
+  const bool stop = refused(w.status);   // looked at behind the first loads
   const int tid = threadIdx.x;
-  // blocks of the pages first, whose shares are the longest; those of the queries behind fill the gaps (the example above:
-  // 46.6 and 33.5 us; the other way round 47.1 and 36.1)
+  // blocks of the pages first, whose shares are the longest; those of the queries behind fill the gaps (46.6 and 33.5 us of
+  // the examples above, then; the other way round 47.1 and 36.1)
   const int block = blockIdx.x, blocks = int(gridDim.x) - q_blocks;
   if (block >= blocks) {
     PagedDims dq = d;
     dq.H = 0;   // queries alone
-    append_rows<uint16_t, D, ROT, AXES>(dq, c, p, w, ax, (block - blocks) * (kAppendThreads / 32) + (tid >> 5), rows_each,
-                                        parts);
+    append_rows<uint16_t, D, ROT, AXES, kDepth8>(dq, c, p, w, ax, stop, (block - blocks) * (kAppendThreads / 32) + (tid >> 5),
+                                                 rows_each, parts);
     return;
   }
   const Rows8<D, ROT, AXES> lanes(d, p, ax);
+  if (stop) return;
   const int G = 2 * d.H, n = p.b.n;
   if (by_row) {   // a unit for each row that is the first of its entry or of a page
     for (int64_t u = block; u < int64_t(p.b.rows) * G; u += blocks) {
@@ -557,8 +572,8 @@ cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const P
   const int at_once = 256 / d.d, kv = d.b8 ? 0 : d.H;
   const int steps = (d.Hq + at_once - 1) / at_once + (kv + at_once - 1) / at_once;
   // warps that are resident; in 8 bits smaller shares, behind those of the pages
-  const int64_t fill = int64_t(num_sms) * 24 * (d.b8 ? 2 : 1);
-  const int most = (steps + kAppendDepth - 1) / kAppendDepth;
+  const int64_t fill = int64_t(num_sms) * (d.b8 ? 48 : kWarps * (d.dtype ? kAppendBlocks<float> : kAppendBlocks<uint16_t>));
+  const int depth = d.b8 ? kDepth8 : kDepth, most = (steps + depth - 1) / depth;
   const int parts = p.b.rows >= fill ? 1 : int(fill / p.b.rows < most ? fill / p.b.rows : most);
   const int rows_each = int((p.b.rows * int64_t(parts) + fill - 1) / fill);
   const int64_t units = (int64_t(p.b.rows) + rows_each - 1) / rows_each * parts;
