@@ -2009,7 +2009,7 @@ mot_status paged_slots(mot_handle h, const PagedCache& c, const int32_t* seqs, i
   return MOT_OK;
 }
 
-mot_status paged_copy(mot_handle h, const mot_paged_cache* cache, const PagedCopy& p, cudaStream_t st) {
+mot_status paged_copy(mot_handle h, const mot_paged_cache* cache, PagedCopy p, cudaStream_t st) {
   PagedCache c;
   mot_status r = paged_args(h, cache, c);
   if (r != MOT_OK) return r;
@@ -2029,6 +2029,7 @@ mot_status paged_copy(mot_handle h, const mot_paged_cache* cache, const PagedCop
   }
   if (cudaSetDevice(h->device) != cudaSuccess) return MOT_ERR_CUDA;
   if (p.n == 0) return MOT_OK;
+  p.early = !h->profile;
   MOT_CUDA_TRY(timed(h, p.store ? "paged_store" : "paged_load", st,
                      [&] { return (d.b8 ? launch_paged8_copy : launch_paged_copy)(d, c, p, h->pw, h->num_sms, st); }));
   return MOT_OK;
@@ -2166,6 +2167,7 @@ mot_status paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cach
   p.freq = h->pfreq;
   p.q_out = q_out;
   // (many entries of a few rows: a scan of all of them in every block would cost more than rows that are no page's first)
+  p.early = !h->profile;
   p.by_row = batch->max_chunk <= 1 || (p.b.n > 1024 && batch->max_chunk <= 16);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   MOT_CUDA_TRY(timed(h, "paged_append", st,
@@ -2241,6 +2243,7 @@ mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cach
   a.status = h->status;
   a.max_chunk = batch->max_chunk;
   a.wait_limit = h->wait_limit;
+  a.early = !h->profile;
   a.stall_test = h->stall_test;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (d.b8) {

@@ -43,6 +43,7 @@ __global__ void __launch_bounds__(kThreads8, 4)
     paged8_store_kernel(const PagedDims d, const PagedCache c, const PagedCopy p, const PagedWork w) {
   constexpr int kRow = D / 8;   // loads of a row
   __shared__ float top[kThreads8 / 32];
+  pdl_wait();
   if (refused(w.status)) return;
   const int n_vec = d.P * kRow, T = max(32, n_vec / kVecs), teams = kThreads8 / T;
   const int team = threadIdx.x / T, t = threadIdx.x % T, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -124,6 +125,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads8)
     paged8_load_kernel(const PagedDims d, const PagedCache c, const PagedCopy p, const PagedWork w) {
   constexpr int kRow = D / 16;   // 16-byte loads of a row
+  pdl_wait();
   const int per_seq = ((p.S - 1) >> d.lp) + 1;
   const int64_t items = int64_t(per_seq) * p.n * p.n_layers;
   const int n_vec = 2 * d.H * d.P * kRow, run = d.P * kRow;
@@ -175,13 +177,13 @@ cudaError_t launch_paged8_copy(const PagedDims& d, const PagedCache& c, const Pa
   // stored in 321 us (339 with as many as are resident) and loaded in 322 (357)
   if (!p.store) {
     const int64_t most = int64_t(num_sms) * 32;
-    return launch_kernel(false, d.d == 64 ? paged8_load_kernel<64> : paged8_load_kernel<128>, int(items < most ? items : most),
-                         kThreads8, 0, st, d, c, p, w);
+    return launch_kernel(p.early, d.d == 64 ? paged8_load_kernel<64> : paged8_load_kernel<128>,
+                         int(items < most ? items : most), kThreads8, 0, st, d, c, p, w);
   }
   const int T = d.P * d.d / 64 > 32 ? d.P * d.d / 64 : 32, teams = kThreads8 / T;
   const int64_t blocks = (items * 2 * d.H + teams - 1) / teams, most = int64_t(num_sms) * 16;
-  return launch_kernel(false, d.d == 64 ? paged8_store_kernel<64> : paged8_store_kernel<128>, int(blocks < most ? blocks : most),
-                       kThreads8, 0, st, d, c, p, w);
+  return launch_kernel(p.early, d.d == 64 ? paged8_store_kernel<64> : paged8_store_kernel<128>,
+                       int(blocks < most ? blocks : most), kThreads8, 0, st, d, c, p, w);
 }
 
 }  // namespace mot

@@ -124,6 +124,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
   }
+  pdl_wait();
   paged_begin<BM, TK, kPad>(a, kLeast, kMost, scan, shares[0], true);
   if (!shares[0].work) return;
   uint32_t tile = 0;   // of this CTA so far
@@ -500,7 +501,7 @@ cudaError_t launch_decode(const PagedAttnArgs& a, const CUtensorMap& tmK, const 
   static SmemOptIn opt_in;
   auto kern = paged8_decode_kernel<D, NT>;
   if (cudaError_t e = opt_in(kern, F::kSmem)) return e;
-  return launch_kernel(false, kern, num_sms * F::kResident, kDecThreads, F::kSmem, st, tmK, tmV, a);
+  return launch_kernel(a.early, kern, num_sms * F::kResident, kDecThreads, F::kSmem, st, tmK, tmV, a);
 }
 
 }  // namespace

@@ -17,7 +17,7 @@
 //                                    the sum (w 2^-e beside 2^-e' of the row's largest), and are not flushed to 0.
 //                       Bound by the chain of products and softmax, with shared memory near its limit beside it (both parts
 //                       of Q and the keys are read from it twice, the values three times): 4,096 tokens of 28 heads on 4
-//                       of 128 on 32,768 positions 1,313 us (1,374 TFLOP/s; 1,175 were the values in fp16 already).
+//                       of 128 on 32,768 positions 1,303 us (1,385 TFLOP/s; 1,175 were the values in fp16 already).
 //                       Every wait is bounded; on a timeout the roles unwind, copies and MMAs in flight are drained,
 //                       TMEM is freed and kStatusTimeout is raised.
 #include "paged_chunk.cuh"
@@ -133,6 +133,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
   }
+  pdl_wait();
   if (warp == 2) {
     tmem_alloc(&sh.tmem, 512);
     tmem_relinquish();
@@ -141,6 +142,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();   // tensor memory is taken
   const uint32_t tmem = sh.tmem;
   if (!share.work) {   // uniform over the CTA
     if (warp == 2) tmem_dealloc(tmem, 512);
@@ -640,7 +642,7 @@ cudaError_t launch_paged8_fmha(const PagedAttnArgs& a, const CUtensorMap& tmK, c
   auto kern = a.d.d == 128 ? paged8_fmha_kernel<128> : paged8_fmha_kernel<64>;
   const int smem = a.d.d == 128 ? Pf8<128>::kSmem : Pf8<64>::kSmem;
   if (cudaError_t e = opt_in[a.d.d == 128](kern, smem)) return e;
-  return launch_kernel(false, kern, num_sms, Pf8<128>::kThreads, smem, st, tmK, tmV, a);
+  return launch_kernel(a.early, kern, num_sms, Pf8<128>::kThreads, smem, st, tmK, tmV, a);
 }
 
 }  // namespace mot

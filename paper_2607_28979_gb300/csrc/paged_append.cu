@@ -14,7 +14,7 @@ namespace {
 // head; fp32 in packed pairs. Angles: F_i = base^(-2 i / rot) / (2 pi) turns per position as a 64-bit
 // fraction, so the upper half of pos * F_i mod 2^64 is the angle in 2^-32 turns (1.5e-9), for any
 // position below 2^30. 10,254 rows of 36 heads of 128, normed and rotated, 37.3 us (5.1 TB/s; bound by
-// loads that stand still while a warp works), in fp32 69.8 (5.4 TB/s); one row 3.7. With three positions of a row 40.0.
+// loads that stand still while a warp works), in fp32 69.8 (5.4 TB/s); one row 3.7. With three positions of a row 39.9.
 constexpr int kAppendThreads = 128;
 // Steps with their loads in flight, and blocks per SM: in 16 bits 4 and 6 (10,254 rows with three positions: 39.7 us; 4
 // and 5 44.0, 6 and 6 42.6, 8 and 5 41.3, 2 and 8 47.1), in fp32 4 and 5 (2,200 rows of 36 heads of 64: 11.8 us; 6 blocks
@@ -281,6 +281,7 @@ template <class T, int D, int ROT, bool AXES>
 __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks<T>)
     paged_append_kernel(const PagedDims d, const PagedCache c, const PagedAppend p, const PagedWork w,
                         const __grid_constant__ PagedAxes ax, int rows_each, int parts) {
+  pdl_wait();
   append_rows<T, D, ROT, AXES, kDepth>(d, c, p, w, ax, refused(w.status),
                                        blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5), rows_each, parts);
 }
@@ -304,9 +305,9 @@ auto append_kernel(const PagedDims& d, const PagedAxes& ax) {
 // memory, a lane's own (kHeld rows; those behind them, of pages of 128 rows of 128, are worked out a second time).
 // Units are dealt out by a scan of the entries in every block, or, with one row to an entry (or few, and many
 // entries), by the row. Bound by instructions, and loads that stand still beside them: 10,254 rows of 28 heads on 4
-// of 128, normed and turned, pages of 64, 44.3 us (4.0 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
-// of 64, pages of 128, 32.5 (52.2). Five blocks per SM 47.9 and 36.6 before the order below, six 49.3 and 39.4, four
-// 54.3 and 38.9. One row for each of eight sequences 3.7.
+// of 128, normed and turned, pages of 64, 43.9 us (4.1 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
+// of 64, pages of 128, 32.2 (52.2). Five blocks per SM 47.9 and 36.6 before the order below, six 49.3 and 39.4, four
+// 54.3 and 38.9. One row for each of eight sequences 3.6.
 constexpr int kHeld = 8;   // rows of a lane that wait in shared memory for their scale
 template <int D, int ROT, bool AXES>
 struct Rows8 {
@@ -491,6 +492,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks8)
   __shared__ int64_t sh[33];
   __shared__ int64_t s_at;
   __shared__ int s_i;
+  pdl_wait();
   const bool stop = refused(w.status);   // looked at behind the first loads
   const int tid = threadIdx.x;
   // blocks of the pages first, whose shares are the longest; those of the queries behind fill the gaps (46.6 and 33.5 us of
@@ -584,12 +586,12 @@ cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const P
     const int64_t blocks = std::min((p.by_row ? int64_t(p.b.rows) : pages) * 2 * d.H, int64_t(num_sms) * 16);
     auto kern = d.d == 64 ? (ax.at ? append8_kernel<64, true>(d) : append8_kernel<64, false>(d))
                           : (ax.at ? append8_kernel<128, true>(d) : append8_kernel<128, false>(d));
-    return launch_kernel(false, kern, int(grid + blocks), kAppendThreads, 0, st, d, c, p, w, ax, grid, rows_each, parts,
+    return launch_kernel(p.early, kern, int(grid + blocks), kAppendThreads, 0, st, d, c, p, w, ax, grid, rows_each, parts,
                          int(p.by_row));
   }
   auto kern = d.dtype == 0 ? (d.d == 64 ? append_kernel<uint16_t, 64>(d, ax) : append_kernel<uint16_t, 128>(d, ax))
                            : (d.d == 64 ? append_kernel<float, 64>(d, ax) : append_kernel<float, 128>(d, ax));
-  return launch_kernel(false, kern, grid, kAppendThreads, 0, st, d, c, p, w, ax, rows_each, parts);
+  return launch_kernel(p.early, kern, grid, kAppendThreads, 0, st, d, c, p, w, ax, rows_each, parts);
 }
 
 }  // namespace mot

@@ -72,6 +72,7 @@ struct PagedCopy {
   void* k;
   void* v;
   bool store;
+  bool early;   // 8-bit pages: the launch may overlap the kernel before it
 };
 cudaError_t launch_paged_copy(const PagedDims& d, const PagedCache& c, const PagedCopy& p,
                               const PagedWork& w, int num_sms, cudaStream_t st);
@@ -89,6 +90,7 @@ struct PagedAppend {
   const uint64_t* freq;             // [rot / 2]: turns per position in units of 2^-64
   void* q_out;                      // [rows][Hq][d]
   bool by_row;                      // 8-bit pages: units by the row, for entries of one row or of few (a hint)
+  bool early;                       // the launch may overlap the kernel before it
 };
 // Rotation by several positions: pair i of a row turns by at[axis[i]][row] times freq[i] 2^-64 turns. at null: by
 // the row's place in its sequence.
@@ -120,6 +122,7 @@ struct PagedAttnArgs {
   int32_t max_chunk;      // most rows of an entry: a hint for the split, never relied on
   long long wait_limit;   // bound of every pipeline wait (SM cycles)
   int32_t stall_test;     // test hook: the tensor-core kernel's first CTA loads nothing
+  bool early;             // 8-bit pages: the launch may overlap the kernel before it
 };
 constexpr int kPagedMaxGroup = 16;   // query heads per key/value head
 size_t paged_part_floats(const PagedDims& d, int num_sms);

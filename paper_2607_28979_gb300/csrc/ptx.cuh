@@ -163,9 +163,11 @@ __device__ __forceinline__ void st_global_v8(void* dst, const uint32_t* p) {
 // are visible. Everything before it touches nothing that another kernel of the call writes. Every
 // CTA calls it, also one without work: a grid whose CTAs all leave without waiting may be complete
 // before its predecessor is, and the next call is ordered behind that grid alone.
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_enter() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  pdl_trigger();
+  pdl_wait();
 }
 
 // What the kernel before this one wrote: a coherent load, behind pdl_enter. __ldg's non-coherent one

@@ -703,6 +703,61 @@ def test_two_handles_on_two_streams_serve_one_cache():
     assert c.status() == M.MOT_OK and M.mot_get_device_status(other) == M.MOT_OK
 
 
+@pytest.mark.parametrize("new", [[1, 1, 1], [150, 3, 40]])
+def test_a_captured_step_behind_work_of_two_streams(new):
+    """Calls whose launches may begin before the kernels in front of them have ended see what these write: inputs that
+    two streams make, pages that the call before has written, one replay after another."""
+    H, Hq, d = 2, 6, 128
+    seqs, rows = [0, 1, 2], sum(new)
+    pair = []
+    for _ in range(2):
+        c = P8.Cache(q_heads=Hq, kv_heads=H, d=d, page=32, n_pages=120, max_pages=32, rot_dim=d, seed=7)
+        c.reserve(seqs + [3], [m + x for m, x in zip(new, (300, 33, 700))] + [90])
+        x = c.normal(rows, Hq + 2 * H, d)
+        flat, back = [[torch.zeros((1, 1, H, 90, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2)]
+        q, out = (torch.zeros((rows, Hq, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        pair.append((c, x, flat, back, q, out, c.batch(seqs, new), i32([3]), x.clone(), flat[0].clone()))
+
+    def step(s, side):
+        c, x, flat, back, q, out, b, slot, src, kv = s
+        st = torch.cuda.current_stream()
+        if side is not None:
+            side.wait_stream(st)
+        with torch.cuda.stream(side or st):
+            for f in flat:
+                f.copy_(kv).mul_(2)
+        x.copy_(src).mul_(0.5)
+        if side is not None:
+            st.wait_stream(side)
+        M.mot_paged_append(c.h, 0, c.c, b, x[:, :Hq], x[:, Hq:Hq + H], x[:, Hq + H:], q)
+        M.mot_paged_attention(c.h, 0, c.c, b, q, out)
+        M.mot_paged_store(c.h, c.c, slot, 1, *flat)
+        M.mot_paged_load(c.h, c.c, slot, 1, *back)
+        x.copy_(out.repeat_interleave(2, 1)[:, :Hq + 2 * H])   # behind the calls: a kernel that overlaps nothing
+        src.add_(x)
+
+    eager, graph = pair
+    st, side = torch.cuda.Stream(), torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        step(graph, side)
+    for k in range(10):
+        kv = torch.full_like(eager[9], 0.25 * (k + 1))
+        for s in pair:
+            s[9].copy_(kv)
+        step(eager, None)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((eager[1], *eager[3], eager[4], eager[5]), (graph[1], *graph[3], graph[4], graph[5])):
+            assert torch.equal(a, b)
+        assert torch.equal(eager[3][0], 2 * kv) and bool(eager[5].isfinite().all())
+    for a, b in zip(eager[0].bytes(), graph[0].bytes()):
+        assert torch.equal(a, b)
+    assert eager[0].status() == M.MOT_OK and graph[0].status() == M.MOT_OK
+
+
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right():
     """The first block loads nothing: every wait of the kernel ends, and nothing is left behind for the next call."""
     for d, new in ((64, 300), (128, 300), (64, 1), (128, 1), (128, 5)):
