@@ -747,7 +747,7 @@ def test_a_captured_step_behind_work_of_two_streams(new):
         kv = torch.full_like(eager[9], 0.25 * (k + 1))
         for s in pair:
             s[9].copy_(kv)
-        step(eager, None)
+        step(eager, side if k % 2 else None)
         g.replay()
         torch.cuda.synchronize()
         for a, b in zip((eager[1], *eager[3], eager[4], eager[5]), (graph[1], *graph[3], graph[4], graph[5])):
