@@ -305,8 +305,8 @@ auto append_kernel(const PagedDims& d, const PagedAxes& ax) {
 // memory, a lane's own (kHeld rows; those behind them, of pages of 128 rows of 128, are worked out a second time).
 // Units are dealt out by a scan of the entries in every block, or, with one row to an entry (or few, and many
 // entries), by the row. Bound by instructions, and loads that stand still beside them: 10,254 rows of 28 heads on 4
-// of 128, normed and turned, pages of 64, 43.9 us (4.1 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
-// of 64, pages of 128, 32.2 (52.2). Five blocks per SM 47.9 and 36.6 before the order below, six 49.3 and 39.4, four
+// of 128, normed and turned, pages of 64, 43.3 us (4.1 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
+// of 64, pages of 128, 31.6 (52.2). Five blocks per SM 47.9 and 36.6 before the order below, six 49.3 and 39.4, four
 // 54.3 and 38.9. One row for each of eight sequences 3.6.
 constexpr int kHeld = 8;   // rows of a lane that wait in shared memory for their scale
 template <int D, int ROT, bool AXES>
@@ -428,14 +428,24 @@ struct Rows8 {
     each(0, [&](int r) {
       if (r >= rows) return;
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (held8(x[k])) big = fmaxf(big, fabsf(x[k]));
+      for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[k]));   // fmaxf passes over NaN, which 8 bits then hold as it is
       if (r < kHeld * kAtOnce && rows > kAtOnce) {   // for this lane, behind the scale
         const int e = r / kAtOnce;
         held[2 * e][threadIdx.x] = make_float4(x[0], x[1], x[2], x[3]);
         held[2 * e + 1][threadIdx.x] = make_float4(x[4], x[5], x[6], x[7]);
       }
     });
+    const bool large = __any_sync(0xffffffffu, !held8(big));   // values that have no part in the scale, and become NaN
+    if (large) {
+      big = 0.f;
+      load(sub);
+      each(0, [&](int r) {
+        if (r >= rows) return;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (held8(x[k])) big = fmaxf(big, fabsf(x[k]));
+      });
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
     if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = big;
@@ -451,9 +461,14 @@ struct Rows8 {
     const float inv = 1.f / scale;
     auto write = [&](int r) {
       if (r >= rows) return;
+      if (large) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (!held8(x[k])) x[k] = __uint_as_float(0x7FC00000u);
+      }
       float y[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = unit8(x[k], inv);
+      for (int k = 0; k < 8; ++k) y[k] = x[k] * inv;
       uint8_t* to = dst + (old + r) * D;
       *reinterpret_cast<uint32_t*>(to + eA) = pack8(y[0], y[1], y[2], y[3]);
       *reinterpret_cast<uint32_t*>(to + eB) = pack8(y[4], y[5], y[6], y[7]);

@@ -342,6 +342,33 @@ def test_rows_that_come_one_by_one_and_grow():
             assert bool(torch.isfinite(c.ks[0, [c.t[1][0], c.t[4][0]]]).all())
 
 
+@pytest.mark.parametrize("d,page,new", [(128, 128, 300), (64, 128, 200), (128, 64, 70), (64, 32, 40), (128, 16, 5)])
+def test_values_that_8_bits_do_not_hold_among_many_rows(d, page, new):
+    """Infinities, NaN and values above 448 2^60, in the first rows of a page, its last, and alone in one: they become
+    NaN and have no part in the scale, in rows that stay in registers, that wait in shared memory and that do not."""
+    c = P8.Cache(q_heads=2, kv_heads=2, d=d, page=page, n_pages=30, max_pages=24)
+    c.reserve([2], [new + 3])
+    x = c.normal(new, 6, d)
+    x[0, 2, 1], x[1, 3, d - 1], x[2, 4, 5], x[3, 5, 7] = math.inf, math.nan, -3e38, 1.7578125 * 2.0 ** 68
+    x[new - 1, 2:, 3] = torch.tensor([math.nan, -math.inf, 1.75 * 2.0 ** 68, math.inf], device="cuda").bfloat16()
+    x[new // 2, 3], x[new // 2, 4] = math.inf, math.nan
+    out = torch.zeros((new, 2, d), dtype=torch.bfloat16, device="cuda")
+    before = [t.double() for t in (c.k, c.v, c.ks, c.vs)]
+    M.mot_paged_append(c.h, 0, c.c, c.batch([2], [new]), x[:, :2], x[:, 2:4], x[:, 4:], out)
+    assert c.status() == M.MOT_OK
+    y = x.double()
+    for pool, scale, old_pool, was, z in ((c.k, c.ks, before[0], before[2], y[:, 2:4]), (c.v, c.vs, before[1], before[3], y[:, 4:])):
+        a = 3
+        while a < c.n[2]:
+            b = min(c.n[2], (a // page + 1) * page)
+            p, o = c.t[2][a // page], a % page
+            for hk in range(2):
+                sc, kept, fresh = P8.joined(old_pool[0, p, hk, :o], was[0, p, hk], z[a - 3:b - 3, hk])
+                assert float(scale[0, p, hk]) == float(sc), (a, hk)
+                assert P8.same(pool[0, p, hk, :o].double(), kept) and P8.same(pool[0, p, hk, o:o + b - a].double(), fresh)
+            a = b
+
+
 @pytest.mark.parametrize("n,hints", [(700, (14, 1)), (1500, (14, 17))])
 def test_many_entries_and_a_hint_that_is_wrong(n, hints):
     """More entries than a block has threads, some without rows; the same with a max_chunk of one, which bounds nothing
