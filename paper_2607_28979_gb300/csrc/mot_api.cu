@@ -14,6 +14,7 @@
 #include "bt_internal.h"
 #include "mot_internal.h"
 #include "paged_internal.h"
+#include "paged_turns.h"
 #include "replay_internal.h"
 
 using namespace mot;
@@ -1855,13 +1856,6 @@ mot_status mot_expert_usage(const int32_t* counts, int32_t n, double* cv2, doubl
 
 // ---------------------------------------------------------------- paged cache
 
-// An angle in radians as a fraction of a turn, in units of 2^-64 (whole turns fall away).
-static uint64_t turn_of(long double radians) {
-  const long double turns = radians / 6.283185307179586476925286766559005768L;
-  const long double part = std::ldexp(turns - std::floor(turns), 64) + 0.5L;
-  return part >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(part);
-}
-
 static mot_status create_paged(const mot_paged_config* cfg, bool b8, mot_handle* out) {
   if (!out) return MOT_ERR_INVALID_ARG;
   *out = nullptr;
@@ -2196,8 +2190,7 @@ mot_status mot_paged_set_axes(mot_handle h, int32_t axes, const int32_t* axis, c
     if (axis[i] < 0 || axis[i] >= axes || (rates && !(std::fabs(rates[i]) <= 65536.0))) return MOT_ERR_INVALID_ARG;
   for (int i = 0; i < pairs; ++i) {
     h->paxes.axis[i] = static_cast<uint8_t>(axis[i]);
-    h->paxes.freq[i] = turn_of(rates ? static_cast<long double>(rates[i])
-                                     : std::pow(static_cast<long double>(h->prot_base), -2.0L * i / h->pd.rot));
+    h->paxes.freq[i] = rates ? turn_of(rates[i]) : turn_of(std::pow(static_cast<long double>(h->prot_base), -2.0L * i / h->pd.rot));
   }
   h->n_axes = axes;
   return MOT_OK;
