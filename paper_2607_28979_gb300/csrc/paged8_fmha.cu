@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------ softmax: warps 4 + 4 i + q, stream i, lane quarter q
-    constexpr float kTau = 8.f;
+    constexpr float kTau = 8.f, kFar = 1048576.f;   // kFar: steps of 2^-4 and less below it
     const int i = (warp - 4) >> 2, quarter = warp & 3;
     const int r = quarter * 32 + lane;   // row of the stream
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           }
           tc_fence_after();
           const Scales8& ring = sh.scales[(tile + kt - p.kt) % kScaleRing];
-          const Scales8 sc = ring;   // in registers
+          Scales8 sc = ring;   // in registers
           uint32_t v[4][32];
 #pragma unroll
           for (int e = 0; e < 4; ++e) tmem_ld_32x32b_x32(tS + 32 * e, v[e]);
@@ -446,8 +446,39 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             x = fmax3(x, __uint_as_float(v[e >> 1][16 * (e & 1) + 14]), __uint_as_float(v[e >> 1][16 * (e & 1) + 15]));
             mg[e] = fmaf(fmaxf(x, y), rf * sc.k[e], sc.e[e]);
           }
-          const float mx = fmaxf(fmax3(mg[0], mg[1], mg[2]), fmax3(mg[3], mg[4], fmax3(mg[5], mg[6], mg[7])));
-          const bool raise = mx > m + kTau;   // always where m = -inf and a key is seen
+          float mx = fmaxf(fmax3(mg[0], mg[1], mg[2]), fmax3(mg[3], mg[4], fmax3(mg[5], mg[6], mg[7])));
+          // scores whose steps in fp32 are large beside 1: s f + (e - R) of two roundings would pass 2^16 where
+          // s f + e, rounded, is R. They are worked out in place once, so that what is left to do is exact
+          const bool far = __any_sync(0xffffffffu, fabsf(mx) > kFar && mx != -INFINITY);
+          if (far) {
+            mx = -INFINITY;
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+              uint32_t u[16];
+              tmem_ld_32x32b_x16(tS + 16 * e, u);
+              tmem_ld_wait(u);
+              const float f = rf * ring.k[e], b = ring.e[e];
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const float x = 16 * e + k > see ? -INFINITY : fmaf(__uint_as_float(u[k]), f, b);
+                mx = fmaxf(mx, x);
+                u[k] = __float_as_uint(x);
+              }
+              tmem_st_32x32b_x16(tS + 16 * e, u);
+            }
+            tmem_st_wait();
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tmem_ld_32x32b_x32(tS + 32 * e, v[e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tmem_ld_wait(v[e]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              sc.k[e] = 1.f;
+              sc.e[e] = 0.f;
+            }
+          }
+          const float rw = far ? 1.f : rf;
+          const bool raise = mx - m > kTau;   // always where m = -inf and a key is seen
           const float alpha = (raise && m != -INFINITY) ? exp2f(m - mx) : 1.f;   // below 2^-126 too
           if (__any_sync(0xffffffffu, alpha != 1.f)) {   // needs the products before in O
             if (!wait(&sh.pv_done[i], (t - 1) & 1u)) {
@@ -475,7 +506,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
               uint32_t u[16];
               tmem_ld_32x32b_x16(tS + 16 * e, u);
               tmem_ld_wait(u);
-              const float f = rf * ring.k[e], b = ring.e[e] - mu;
+              const float f = far ? 1.f : rf * ring.k[e], b = (far ? 0.f : ring.e[e]) - mu;
               float g = 0.f;
 #pragma unroll
               for (int k = 0; k < 16; ++k) g += 16 * e + k > see ? 0.f : exp2f(fmaf(__uint_as_float(u[k]), f, b));
@@ -488,7 +519,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             uint32_t pk[16];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const float f = rf * sc.k[2 * e + y], b = sc.e[2 * e + y] - mu;
+              const float f = rw * sc.k[2 * e + y], b = sc.e[2 * e + y] - mu;
               const uint64_t s2 = f32x2(f, f), b2 = f32x2(b, b);
               uint64_t sum[2] = {0, 0};
 #pragma unroll
