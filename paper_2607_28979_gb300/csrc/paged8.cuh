@@ -52,17 +52,19 @@ __device__ __forceinline__ float2 float2_of8(uint32_t pair) {
 
 // A query's row in two 8-bit parts, q = (hi + lo) 2^-up: put by a power of two so that its largest value is at 2^7,
 // each part takes 4 of the 8 bits that a bf16 has. That is exact from 2^-9 of the row's largest on, and off by 2^-17
-// of that below (or by 2^-70: the power is 2^60 at most, so that a score's factor stays above 0 with any key scale).
+// of that below (or by 2^-130, which no key makes count: the power is 2^120 at most).
 // Two products with 8-bit keys take as long as one of 16 bits, and no key is converted.
 struct Split8 {
   float by;       // 2^up
   float factor;   // 2^-up; NaN for a row that holds an infinity or NaN
   // top: the largest magnitude of the row as the bits of a bf16
   __device__ __forceinline__ explicit Split8(uint32_t top) {
-    const int up = min(7 + 127 - int(top >> 7), 60);
+    const int up = top ? min(7 + 127 - int(top >> 7), 120) : 0;
     by = __uint_as_float(uint32_t(up + 127) << 23);
     factor = top >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float(uint32_t(127 - up) << 23);
   }
+  // Whether some key scale takes the factor out of fp32's range (factor8); for a row that is not finite, true.
+  __device__ __forceinline__ bool far() const { return !(factor >= 0x1p-60f && factor <= 0x1p60f); }
   // Four bf16 in two words.
   __device__ __forceinline__ void operator()(uint32_t w0, uint32_t w1, uint32_t& hi, uint32_t& lo) const {
     const float a = __uint_as_float(w0 << 16) * by, b = __uint_as_float(w0 & 0xFFFF0000u) * by;
@@ -72,6 +74,14 @@ struct Split8 {
     lo = pack8(a - x.x, b - x.y, c - y.x, d - y.y);
   }
 };
+// A row's factor times a key scale, held to fp32's normal range: from 2^-126 up, so that nothing masked by -inf is
+// multiplied by 0 (scores below 2^-100 then, which make no weight), and finite, so that a score of 0 stays 0. NaN stays.
+__device__ __forceinline__ float factor8(float row, float key_scale) {
+  float x = row * key_scale;
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(0x1p-126f));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(0x1.fffffep127f));
+  return x;
+}
 // The largest magnitude among eight bf16 and `top`, in each half: magnitudes of bf16 are ordered as integers.
 __device__ __forceinline__ uint32_t top_bf16x2(uint32_t top, const uint4& u) {
   return __vmaxu2(top, __vmaxu2(__vmaxu2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu),

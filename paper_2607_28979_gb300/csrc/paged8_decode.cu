@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
           for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {   // key 16 b + row_of(g) + 8 (e / 2), row 2 t + e % 2
-              s[n][b][e] = fmaf(s[n][b][e] + s2[n][b][e], rf[n][e & 1] * key_scale[b], ev[b]);
+              s[n][b][e] = fmaf(s[n][b][e] + s2[n][b][e], factor8(rf[n][e & 1], key_scale[b]), ev[b]);
               if (part_seen && k0 + 16 * b + row_of<D>(g) + 8 * (e >> 1) > pos[n][e & 1]) s[n][b][e] = -INFINITY;
             }
 #pragma unroll

@@ -385,6 +385,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
       const int pos = valid ? c.s.len - c.s.m + row / G : -1;
       const int64_t out_row = valid ? paged_out_row(c, H, G, row) : 0;
       float m = -INFINITY, l = 0.f, rf = 0.f;
+      bool far_rows = false;   // of the warp
       if (active) {
         // the row's query in two parts, swizzled as TMA would write them
         const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + out_row * D);
@@ -393,6 +394,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
         for (int e = 0; e < D / 8; ++e) top = top_bf16x2(top, valid ? src[e] : make_uint4(0u, 0u, 0u, 0u));
         const Split8 split(max(top & 0xFFFFu, top >> 16));
         rf = sl2 * split.factor;
+        far_rows = __any_sync(0xffffffffu, split.far());
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) {
           uint32_t hi[4], lo[4];
@@ -448,8 +450,9 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           }
           float mx = fmaxf(fmax3(mg[0], mg[1], mg[2]), fmax3(mg[3], mg[4], fmax3(mg[5], mg[6], mg[7])));
           // scores whose steps in fp32 are large beside 1: s f + (e - R) of two roundings would pass 2^16 where
-          // s f + e, rounded, is R. They are worked out in place once, so that what is left to do is exact
-          const bool far = __any_sync(0xffffffffu, fabsf(mx) > kFar && mx != -INFINITY);
+          // s f + e, rounded, is R. They are worked out in place once, so that what is left to do is exact; rows so far
+          // from 1 that f may leave fp32's range too
+          const bool far = far_rows || __any_sync(0xffffffffu, fabsf(mx) > kFar && mx != -INFINITY);
           if (far) {
             mx = -INFINITY;
 #pragma unroll 1
@@ -457,7 +460,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
               uint32_t u[16];
               tmem_ld_32x32b_x16(tS + 16 * e, u);
               tmem_ld_wait(u);
-              const float f = rf * ring.k[e], b = ring.e[e];
+              const float f = factor8(rf, ring.k[e]), b = ring.e[e];
 #pragma unroll
               for (int k = 0; k < 16; ++k) {
                 const float x = 16 * e + k > see ? -INFINITY : fmaf(__uint_as_float(u[k]), f, b);

@@ -45,3 +45,40 @@ def test_scores_far_from_zero(size, new, d):
     for r in range(new):
         best = int((keys[:250 - new + r + 1].double() * size).argmax())
         assert torch.equal(out[r].double(), V[:, best]), r
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 9, 140])
+@pytest.mark.parametrize("eq,ek", [(-58, 59), (-64, 65), (-66, 66), (-100, 66), (52, -52), (30, -29)])
+def test_queries_and_keys_that_meet_from_far(eq, ek, new, d):
+    """Queries of about 2^eq against keys of about 2^ek, whose products are scores of some size: every element counts."""
+    c = P8.Cache(q_heads=8, kv_heads=2, d=d, page=32, n_pages=12, max_pages=8)
+    c.reserve([0], [200])
+    c.ks[0, c.t[0]] = torch.exp2(torch.tensor([ek - 6.0, ek - 7.0, ek - 6.0, ek - 8.0, ek - 6.0, ek - 5.0, ek - 6.0], device="cuda")
+                                 .clamp(-60, 60))[:, None].expand(-1, 2)
+    q = c.normal(new, 8, d) * 2.0 ** eq
+    _, out = _attend(c, [0], [new], q=q)
+    assert c.status() == M.MOT_OK
+    P8.check_attention(c, [0], [new], q, out, label=f"{eq} {ek}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 9, 140])
+@pytest.mark.parametrize("size,ek", [(2.0 ** 127, 60), (1.99 * 2.0 ** 127, -60), (2.0 ** 100, 60), (2.0 ** -130, -60), (2.0 ** -133, 60)])
+def test_queries_at_the_ends_of_bf16_that_no_key_meets(size, ek, new, d):
+    """One element of each query at an end of bf16, keys that are 0 there and of any scale elsewhere: scores of 0, and
+    the mean of the values that are seen."""
+    c = P8.Cache(q_heads=4, kv_heads=2, d=d, page=16, n_pages=20, max_pages=16)
+    c.reserve([0], [200])
+    c.k.view(torch.uint8)[..., 3] = 0
+    c.ks[0, c.t[0]] = 2.0 ** ek
+    c.ks[0, c.t[0][3]] = 2.0 ** -ek
+    q = torch.zeros((new, 4, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 3] = size
+    _, out = _attend(c, [0], [new], q=q)
+    assert c.status() == M.MOT_OK
+    V = c.rows(0)[1].repeat_interleave(2, 0)
+    for r in range(new):
+        seen = V[:, :200 - new + r + 1]
+        # weights that are powers of two, exact in fp16; sums of n values in fp32; the result rounded once
+        P.assert_close(out[r], seen.mean(1), 2.0 ** -8 * seen.mean(1).abs() + 210 * 2.0 ** -24 * seen.abs().mean(1), f"row {r}")
