@@ -14,8 +14,8 @@
 //                         Which key is row g of a block, and which dimensions are a thread's, is free too, and such
 //                         that no quarter of a warp meets a bank of the swizzled rows twice (row_of, part_of).
 //                         The scales: a block's key scale multiplies its scores. Its value scale 2^e goes into the
-//                         weights, w = 2^(s + e - R) with R the running maximum of s + e, so that all of them are
-//                         at most 1 and in fp16 (2^-11 of each, 2^-25 of the largest at the least); the sum
+//                         weights, w = 2^(s + e - R) with R the running maximum of s + e less 15, so that all of them
+//                         are at most 2^15 and in fp16 (2^-11 of each, 2^-40 of the largest at the least); the sum
 //                         of the weights in fp32 takes 2^e out again, exactly.
 //                         One token of 28 heads on 4 of 128 on 131,072 positions and on 70,001: 46.2 us (4.4 TB/s), 64 of 100
 //                         to 16,384 48.3 (4.5 TB/s), 32 heads on 32 on the two contexts 248 (6.6 TB/s); 57.8 and 64.1 with
@@ -35,6 +35,7 @@ constexpr int kDecTK = 32 * kWarps;
 // positions takes 48.3 us with three units for each, 65.8 with none, 49.0 with six; 64 of 4,096 take 55.5 for 55.0.
 // Pieces where they make no CTA's work much longer: contexts of 131,072 and 70,001 positions 46.2 us, 53.9 in runs.
 constexpr int kLeast = 1, kMost = 4, kPad = 3;
+constexpr float kTop = 15.f;   // weights are 2^15 at most: fp16 holds them down to 2^-40 of that, and many small ones count
 
 // Key of a block of 16 that is row g of its first 8: of the swizzled rows of 128 bytes a quarter of a warp takes
 // those that differ in the upper half of the 16-byte pieces, of the rows of 64 bytes both halves of 128.
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
         }
       }
       const int all_pos = len - c.s.m + r0 / G;   // every row sees the keys up to here
-      float m[NT][2], l[NT][2], o[NT][kX][4];     // m: of scores with the value scale's exponent
+      float m[NT][2], l[NT][2], o[NT][kX][4];     // m: largest score with the value scale's exponent, less kTop
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -322,8 +323,8 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
             float x = fmaxf(fmaxf(s[n][0][e], s[n][0][e + 2]), fmaxf(s[n][1][e], s[n][1][e + 2]));
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
-            mx[n][e] = x;
-            up |= x > m[n][e];
+            mx[n][e] = __fadd_ru(x, -kTop);
+            up |= mx[n][e] > m[n][e];
           }
         }
         if (__any_sync(0xffffffffu, up)) {

@@ -10,9 +10,10 @@
 //                                    are, but cost the softmax, which paces the kernel, three conversions for one;
 //                         scales     of 16 keys (a page has 16 at least) each, by way of a ring: that of the keys
 //                                    multiplies the scores, that of the values, 2^e, goes into the weights, w =
-//                                    2^(s + e - R) with R the running maximum of s + e (raised only where a tile
-//                                    passes it by 2^8, so that w is below 2^8, and in fp16 off by 2^-11 of itself or
-//                                    2^-25 at the least); the sum takes 2^e out again, exactly. Where the scales of a
+//                                    2^(s + e - R) with R the running maximum of s + e less 7 (raised only where a
+//                                    tile passes that maximum by 8, so that w is 2^15 at most, and in fp16 off by 2^-11
+//                                    of itself or 2^-25 at the least, 2^-32 of the row's largest); the sum takes 2^e
+//                                    out again, exactly. Where the scales of a
 //                                    tile and of those before it span more than 2^60, weights below 2^-126 count in
 //                                    the sum (w 2^-e beside 2^-e' of the row's largest), and are not flushed to 0.
 //                       Bound by the chain of products and softmax, with shared memory near its limit beside it (both parts
@@ -367,7 +368,8 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------ softmax: warps 4 + 4 i + q, stream i, lane quarter q
-    constexpr float kTau = 8.f, kFar = 1048576.f;   // kFar: steps of 2^-4 and less below it
+    // m is a row's maximum less kTop, and raised where a tile's passes that maximum by kTau. kFar: steps of 2^-4 and less
+    constexpr float kTau = 8.f, kTop = 7.f, kFar = 1048576.f;
     const int i = (warp - 4) >> 2, quarter = warp & 3;
     const int r = quarter * 32 + lane;   // row of the stream
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
@@ -481,8 +483,9 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             }
           }
           const float rw = far ? 1.f : rf;
-          const bool raise = mx - m > kTau;   // always where m = -inf and a key is seen
-          const float alpha = (raise && m != -INFINITY) ? exp2f(m - mx) : 1.f;   // below 2^-126 too
+          const bool raise = mx - m > kTau + kTop;   // always where m = -inf and a key is seen
+          const float to = __fadd_ru(mx, -kTop);     // mx - to is kTop at most, whatever the steps of mx
+          const float alpha = (raise && m != -INFINITY) ? exp2f(m - to) : 1.f;   // below 2^-126 too
           if (__any_sync(0xffffffffu, alpha != 1.f)) {   // needs the products before in O
             if (!wait(&sh.pv_done[i], (t - 1) & 1u)) {
               ok = false;
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             }
             l *= alpha;
           }
-          if (raise) m = mx;
+          if (raise) m = to;
           const float mu = m == -INFINITY ? 0.f : m;
           float wide_sum = 0.f;
           if (ring.wide) {   // the sum by itself, from the scores again: small code beside the loop below

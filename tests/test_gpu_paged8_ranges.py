@@ -82,3 +82,28 @@ def test_queries_at_the_ends_of_bf16_that_no_key_meets(size, ek, new, d):
         seen = V[:, :200 - new + r + 1]
         # weights that are powers of two, exact in fp16; sums of n values in fp32; the result rounded once
         P.assert_close(out[r], seen.mean(1), 2.0 ** -8 * seen.mean(1).abs() + 210 * 2.0 ** -24 * seen.abs().mean(1), f"row {r}")
+
+
+@pytest.mark.parametrize("where", ["first", "last"])
+@pytest.mark.parametrize("new", [1, 9])
+def test_many_small_weights_count_as_much_as_the_sum_says(new, where):
+    """One key 25.4 powers of two ahead of 131,000 others, all values the same, and as many heads as keep an item's keys
+    in one piece: what the others add to the sum of the weights (0.3% of it) they add to the result."""
+    n, page, d = 131000, 128, 64
+    heads = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    c = P8.Cache(q_heads=2 * heads, kv_heads=heads, d=d, page=page, n_pages=1024, max_pages=1024, max_seqs=1)
+    c.reserve([0], [n])
+    c.k.zero_()
+    c.ks.fill_(1.0)
+    c.v.view(torch.uint8).fill_(torch.tensor(1.875).to(P8.F8).view(torch.uint8).item())
+    c.vs.fill_(0.25)
+    at = 0 if where == "first" else n - new
+    c.k.view(torch.uint8)[0, c.t[0][at // page], :, at % page, 0] = torch.tensor(16.0).to(P8.F8).view(torch.uint8).item()
+    q = torch.zeros((new, 2 * heads, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 25.4 * math.log(2) * math.sqrt(d) / 16
+    # the others' part of the sum is 131,000 2^-25.4 = 0.003. In fp16 it is off by 2^-7 of itself (2^-32 of the largest
+    # for each); in fp32 sums beside the largest a step of 16 keys is off by a third of itself at most, 0.001 in all; the
+    # border to the next bf16 is 2^-9 of the value away
+    _, out = _attend(c, [0], [new], q=q)
+    assert c.status() == M.MOT_OK
+    assert bool((out == 1.875 / 4).all()), out.double().unique()
