@@ -667,11 +667,12 @@ mot_status mot_paged_append_at(mot_handle h, int32_t layer, const mot_paged_cach
  * parts (2^-17), so that the last bits of a row may differ with the call that it is in.
  * Over 8-bit pages keys and values enter exactly, a query's elements too (those
  * below 2^-9 of its row's largest are off by 2^-17 of that, or by 2^-130), and a weight,
- * times the scale of its page's values and beside the row's largest such product, rounded
- * to fp16 (2^-11 of it, 2^-32 of the largest at the least). Their sum takes them before
- * that rounding, so that a mean of equal values may be off by as much before its own. A
- * NaN that is seen gives NaN, in a value for its dimension alone; so does a query that
- * holds one or an infinity, for its whole row.
+ * times the scale of its page's values (whose exponent is added to the score, in fp32) and
+ * beside the row's largest such product, rounded to fp16 (2^-11 of it, 2^-32 of the largest
+ * at the least). Their sum takes them before that rounding, so that a mean of equal values
+ * may be off by as much before its own. A NaN that is seen gives NaN, in a value for its
+ * dimension alone; so does a query that holds one or an infinity, or a score above fp32's
+ * range, for its whole row.
  */
 mot_status mot_paged_attention(mot_handle h, int32_t layer, const mot_paged_cache* cache,
                                const mot_paged_batch* batch, const void* q, void* out,

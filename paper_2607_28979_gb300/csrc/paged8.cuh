@@ -59,12 +59,10 @@ struct Split8 {
   float factor;   // 2^-up; NaN for a row that holds an infinity or NaN
   // top: the largest magnitude of the row as the bits of a bf16
   __device__ __forceinline__ explicit Split8(uint32_t top) {
-    const int up = top ? min(7 + 127 - int(top >> 7), 120) : 0;
+    const int up = min(7 + 127 - int(top >> 7), top ? 120 : 60);   // a row of zeros: any
     by = __uint_as_float(uint32_t(up + 127) << 23);
     factor = top >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float(uint32_t(127 - up) << 23);
   }
-  // Whether some key scale takes the factor out of fp32's range (factor8); for a row that is not finite, true.
-  __device__ __forceinline__ bool far() const { return !(factor >= 0x1p-60f && factor <= 0x1p60f); }
   // Four bf16 in two words.
   __device__ __forceinline__ void operator()(uint32_t w0, uint32_t w1, uint32_t& hi, uint32_t& lo) const {
     const float a = __uint_as_float(w0 << 16) * by, b = __uint_as_float(w0 & 0xFFFF0000u) * by;

@@ -42,7 +42,7 @@ struct Pf8 {
   static constexpr int kNK = 2, kNV = 3, kNH = 2;      // tiles in flight: keys, values, values in fp16
   static constexpr int kThreads = 32 * 12;
   static constexpr int kBytes = (4 + kNK + kNV) * kTile + kNH * kTile16;
-  static constexpr int kSmem = kBytes + 2048 + 1024;   // barriers, scales and notes; alignment
+  static constexpr int kSmem = kBytes + 4096 + 1024;   // barriers, scales and notes; alignment
   static constexpr int kO = 256;                       // TMEM: S at 0 and 128, O at 256 and 256 + D
   // 16-byte piece c of row r, swizzled as TMA writes rows of D bytes
   static __device__ __forceinline__ uint32_t at(int r, int c) {
@@ -53,10 +53,9 @@ static_assert(Pf8<128>::kSmem <= 232448, "shared memory budget");
 static_assert(Pf8<128>::kO + 2 * 128 <= 512, "TMEM columns");
 
 constexpr int kScaleRing = 8;
-struct Scales8 {   // of a tile's groups of 16 keys
+struct alignas(16) Scales8 {   // of a tile's groups of 16 keys
   float k[8], e[8], inv[8];   // of keys; a value scale's exponent and 2^-e
   int32_t wide;               // value scales so far apart that a weight in the sum may lie below 2^-126
-  int32_t pad[3];
 };
 
 // Barriers and what the roles leave for one another.
@@ -67,9 +66,11 @@ struct Pf8Shared {
   int32_t abort;
   PagedJoinShared join;
   uint32_t notes[4][4][4];   // [piece & 3][tile of the masked ones][128 keys]: values that are NaN
-  alignas(16) Scales8 scales[kScaleRing];
+  Scales8 scales[kScaleRing];
+  Scales8 done[8];   // a softmax warp's, of a tile whose scores are worked out already
+  float rf[256];     // what takes a row's scores to base-2 exponents, but for the key scales: a thread's own
 };
-static_assert(sizeof(Pf8Shared) <= 2048, "barrier block");
+static_assert(sizeof(Pf8Shared) <= 4096, "barrier block");
 
 // K-major operand of 64-byte rows with 64-byte swizzling: 8-row groups 512 B apart.
 __device__ __forceinline__ uint64_t sdesc_k_sw64(uint32_t saddr) {
@@ -368,8 +369,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------ softmax: warps 4 + 4 i + q, stream i, lane quarter q
-    // m is a row's maximum less kTop, and raised where a tile's passes that maximum by kTau. kFar: steps of 2^-4 and less
-    constexpr float kTau = 8.f, kTop = 7.f, kFar = 1048576.f;
+    constexpr float kTau = 8.f, kTop = 7.f;   // m is a row's maximum less kTop, raised where a tile's passes that by kTau
     const int i = (warp - 4) >> 2, quarter = warp & 3;
     const int r = quarter * 32 + lane;   // row of the stream
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
@@ -386,8 +386,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
       const bool valid = row < n_rows;
       const int pos = valid ? c.s.len - c.s.m + row / G : -1;
       const int64_t out_row = valid ? paged_out_row(c, H, G, row) : 0;
-      float m = -INFINITY, l = 0.f, rf = 0.f;
-      bool far_rows = false;   // of the warp
+      float m = -INFINITY, l = 0.f;
       if (active) {
         // the row's query in two parts, swizzled as TMA would write them
         const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + out_row * D);
@@ -395,8 +394,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
 #pragma unroll
         for (int e = 0; e < D / 8; ++e) top = top_bf16x2(top, valid ? src[e] : make_uint4(0u, 0u, 0u, 0u));
         const Split8 split(max(top & 0xFFFFu, top >> 16));
-        rf = sl2 * split.factor;
-        far_rows = __any_sync(0xffffffffu, split.far());
+        sh.rf[tid - 128] = sl2 * split.factor;
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) {
           uint32_t hi[4], lo[4];
@@ -420,14 +418,16 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             break;
           }
           tc_fence_after();
-          const Scales8& ring = sh.scales[(tile + kt - p.kt) % kScaleRing];
-          Scales8 sc = ring;   // in registers
+          const int see = pos - kt * F::kTK;   // keys 0 .. see of the tile count
+          const Scales8* ring = &sh.scales[(tile + kt - p.kt) % kScaleRing];
+          float rf = sh.rf[tid - 128];
+        again:
+          const Scales8 sc = *ring;   // in registers
           uint32_t v[4][32];
 #pragma unroll
           for (int e = 0; e < 4; ++e) tmem_ld_32x32b_x32(tS + 32 * e, v[e]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) tmem_ld_wait(v[e]);
-          const int see = pos - kt * F::kTK;   // keys 0 .. see of the tile count
           if (!__all_sync(0xffffffffu, see >= F::kTK - 1)) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -450,43 +450,42 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             x = fmax3(x, __uint_as_float(v[e >> 1][16 * (e & 1) + 14]), __uint_as_float(v[e >> 1][16 * (e & 1) + 15]));
             mg[e] = fmaf(fmaxf(x, y), rf * sc.k[e], sc.e[e]);
           }
-          float mx = fmaxf(fmax3(mg[0], mg[1], mg[2]), fmax3(mg[3], mg[4], fmax3(mg[5], mg[6], mg[7])));
-          // scores whose steps in fp32 are large beside 1: s f + (e - R) of two roundings would pass 2^16 where
-          // s f + e, rounded, is R. They are worked out in place once, so that what is left to do is exact; rows so far
-          // from 1 that f may leave fp32's range too
-          const bool far = far_rows || __any_sync(0xffffffffu, fabsf(mx) > kFar && mx != -INFINITY);
-          if (far) {
-            mx = -INFINITY;
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-              uint32_t u[16];
-              tmem_ld_32x32b_x16(tS + 16 * e, u);
-              tmem_ld_wait(u);
-              const float f = factor8(rf, ring.k[e]), b = ring.e[e];
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const float x = 16 * e + k > see ? -INFINITY : fmaf(__uint_as_float(u[k]), f, b);
-                mx = fmaxf(mx, x);
-                u[k] = __float_as_uint(x);
-              }
-              tmem_st_32x32b_x16(tS + 16 * e, u);
-            }
-            tmem_st_wait();
-#pragma unroll
-            for (int e = 0; e < 4; ++e) tmem_ld_32x32b_x32(tS + 32 * e, v[e]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) tmem_ld_wait(v[e]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              sc.k[e] = 1.f;
-              sc.e[e] = 0.f;
-            }
-          }
-          const float rw = far ? 1.f : rf;
+          const float mx = fmaxf(fmax3(mg[0], mg[1], mg[2]), fmax3(mg[3], mg[4], fmax3(mg[5], mg[6], mg[7])));
           const bool raise = mx - m > kTau + kTop;   // always where m = -inf and a key is seen
           const float to = __fadd_ru(mx, -kTop);     // mx - to is kTop at most, whatever the steps of mx
           const float alpha = (raise && m != -INFINITY) ? exp2f(m - to) : 1.f;   // below 2^-126 too
-          if (__any_sync(0xffffffffu, alpha != 1.f)) {   // needs the products before in O
+          // Scores from 2^22 on: beside their steps in fp32 the weights' s f + (e - R) of two roundings could pass 2^16
+          // where s f + e, rounded, is R. They are worked out in place first, in one rounding, so that what is left to
+          // do is exact, with 1 as the row's factor (which no other row has: it is a power of two over sqrt(d) ln 2). So
+          // are those of rows whose factor may leave fp32's range with a key scale.
+          const bool far =
+              rf != 1.f && (!(rf >= 0x1p-66f && rf <= 0x1p67f) || (fabsf(mx) > 0x1p22f && mx != -INFINITY));
+          if (__any_sync(0xffffffffu, alpha != 1.f || far)) {
+            if (__any_sync(0xffffffffu, far)) {
+              Scales8& done = sh.done[warp - 4];
+#pragma unroll 1
+              for (int e = 0; e < 8; ++e) {
+                uint32_t u[16];
+                tmem_ld_32x32b_x16(tS + 16 * e, u);
+                tmem_ld_wait(u);
+                const float f = factor8(rf, ring->k[e]), b = ring->e[e];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) u[k] = __float_as_uint(fmaf(__uint_as_float(u[k]), f, b));
+                tmem_st_32x32b_x16(tS + 16 * e, u);
+              }
+              tmem_st_wait();
+              if (lane < 8) {
+                done.k[lane] = 1.f;
+                done.e[lane] = 0.f;
+                done.inv[lane] = ring->inv[lane];
+              }
+              if (lane == 0) done.wide = ring->wide;
+              __syncwarp();
+              ring = &done;
+              rf = 1.f;
+              goto again;
+            }
+            // needs the products before in O
             if (!wait(&sh.pv_done[i], (t - 1) & 1u)) {
               ok = false;
               break;
@@ -506,17 +505,17 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           if (raise) m = to;
           const float mu = m == -INFINITY ? 0.f : m;
           float wide_sum = 0.f;
-          if (ring.wide) {   // the sum by itself, from the scores again: small code beside the loop below
+          if (ring->wide) {   // the sum by itself, from the scores again: small code beside the loop below
 #pragma unroll 1
             for (int e = 0; e < 8; ++e) {
               uint32_t u[16];
               tmem_ld_32x32b_x16(tS + 16 * e, u);
               tmem_ld_wait(u);
-              const float f = far ? 1.f : rf * ring.k[e], b = (far ? 0.f : ring.e[e]) - mu;
+              const float f = rf * ring->k[e], b = ring->e[e] - mu;
               float g = 0.f;
 #pragma unroll
               for (int k = 0; k < 16; ++k) g += 16 * e + k > see ? 0.f : exp2f(fmaf(__uint_as_float(u[k]), f, b));
-              wide_sum = fmaf(g, ring.inv[e], wide_sum);
+              wide_sum = fmaf(g, ring->inv[e], wide_sum);
             }
             wide_sum += l;
           }
@@ -525,7 +524,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             uint32_t pk[16];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const float f = rw * sc.k[2 * e + y], b = sc.e[2 * e + y] - mu;
+              const float f = rf * sc.k[2 * e + y], b = sc.e[2 * e + y] - mu;
               const uint64_t s2 = f32x2(f, f), b2 = f32x2(b, b);
               uint64_t sum[2] = {0, 0};
 #pragma unroll
@@ -539,7 +538,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
               }
               sum[0] = fadd_x2(sum[0], sum[1]);
               l = fmaf(__uint_as_float(static_cast<uint32_t>(sum[0])) + __uint_as_float(static_cast<uint32_t>(sum[0] >> 32)),
-                       sc.inv[2 * e + y], l);
+                       ring->inv[2 * e + y], l);
             }
             tmem_st_32x32b_x16(tS + 16 * e, pk);
             if (e & 1) {
@@ -549,7 +548,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
               if (lane == 0) mbar_arrive(&sh.p_half[i][e >> 1]);
             }
           }
-          if (ring.wide) l = wide_sum;
+          if (ring->wide) l = wide_sum;
         }
         ok = ok && wait(&sh.pv_done[i], (t - 1) & 1u);
       }

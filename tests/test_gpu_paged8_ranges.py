@@ -84,6 +84,32 @@ def test_queries_at_the_ends_of_bf16_that_no_key_meets(size, ek, new, d):
         P.assert_close(out[r], seen.mean(1), 2.0 ** -8 * seen.mean(1).abs() + 210 * 2.0 ** -24 * seen.abs().mean(1), f"row {r}")
 
 
+@pytest.mark.parametrize("new", [1, 9, 140])
+def test_scores_that_fp32_does_not_hold(new):
+    """A score above 2^128 makes the rows that see it NaN, one below -2^128 counts for nothing beside others. Value scales
+    of 1: another's exponent would be added to scores of 2^97, whose steps in fp32 are larger."""
+    c = P8.Cache(q_heads=4, kv_heads=2, d=64, page=16, n_pages=20, max_pages=16)
+    c.reserve([0], [200])
+    c.vs.fill_(1.0)
+    keys = torch.full((200,), 1.0, device="cuda")
+    keys[[3, 70]] = -448.0
+    _one_dimension(c, 0, keys)
+    c.ks[0, c.t[0][70 // 16]] = c.ks[0, c.t[0][0]] = 2.0 ** 60
+    c.k.view(torch.uint8)[0, c.t[0][70 // 16], :, :, 0] = c.k.view(torch.uint8)[0, c.t[0][0], :, :, 0] = 0
+    for j in (3, 70):
+        c.k[0, c.t[0][j // 16], :, j % 16, 0] = torch.tensor(-448.0, device="cuda").to(P8.F8)
+    q = torch.zeros((new, 4, 64), dtype=torch.bfloat16, device="cuda")
+    q[:, :2, 0], q[:, 2:, 0] = 2.0 ** 100, -(2.0 ** 100)
+    _, out = _attend(c, [0], [new], q=q)
+    assert c.status() == M.MOT_OK
+    assert bool(out[:, 2:].isnan().all())
+    V = c.rows(0)[1][0]
+    best = [j for j in range(200) if keys[j] > 0 and j // 16 not in (0, 70 // 16)]   # scores of 2^97; the others 0 or less
+    for r in range(new):
+        ref = V[[j for j in best if j <= 200 - new + r]].mean(0)
+        P.assert_close(out[r, 0], ref, 2.0 ** -8 * ref.abs() + 210 * 2.0 ** -24 * V.abs().mean(0), f"row {r}")
+
+
 @pytest.mark.parametrize("where", ["first", "last"])
 @pytest.mark.parametrize("new", [1, 9])
 def test_many_small_weights_count_as_much_as_the_sum_says(new, where):
