@@ -539,8 +539,10 @@ mot_status mot_create_paged(const mot_paged_config* cfg, mot_handle* out);
  * fills in part) its scale never falls; where it rises, the rows that were there are
  * rounded again. A page without rows before those has no scale to
  * keep: the memory of the scales needs no initial value. Scales that the caller
- * writes are powers of two from 2^-60 to 2^60. A value that is not finite, or above
- * 448 2^60, is held as NaN and has no part in a scale.
+ * writes are powers of two from 2^-60 to 2^60; every call that meets another takes the
+ * one below its magnitude in that range (NaN: the largest) and reports it
+ * (MOT_PAGES_HELD). A value that is not finite, or above 448 2^60, is held as NaN and
+ * has no part in a scale.
  *
  * A handle of mot_create_paged8 takes every call of a paged one, with queries, new
  * keys and values, outputs and contiguous caches in bf16 (cfg.dtype; fp32:

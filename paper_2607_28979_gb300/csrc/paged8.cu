@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kThreads8, 4)
 #pragma unroll
     for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
     float* place = (is_v ? c.vs : c.ks) + (int64_t(p.first + l) * d.n_pages + s.page) * d.H + hk;
-    const float was = s.filled > s.rows ? *place : 0.f;   // rows that stay: max_seq cuts the page
+    const float was = s.filled > s.rows ? scale_of_page(place, w.status) : 0.f;   // rows that stay: max_seq cuts the page
     if (T > 32) {
       if (lane == 0) top[warp] = big;
       together();
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kThreads8)
         if (v >= n_vec || r / kRow >= s.rows) continue;
         const bool is_v = g >= d.H;
         const int hk = is_v ? g - d.H : g;
-        f[e] = (is_v ? c.vs : c.ks)[at + hk];
+        f[e] = scale_of_page((is_v ? c.vs : c.ks) + at + hk, w.status);
         q[e] = (static_cast<const uint4*>(is_v ? c.v : c.k) + (at + hk) * run)[r];
         to[e] = static_cast<uint4*>(is_v ? p.v : p.k) +
                 ((((int64_t(l) * p.B + i) * d.H + hk) * p.S + (j << d.lp)) * kRow + r) * 2;

@@ -25,6 +25,14 @@ __device__ __forceinline__ float scale8(float top) {
   return __uint_as_float(uint32_t(min(max(e, -60), 60) + 127) << 23);
 }
 
+// A page's scale as it lies in memory: a caller may have written it. What is not a power of two in range is taken as the
+// one below (the end of the range beyond it), by every call alike, and reported.
+__device__ __forceinline__ float scale_of_page(const float* place, int32_t* status) {
+  const uint32_t u = __float_as_uint(*place), e = min(max(u >> 23 & 255u, 67u), 187u) << 23;
+  if (u != e) atomicOr(status, kStatusPageUse);
+  return __uint_as_float(e);
+}
+
 // Four values in units of the scale to 8 bits, to the nearest, ties to the even one; the first in the lowest byte.
 __device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d) {
   uint16_t lo, hi;

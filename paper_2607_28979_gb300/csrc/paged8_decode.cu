@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
         };
         auto scale = [&](int kt, int page) {
           const int64_t x = int64_t(page) * H + c.hk;
-          return mine(kt) ? make_float2(a.ks[x], a.vs[x]) : make_float2(1.f, 1.f);
+          return mine(kt) ? make_float2(scale_of_page(a.ks + x, a.status), scale_of_page(a.vs + x, a.status))
+                          : make_float2(1.f, 1.f);
         };
         int page = entry(p.kt), next = entry(p.kt + 1);
         float2 sc = scale(p.kt, page);

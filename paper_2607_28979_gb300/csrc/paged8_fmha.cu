@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
         };
         auto scales = [&](int kt, int page) -> float2 {
           const int64_t x = int64_t(page) * H + c.hk;
-          return mine(kt) ? make_float2(a.ks[x], a.vs[x]) : make_float2(1.f, 1.f);
+          return mine(kt) ? make_float2(scale_of_page(a.ks + x, a.status), scale_of_page(a.vs + x, a.status))
+                          : make_float2(1.f, 1.f);
         };
         int page = entry(p.kt), next = entry(p.kt + 1);
         float2 sc = scales(p.kt, page);

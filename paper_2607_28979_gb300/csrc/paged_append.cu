@@ -411,7 +411,7 @@ struct Rows8 {
     const int64_t at_head = (int64_t(p.layer) * d.n_pages + page) * d.H + hk;
     float* place = (key ? c.ks : c.vs) + at_head;
     uint8_t* dst = static_cast<uint8_t*>(key ? c.k : c.v) + (at_head << d.lp) * D;
-    const float was = old ? *place : 0.f;
+    const float was = old ? scale_of_page(place, status) : 0.f;
     float x[8], big = 0.f;
     auto each = [&](int from, auto&& use) {
       for (int r0 = from + sub; r0 < rows + sub; r0 += kAhead * kAtOnce) {   // as often for every lane

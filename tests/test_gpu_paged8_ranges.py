@@ -133,3 +133,61 @@ def test_many_small_weights_count_as_much_as_the_sum_says(new, where):
     _, out = _attend(c, [0], [new], q=q)
     assert c.status() == M.MOT_OK
     assert bool((out == 1.875 / 4).all()), out.double().unique()
+
+
+BAD = {3.0: 2.0, 0.0: 2.0 ** -60, -4.0: 4.0, math.nan: 2.0 ** 60, math.inf: 2.0 ** 60, -math.inf: 2.0 ** 60, 2.0 ** 61: 2.0 ** 60,
+       2.0 ** -61: 2.0 ** -60, 1e-40: 2.0 ** -60, 0.75: 0.5}
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("bad", BAD, ids=str)
+def test_a_scale_that_is_no_power_of_two_is_the_same_to_every_call_and_reported(bad, d, page):
+    """Attention of few rows and of chunks, load, a store that cuts a page and appends to one: what they give for the
+    power that the scale is taken as, and a status that says so; nothing for scales of pages that no call meets."""
+    made = []
+    for way in ("good", "bad"):
+        got = []
+        for which in ("ks", "vs"):
+            c = P8.Cache(q_heads=6, kv_heads=2, d=d, page=page, n_pages=40, max_pages=12, seed=3)
+            c.reserve([0, 1], [5 * page + 5, page + 3])
+            scales = getattr(c, which)
+            at = c.t[0][2], c.t[0][-1]   # a full page, and the last
+            scales[0, [p for p in range(40) if p not in c.t[0] + c.t[1]]] = bad
+
+            def put(p):
+                scales[0, p, 1] = bad if way == "bad" else BAD[bad]
+
+            def status(met=True):
+                s = M.mot_get_device_status(c.h)
+                assert s == (M.MOT_ERR_PAGES if way == "bad" and met else M.MOT_OK)
+                if s != M.MOT_OK:
+                    assert M.mot_paged_cause(c.h) == M.MOT_PAGES_HELD
+
+            put(at[0])
+            for new in (1, 40):
+                q, out = _attend(c, [0], [new])
+                got.append(out)
+                status()
+                got.append(_attend(c, [1], [new], q=q)[1])   # of the other sequence
+                status(False)
+            flat = [torch.zeros((1, 2, 2, 5 * page + 9, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+            M.mot_paged_load(c.h, c.c, i32([0, 1]), 2, *flat)
+            status()
+            got += flat
+            scales[0, at[0], 1] = 1.0
+            x = c.normal(3, 10, d)
+            q = torch.zeros((3, 6, d), dtype=torch.bfloat16, device="cuda")
+            for new in ([2, 1], [1]):
+                put(at[1])
+                c.reserve([0, 1][:len(new)], new)
+                M.mot_paged_append(c.h, 0, c.c, c.batch([0, 1][:len(new)], new), x[:, :6], x[:, 6:8], x[:, 8:], q)
+                status()
+                got += [q.clone()] + [t[0, c.t[0] + c.t[1]].clone() for t in c.bytes()[:2]]
+                got.append(scales[0, at[1]].clone())
+            put(at[1])
+            M.mot_paged_store(c.h, c.c, i32([0]), 1, *[c.normal(1, 1, 2, 5 * page + 2, d) for _ in range(2)])
+            assert M.mot_get_device_status(c.h) == M.MOT_ERR_PAGES   # it is shorter than the sequence, too
+            got += [t[0, c.t[0]].clone() for t in c.bytes()[:2]] + [scales[0, at[1]].clone()]
+        made.append(got)
+    for k, (a, b) in enumerate(zip(*made)):
+        assert P8.same(a.double(), b.double()), k
