@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kThreads8, 4)
 #pragma unroll
     for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
     float* place = (is_v ? c.vs : c.ks) + (int64_t(p.first + l) * d.n_pages + s.page) * d.H + hk;
-    const float was = s.filled > s.rows ? scale_of_page(place, w.status) : 0.f;   // rows that stay: max_seq cuts the page
+    const float was = s.filled > s.rows ? *place : 0.f;   // rows that stay: max_seq cuts the page
     if (T > 32) {
       if (lane == 0) top[warp] = big;
       together();
@@ -99,8 +99,9 @@ __global__ void __launch_bounds__(kThreads8, 4)
     uint8_t* dst = static_cast<uint8_t*>(is_v ? c.v : c.k) +
                    ((int64_t(p.first + l) * d.n_pages + s.page) * d.H + hk) * d.P * D;
     if (s.filled > s.rows) {
-      scale = fmaxf(scale, was);
-      if (scale != was) rescale8(dst + s.rows * D, (s.filled - s.rows) * D, was / scale, t, T);
+      const float old = scale_of_page(was, w.status);
+      scale = fmaxf(scale, old);
+      if (scale != old) rescale8(dst + s.rows * D, (s.filled - s.rows) * D, old / scale, t, T);
     }
     const float inv = 1.f / scale;
 #pragma unroll
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(kThreads8)
         if (v >= n_vec || r / kRow >= s.rows) continue;
         const bool is_v = g >= d.H;
         const int hk = is_v ? g - d.H : g;
-        f[e] = scale_of_page((is_v ? c.vs : c.ks) + at + hk, w.status);
+        f[e] = (is_v ? c.vs : c.ks)[at + hk];
         q[e] = (static_cast<const uint4*>(is_v ? c.v : c.k) + (at + hk) * run)[r];
         to[e] = static_cast<uint4*>(is_v ? p.v : p.k) +
                 ((((int64_t(l) * p.B + i) * d.H + hk) * p.S + (j << d.lp)) * kRow + r) * 2;
@@ -153,12 +154,13 @@ __global__ void __launch_bounds__(kThreads8)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (!to[e]) continue;
+        const float by = scale_of_page(f[e], w.status);
         const uint32_t b[4] = {q[e].x, q[e].y, q[e].z, q[e].w};
         uint32_t o[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float2 z = float2_of8(k & 1 ? b[k >> 1] >> 16 : b[k >> 1]);
-          const __nv_bfloat162 r = __floats2bfloat162_rn(z.x * f[e], z.y * f[e]);
+          const __nv_bfloat162 r = __floats2bfloat162_rn(z.x * by, z.y * by);
           o[k] = *reinterpret_cast<const uint32_t*>(&r);
         }
         to[e][0] = make_uint4(o[0], o[1], o[2], o[3]);

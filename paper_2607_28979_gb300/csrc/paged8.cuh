@@ -25,12 +25,17 @@ __device__ __forceinline__ float scale8(float top) {
   return __uint_as_float(uint32_t(min(max(e, -60), 60) + 127) << 23);
 }
 
-// A page's scale as it lies in memory: a caller may have written it. What is not a power of two in range is taken as the
-// one below (the end of the range beyond it), by every call alike, and reported.
-__device__ __forceinline__ float scale_of_page(const float* place, int32_t* status) {
-  const uint32_t u = __float_as_uint(*place), e = min(max(u >> 23 & 255u, 67u), 187u) << 23;
-  if (u != e) atomicOr(status, kStatusPageUse);
-  return __uint_as_float(e);
+// A page's scale x as it lay in memory: a caller may have written it. What is not a power of two in range is taken as the
+// one below (the end of the range beyond it), by every call alike, and reported. Asked some time after the load, which
+// is waited for there: asked beside it, 64 decoding steps of 100 to 16,384 positions take 58.1 us for 54.6.
+__device__ __forceinline__ bool is_scale8(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return (u & 0x7FFFFFu) == 0 && u - (67u << 23) <= 120u << 23;
+}
+__device__ __forceinline__ float scale_of_page(float x, int32_t* status) {
+  if (is_scale8(x)) return x;
+  atomicOr(status, kStatusPageUse);
+  return __uint_as_float(min(max(__float_as_uint(x) >> 23 & 255u, 67u), 187u) << 23);
 }
 
 // Four values in units of the scale to 8 bits, to the nearest, ties to the even one; the first in the lowest byte.

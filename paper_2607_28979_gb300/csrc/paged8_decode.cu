@@ -148,14 +148,15 @@ __global__ void __launch_bounds__(kDecThreads, Dec8<D, NT>::kResident)
         };
         auto scale = [&](int kt, int page) {
           const int64_t x = int64_t(page) * H + c.hk;
-          return mine(kt) ? make_float2(scale_of_page(a.ks + x, a.status), scale_of_page(a.vs + x, a.status))
-                          : make_float2(1.f, 1.f);
+          return mine(kt) ? make_float2(a.ks[x], a.vs[x]) : make_float2(1.f, 1.f);
         };
         int page = entry(p.kt), next = entry(p.kt + 1);
         float2 sc = scale(p.kt, page);
         for (int kt = p.kt; kt < kt_end; ++kt, ++tile) {
           const int next2 = entry(kt + 2);
           const float2 sc2 = scale(kt + 1, next);
+          if (!is_scale8(sc.x) || !is_scale8(sc.y))
+            sc = make_float2(scale_of_page(sc.x, a.status), scale_of_page(sc.y, a.status));
           const uint32_t s = tile % kS;
           ok = __all_sync(0xffffffffu, mbar_wait(&empty[s], ((tile / kS) & 1u) ^ 1u, abort_flag, a.wait_limit));
           if (!ok) break;

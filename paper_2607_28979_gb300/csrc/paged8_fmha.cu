@@ -93,6 +93,11 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_
       : "memory");
 }
 
+// Scales out of the rule, in a call of its own: written out in the producer's loop it cost the kernel 2%.
+__device__ __noinline__ float2 held_scales(float2 s, int32_t* status) {
+  return make_float2(scale_of_page(s.x, status), scale_of_page(s.y, status));
+}
+
 template <int D>
 __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
     paged8_fmha_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -180,8 +185,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
         };
         auto scales = [&](int kt, int page) -> float2 {
           const int64_t x = int64_t(page) * H + c.hk;
-          return mine(kt) ? make_float2(scale_of_page(a.ks + x, a.status), scale_of_page(a.vs + x, a.status))
-                          : make_float2(1.f, 1.f);
+          return mine(kt) ? make_float2(a.ks[x], a.vs[x]) : make_float2(1.f, 1.f);
         };
         int page = entry(p.kt), next = entry(p.kt + 1);
         float2 sc = scales(p.kt, page);
@@ -190,6 +194,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
           const int k0 = kt * F::kTK, n_keys = min(F::kTK, c.s.len - k0);
           const int next2 = entry(kt + 2);
           const float2 sc2 = scales(kt + 1, next);
+          if (!is_scale8(sc.x) || !is_scale8(sc.y)) sc = held_scales(sc, a.status);
           const bool load = mine(kt) && (16 * lane & (a.d.P - 1)) == 0;
           const int row = (page * H + c.hk) << a.d.lp;
           const uint32_t bytes =
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
             if (!wait(v ? &sh.v_empty[st] : &sh.k_empty[st], (use & 1u) ^ 1u)) return false;
             if (!v) {   // the softmax is through the tile that had this place: it is kScaleRing back
               Scales8& to = sh.scales[t % kScaleRing];
-              const int e = int(__float_as_uint(sc.y) >> 23 & 255u) - 127;
+              const int e = int(__float_as_uint(sc.y) >> 23) - 127;
               e_top = max(e_top, __reduce_max_sync(0xffffffffu, mine(kt) ? e : -127));
               const int least = __reduce_min_sync(0xffffffffu, mine(kt) ? e : 128);
               if (lane < 8) {

@@ -411,7 +411,7 @@ struct Rows8 {
     const int64_t at_head = (int64_t(p.layer) * d.n_pages + page) * d.H + hk;
     float* place = (key ? c.ks : c.vs) + at_head;
     uint8_t* dst = static_cast<uint8_t*>(key ? c.k : c.v) + (at_head << d.lp) * D;
-    const float was = old ? scale_of_page(place, status) : 0.f;
+    float was = old ? *place : 0.f;
     float x[8], big = 0.f;
     auto each = [&](int from, auto&& use) {
       for (int r0 = from + sub; r0 < rows + sub; r0 += kAhead * kAtOnce) {   // as often for every lane
@@ -454,6 +454,7 @@ struct Rows8 {
     for (int k = 0; k < kAppendThreads / 32; ++k) big = fmaxf(big, top[k]);
     float scale = scale8(big);
     if (old) {
+      was = scale_of_page(was, status);
       scale = fmaxf(scale, was);
       if (scale != was) rescale8(dst, old * D, was / scale, threadIdx.x, kAppendThreads);
     }
