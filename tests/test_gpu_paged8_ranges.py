@@ -191,3 +191,55 @@ def test_a_scale_that_is_no_power_of_two_is_the_same_to_every_call_and_reported(
         made.append(got)
     for k, (a, b) in enumerate(zip(*made)):
         assert P8.same(a.double(), b.double()), k
+
+
+def _exponents(kind, n, gen):
+    """Value scales' exponents of n pages of 16 positions, eight to a tile of 128 keys."""
+    j = torch.arange(n, device="cuda")
+    if kind == "rise":      # by 20 from tile to tile, within each by 14
+        return (-60 + 20 * (j // 8 % 7) - 2 * (j % 8)).clamp(-60, 60)
+    if kind == "fall":
+        return (60 - 20 * (j // 8 % 7) + 2 * (j % 8)).clamp(-60, 60)
+    if kind == "tiles":     # one tile's at the end, the next one's at the other
+        return torch.where(j // 8 % 2 == 0, 55 + j % 6, -60 + j % 6)
+    if kind == "pages":
+        return torch.where(j % 2 == 0, 60, -60)
+    if kind == "steps":     # spans of just about 60 in a tile
+        return torch.where(j % 8 < 4, 30, -29 - j // 8 % 3)
+    return torch.randint(-60, 61, (n,), generator=gen, device="cuda")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 9])
+@pytest.mark.parametrize("kind", ["rise", "fall", "tiles", "pages", "steps", "any"])
+def test_scales_far_apart_in_pieces_of_several_tiles(kind, new, d):
+    """Value scales up to 2^120 apart from tile to tile and within one, where a CTA goes over many tiles of an item under a
+    running maximum: 48 items of 11 to 17 tiles in pieces of about seven, of 34 to 48 in pieces or runs of five and more."""
+    lens = [6100, 4300, 5700] if new == 1 else [2100, 1300, 1700]
+    c = P8.Cache(q_heads=32, kv_heads=16, d=d, page=16, n_pages=1010, max_pages=400)
+    c.reserve([0, 1, 2], lens)
+    for s in range(3):
+        for x in range(16):
+            e = _exponents(kind, len(c.t[s]), c.gen)
+            c.vs[0, c.t[s], x] = torch.exp2(e.float()) if x % 2 else torch.exp2(e.flip(0).float())
+    q, out = _attend(c, [0, 1, 2], [new] * 3)
+    assert c.status() == M.MOT_OK
+    P8.check_attention(c, [0, 1, 2], [new] * 3, q, out, label=kind)
+    # the keys of the small scales' pages have nearly all of the weight in half of the heads
+    for s in range(3):
+        small = [p for k, p in enumerate(c.t[s]) if k % 3 == 0]
+        c.ks[0, small, :8] = 4.0
+    _, out = _attend(c, [0, 1, 2], [new] * 3, q=q)
+    assert c.status() == M.MOT_OK
+    P8.check_attention(c, [0, 1, 2], [new] * 3, q, out, label=kind + " weighted")
+
+
+@pytest.mark.parametrize("kind", ["tiles", "any"])
+def test_scales_far_apart_in_chunks_of_two_streams(kind):
+    c = P8.Cache(q_heads=8, kv_heads=1, d=128, page=16, n_pages=140, max_pages=140)
+    c.reserve([0], [2100])
+    c.vs[0, c.t[0], 0] = torch.exp2(_exponents(kind, len(c.t[0]), c.gen).float())
+    for new in (40, 300):
+        q, out = _attend(c, [0], [new])
+        P8.check_attention(c, [0], [new], q, out, label=kind)
+    assert c.status() == M.MOT_OK
