@@ -2160,9 +2160,7 @@ mot_status paged_append(mot_handle h, int32_t layer, const mot_paged_cache* cach
   p.k_norm = k_norm;
   p.freq = h->pfreq;
   p.q_out = q_out;
-  // (many entries of a few rows: a scan of all of them in every block would cost more than rows that are no page's first)
   p.early = !h->profile;
-  p.by_row = batch->max_chunk <= 1 || (p.b.n > 1024 && batch->max_chunk <= 16);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   MOT_CUDA_TRY(timed(h, "paged_append", st,
                      [&] { return launch_paged_append(d, c, p, h->pw, ax, h->num_sms, st); }));

@@ -303,8 +303,7 @@ auto append_kernel(const PagedDims& d, const PagedAxes& ax) {
 // 16 of the rows at a time, d / 8 lanes to a row and the lane's pairs turned by angles of its own (a row of one head
 // has each angle once). What comes out waits for the scale in fp32: in registers where that is all, else in shared
 // memory, a lane's own (kHeld rows; those behind them, of pages of 128 rows of 128, are worked out a second time).
-// Units are dealt out by a scan of the entries in every block, or, with one row to an entry (or few, and many
-// entries), by the row. Bound by instructions, and loads that stand still beside them: 10,254 rows of 28 heads on 4
+// Units are dealt out by a scan of the entries in every block, or, with few rows to an entry, by the row. Bound by instructions, and loads that stand still beside them: 10,254 rows of 28 heads on 4
 // of 128, normed and turned, pages of 64, 43.3 us (4.1 TB/s; 51.9 with every row worked out twice), of 12 heads on 12
 // of 64, pages of 128, 31.6 (52.2). Five blocks per SM 47.9 and 36.6 before the order below, six 49.3 and 39.4, four
 // 54.3 and 38.9. One row for each of eight sequences 3.6.
@@ -597,13 +596,19 @@ cudaError_t launch_paged_append(const PagedDims& d, const PagedCache& c, const P
   const int64_t units = (int64_t(p.b.rows) + rows_each - 1) / rows_each * parts;
   const int grid = int((units + kWarps - 1) / kWarps);
   if (d.b8) {
+    // Units by the row where entries have two rows at most on the average, whatever the longest has: rows that are no
+    // page's first cost a look each, a scan has every block read all entries. 2,000 single rows of 4 key/value heads of
+    // 128 57 us (98 by a scan), with a prompt of 500 beside them 63 (110), with one of 4,000 103 (118); of 12 of 64 on
+    // pages of 16 167 (159), 181 (160) and 293 (194); four rows each 142 (111) and 384 (208), sixteen 582 (156) and
+    // 1,275 (322). 64 single rows 4.3 (4.9), with a prompt of 500 11.7 (9.0).
+    const bool by_row = p.b.rows <= 2 * int64_t(p.b.n);
     // pages that the rows touch: an entry of m rows at most (m - 2) / P + 2
     const int64_t pages = std::min(int64_t(p.b.rows), int64_t(p.b.rows) / d.P + 2 * int64_t(p.b.n));
-    const int64_t blocks = std::min((p.by_row ? int64_t(p.b.rows) : pages) * 2 * d.H, int64_t(num_sms) * 16);
+    const int64_t blocks = std::min((by_row ? int64_t(p.b.rows) : pages) * 2 * d.H, int64_t(num_sms) * 16);
     auto kern = d.d == 64 ? (ax.at ? append8_kernel<64, true>(d) : append8_kernel<64, false>(d))
                           : (ax.at ? append8_kernel<128, true>(d) : append8_kernel<128, false>(d));
     return launch_kernel(p.early, kern, int(grid + blocks), kAppendThreads, 0, st, d, c, p, w, ax, grid, rows_each, parts,
-                         int(p.by_row));
+                         int(by_row));
   }
   auto kern = d.dtype == 0 ? (d.d == 64 ? append_kernel<uint16_t, 64>(d, ax) : append_kernel<uint16_t, 128>(d, ax))
                            : (d.d == 64 ? append_kernel<float, 64>(d, ax) : append_kernel<float, 128>(d, ax));

@@ -89,7 +89,6 @@ struct PagedAppend {
   const void *q_norm, *k_norm;      // [d] or null
   const uint64_t* freq;             // [rot / 2]: turns per position in units of 2^-64
   void* q_out;                      // [rows][Hq][d]
-  bool by_row;                      // 8-bit pages: units by the row, for entries of one row or of few (a hint)
   bool early;                       // the launch may overlap the kernel before it
 };
 // Rotation by several positions: pair i of a row turns by at[axis[i]][row] times freq[i] 2^-64 turns. at null: by
