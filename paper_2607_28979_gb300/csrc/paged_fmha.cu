@@ -348,6 +348,8 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
             break;
           }
           tc_fence_after();
+          float by = sl2;   // what takes the scores in tensor memory to base-2 exponents
+        again:
           uint32_t v[4][32];
 #pragma unroll
           for (int e = 0; e < 4; ++e) tmem_ld_32x32b_x32(tS + 32 * e, v[e]);
@@ -370,10 +372,28 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
             for (int k = 0; k < 16; ++k)
               mk[k & 7] = fmax3(mk[k & 7], __uint_as_float(v[e][2 * k]), __uint_as_float(v[e][2 * k + 1]));
           const float mx =
-              fmaxf(fmax3(mk[0], mk[1], mk[2]), fmax3(mk[3], mk[4], fmax3(mk[5], mk[6], mk[7]))) * sl2;
+              fmaxf(fmax3(mk[0], mk[1], mk[2]), fmax3(mk[3], mk[4], fmax3(mk[5], mk[6], mk[7]))) * by;
           const bool raise = mx > m + kTau;   // always where m = -inf and a key is seen
           const float alpha = (raise && m != -INFINITY) ? ex2_fast(m - mx) : 1.f;
-          if (__any_sync(0xffffffffu, alpha != 1.f)) {   // needs the products before in O
+          // From 2^28 on s sl2 - R may be far from 0 where s sl2, rounded, is R, and the weight of a row's best key 0 or
+          // infinite: such scores are worked out in place first, so that what is left to do is exact.
+          const bool far = by != 1.f && fabsf(mx) > 0x1p28f && mx != -INFINITY;
+          if (__any_sync(0xffffffffu, alpha != 1.f || far)) {
+            if (__any_sync(0xffffffffu, far)) {
+#pragma unroll 1
+              for (int e = 0; e < 8; ++e) {
+                uint32_t u[16];
+                tmem_ld_32x32b_x16(tS + 16 * e, u);
+                tmem_ld_wait(u);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) u[k] = __float_as_uint(__uint_as_float(u[k]) * sl2);
+                tmem_st_32x32b_x16(tS + 16 * e, u);
+              }
+              tmem_st_wait();
+              by = 1.f;
+              goto again;
+            }
+            // needs the products before in O
             if (!wait(&sh.pv_done[i], (t - 1) & 1u)) {
               ok = false;
               break;
@@ -392,7 +412,7 @@ __global__ void __launch_bounds__(Pf<D>::kThreads, 1)
           }
           if (raise) m = mx;
           const float mu = m == -INFINITY ? 0.f : m;
-          const uint64_t s2 = f32x2(sl2, sl2), nm2 = f32x2(-mu, -mu);
+          const uint64_t s2 = f32x2(by, by), nm2 = f32x2(-mu, -mu);
           // the sum of the weights as the product takes them: where one of them is most of it, its rounding cancels
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
