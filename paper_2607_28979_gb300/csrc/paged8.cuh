@@ -26,8 +26,8 @@ __device__ __forceinline__ float scale8(float top) {
 }
 
 // A page's scale x as it lay in memory: a caller may have written it. What is not a power of two in range is taken as the
-// one below (the end of the range beyond it), by every call alike, and reported. Asked some time after the load, which
-// is waited for there: asked beside it, 64 decoding steps of 100 to 16,384 positions take 58.1 us for 54.6.
+// one below (the end of the range beyond it), by every call alike, and reported. The question waits for the load: asked
+// beside it, 64 decoding steps of 100 to 16,384 positions took 58.1 us for 54.6.
 __device__ __forceinline__ bool is_scale8(float x) {
   const uint32_t u = __float_as_uint(x);
   return (u & 0x7FFFFFu) == 0 && u - (67u << 23) <= 120u << 23;

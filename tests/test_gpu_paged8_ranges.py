@@ -243,3 +243,21 @@ def test_scales_far_apart_in_chunks_of_two_streams(kind):
         q, out = _attend(c, [0], [new])
         P8.check_attention(c, [0], [new], q, out, label=kind)
     assert c.status() == M.MOT_OK
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("kind", ["tiles", "pages", "any"])
+def test_value_scales_far_apart_under_queries_far_from_their_keys(kind, new, d):
+    """Both at once: rows whose scores are worked out first (queries of 2^-66 and keys of 2^66) beside rows of zeros, in
+    tiles whose value scales lie further apart than a weight reaches."""
+    c = P8.Cache(q_heads=4, kv_heads=2, d=d, page=16, n_pages=60, max_pages=40)
+    c.reserve([0], [600])
+    c.ks[0, c.t[0]] = 2.0 ** 60
+    e = _exponents(kind, len(c.t[0]), c.gen).float()
+    c.vs[0, c.t[0]] = torch.exp2(torch.stack([e, e.flip(0)], 1))
+    q = c.normal(new, 4, d) * 2.0 ** -66
+    q[:, 1::2][new // 2:] = 0.0
+    _, out = _attend(c, [0], [new], q=q)
+    assert c.status() == M.MOT_OK
+    P8.check_attention(c, [0], [new], q, out, label=kind)
