@@ -33,7 +33,9 @@ constexpr int kDecTK = 32 * kWarps;
 // Units of a share, and what an item costs a CTA beside its units (its queries, the results' end: some microseconds). A
 // CTA whose run is many short items would finish last: one token of 28 heads on 4 for 64 sequences of 100 to 16,384
 // positions takes 48.3 us with three units for each, 65.8 with none, 49.0 with six; 64 of 4,096 take 55.5 for 55.0.
-// Pieces where they make no CTA's work much longer: contexts of 131,072 and 70,001 positions 46.2 us, 53.9 in runs.
+// Pieces where they make no CTA's work much longer: contexts of 131,072 and 70,001 positions 46.2 us, 53.9 in runs. Of one
+// tile at least: 517 positions of 12 heads on 2 take 10.0 us, with two 11.2, with four 12.7, 8,000 14.4, 15.0 and 16.5;
+// between them two are better, at 200 (8.4 us for 9.7) and at 2,000 (11.6 for 12.9).
 constexpr int kLeast = 1, kMost = 4, kPad = 3;
 constexpr float kTop = 15.f;   // weights are 2^15 at most: fp16 holds them down to 2^-40 of that, and many small ones count
 

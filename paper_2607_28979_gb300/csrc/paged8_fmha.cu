@@ -18,7 +18,7 @@
 //                                    the sum (w 2^-e beside 2^-e' of the row's largest), and are not flushed to 0.
 //                       Bound by the chain of products and softmax, with shared memory near its limit beside it (both parts
 //                       of Q and the keys are read from it twice, the values three times): 4,096 tokens of 28 heads on 4
-//                       of 128 on 32,768 positions 1,303 us (1,385 TFLOP/s; 1,175 were the values in fp16 already).
+//                       of 128 on 32,768 positions 1,287 us (1,402 TFLOP/s; a tenth less were the values in fp16 already).
 //                       Every wait is bounded; on a timeout the roles unwind, copies and MMAs in flight are drained,
 //                       TMEM is freed and kStatusTimeout is raised.
 #include "paged_chunk.cuh"
@@ -29,7 +29,7 @@ namespace {
 
 // Units of a share, as with 16-bit pages, and what an item costs beside its units: its queries and its end, about as
 // much as eight tiles, which a CTA with a run of short items has many times. 28 heads on 4, prompts of 2,111, 700 and 3,000
-// tokens from nothing: 174 us with eight, 176 with six, 178 with ten, 295 with none; a mixture with long contexts (500
+// tokens from nothing: 174 us with eight, 176 with six, 178 with ten, 295 with none (now 182); a mixture with long contexts (500
 // of 9,000, 2,111 of 2,500, 1,999 of 4,097, 48 of 700) 229, 249, 238 and 363.
 constexpr int kLeast = 1, kMost = 16, kPad = 8;
 
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(Pf8<D>::kThreads, 1)
   uint32_t k_issued = 0, k_par = 0, v_issued = 0, v_par = 0;
 
   if (warp < 4) {
-    // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; at 168 the softmax spills a row's scores (2,180 us for 1,313)
+    // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; at 168 the softmax spills a row's scores (2,180 us for 1,313 then)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 0) {
       // ------------------------------------------------ TMA producer
